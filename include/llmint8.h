@@ -230,6 +230,94 @@ int llmint8_zp_linear(const void *X_f16, int s, int h, float alpha, const int8_t
                       int8_t *Xq, int32_t *zc_x, void *Xo_f16, void *Out_f16, void *ws, size_t ws_bytes,
                       llmint8_stream_t stream);
 
+/* ---- 8-bit key/value cache and the attention that reads it ------------------------------------------------------------
+ * A decoder layer around the products above, with its cache in 8 bits: llmint8_kv_append puts the keys and values of new tokens
+ * into a paged cache (and rotates queries and keys by their positions on the way), llmint8_kv_attention computes the attention
+ * of query rows over the cache, llmint8_kv_read gives cached keys and values as fp16.
+ *
+ * The cache holds, per key/value head, blocks of LLMINT8_KV_BLOCK positions.  A full block is held as absmax codes (Section
+ * 2.1) with ONE constant c = max |x| (fp16) over its keys and one over its values: code = round-half-even(127 x / c), value
+ * c code / 127.  The positions behind the last full block are held as they came, fp16, in a ring of LLMINT8_KV_RING positions a
+ * sequence (position p at place p % LLMINT8_KV_RING), and become codes when their block is full: what is held depends on
+ * the tokens, not on how they were cut into calls.  A sequence may be shortened, by calling with a smaller kv_len, to any multiple
+ * of 32 positions, or to any length at most 32 below the greatest that it has had since it was last shortened to such a multiple
+ * (and not below that).
+ *
+ *   codes   [n_pages][heads][page_tokens / 32][2][32 * dpad] int8, dpad = d rounded up to 32: the tiles of a block's keys, then
+ *           those of its values, 32 positions x 32 features and 1 KiB each, features 0 .. 31 first; zero past d.
+ *           Keys: byte (position r, feature f) of a tile at (f / 16) * 512 + r * 16 + f % 16.
+ *           Values: at (r / 4 % 2) * 512 + f * 16 + r / 8 * 4 + r % 4.
+ *   consts  [n_pages][heads][page_tokens / 32][2] fp16: constants of keys and values of a block
+ *   ring    [n_slots][heads][2][LLMINT8_KV_RING][d] fp16: keys, values
+ * All three start on 16 bytes.  Nothing in them needs to start at zero.  Pages may be shared between sequences by full
+ * blocks that both have.
+ *
+ * A batch says which rows of a call belong to which sequence, and where these are in the cache:
+ *   row_start [n_seqs + 1]  sequence b has rows row_start[b] .. row_start[b+1] - 1 (none is allowed)
+ *   kv_len    [n_seqs]      its positions, those of the call's own tokens included: row i of its n is at position
+ *                           kv_len[b] - n + i.  0: the sequence is idle (append: its rows are left out)
+ *   pages     [n_seqs][page_stride]  its pages in order; entries past its length are not read
+ *   slots     [n_seqs]      its slot of the ring, one of its own; NULL: b
+ *   status    one word, or NULL: bits are set (never cleared) where the arrays hold what cannot be, which only the
+ *             device sees: LLMINT8_KV_BAD_BATCH for row_start, kv_len or slots out of range (or beyond max_rows, max_len, the
+ *             table's width, the rotation's table; append: fewer positions than rows): the sequence is left out, outputs zero;
+ *             LLMINT8_KV_BAD_PAGE for a page that does not exist: its positions are left out;
+ *             LLMINT8_KV_NOT_FINITE: a key or value was infinite or NaN, or became so by its rotation.  The cache holds
+ *             +-65504, or 0 for NaN, in its place, so that no other row's result is touched.
+ *   max_rows, max_len       at least the largest n and the largest kv_len: they size launches and workspace, results do not
+ *                           depend on them beyond the order of sums.                                                        */
+#define LLMINT8_KV_BLOCK 32
+#define LLMINT8_KV_RING 64
+#define LLMINT8_KV_MAX_D 256
+enum { LLMINT8_KV_BAD_BATCH = 1, LLMINT8_KV_BAD_PAGE = 2, LLMINT8_KV_NOT_FINITE = 4 };
+typedef struct {
+    int8_t *codes;
+    void *consts;
+    void *ring;
+    int n_pages, page_tokens, n_slots, heads, d;
+} llmint8_kv_cache_t;
+typedef struct {
+    const int32_t *row_start;
+    const int32_t *kv_len;
+    const int32_t *pages;
+    const int32_t *slots;
+    int32_t *status;
+    int n_seqs, n_rows, page_stride, max_rows, max_len;
+} llmint8_kv_batch_t;
+
+/* Bytes of the three arrays; 0 for sizes that are refused (page_tokens not a multiple of 32, d > LLMINT8_KV_MAX_D). */
+size_t llmint8_kv_codes_bytes(int n_pages, int page_tokens, int heads, int d);
+size_t llmint8_kv_consts_bytes(int n_pages, int page_tokens, int heads);
+size_t llmint8_kv_ring_bytes(int n_slots, int heads, int d);
+
+/* Puts keys and values of the batch's rows into the cache.
+ *   k, v     in   fp16, row r and head g at r * ld + g * d (a slice of a joint projection's output has ld of the whole)
+ *   q        in   NULL, or fp16 rows of heads_q heads, rotated like the keys into q_out (which may be q, if ld_q_out == ld_q)
+ *   cos, sin in   [n_pos][rot / 2] fp32, or NULL with rot 0 (no rotation): the first rot <= d features of a head are turned by
+ *                 pairs (a, b) -> (a cos - b sin, b cos + a sin), every operation rounded to fp32, the result to fp16.
+ *                 pairs 0: feature i with i + rot / 2; 1: feature 2 i with 2 i + 1                                          */
+int llmint8_kv_append(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *batch, const void *k_f16, int64_t ld_k,
+                      const void *v_f16, int64_t ld_v, const void *q_f16, int64_t ld_q, void *q_out_f16, int64_t ld_q_out,
+                      int heads_q, const float *cos, const float *sin, int n_pos, int rot, int pairs, llmint8_stream_t stream);
+
+/* out row of query head g = sum_j w_j v_j, w = softmax over j of scale * q . k_j, with the keys and values of head
+ * g / (heads_q / heads) at the positions j that the row sees: causal != 0: j up to its own position, else all kv_len; window > 0
+ * (causal only): no j further back than window - 1 before its own.  A row that sees nothing (kv_len smaller than its
+ * sequence's rows, an idle sequence) is zero.  scale >= 0.  Sums, maxima and weights are fp32; weights are rounded to fp16 for the
+ * matrix units, the result once to fp16.
+ *   q    in   fp16, row r and head g at r * ld_q + g * d;  heads_q a multiple of the cache's heads
+ *   out  out  fp16, the same with ld_out
+ *   ws        llmint8_kv_attention_workspace_bytes(batch, heads_q, heads, d) bytes; may be NULL where that is 0              */
+size_t llmint8_kv_attention_workspace_bytes(const llmint8_kv_batch_t *batch, int heads_q, int heads, int d);
+int llmint8_kv_attention(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *batch, const void *q_f16, int64_t ld_q,
+                         int heads_q, float scale, int causal, int window, void *out_f16, int64_t ld_out, void *ws,
+                         size_t ws_bytes, llmint8_stream_t stream);
+
+/* The keys and values at the batch's rows' positions as fp16 [n_rows][heads][d], c code / 127 rounded once, or as they came
+ * where their block is not full.  k_out or v_out may be NULL.  Rows of positions that do not exist are zero. */
+int llmint8_kv_read(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *batch, void *k_out_f16, void *v_out_f16,
+                    llmint8_stream_t stream);
+
 /* Measurement support: the ceilings the roofline fractions are held against, measured on the box itself.
  * llmint8_probe_mfma: one workgroup per compute unit runs a register-only issue loop of the int8 MFMA
  *   (16 x 16 x 64) in the shape of the prefill GEMM's main loop (Eq. 7: eight waves, 8 x 4 accumulator tiles each,

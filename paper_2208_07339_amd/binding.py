@@ -18,9 +18,22 @@ SYMBOLS = [
     "llmint8_export_rows", "llmint8_debug_prefill_tile", "llmint8_debug_prefill_tile_for",
     "llmint8_debug_decode_shape", "llmint8_debug_kernel_for", "llmint8_debug_mfma_for",
     "llmint8_debug_weight_reads_for",
+    "llmint8_kv_codes_bytes", "llmint8_kv_consts_bytes", "llmint8_kv_ring_bytes", "llmint8_kv_append",
+    "llmint8_kv_attention_workspace_bytes", "llmint8_kv_attention", "llmint8_kv_read",
 ]
 
 _lib = None
+
+
+class _KvCache(C.Structure):  # llmint8_kv_cache_t
+    _fields_ = [("codes", C.c_void_p), ("consts", C.c_void_p), ("ring", C.c_void_p), ("n_pages", C.c_int),
+                ("page_tokens", C.c_int), ("n_slots", C.c_int), ("heads", C.c_int), ("d", C.c_int)]
+
+
+class _KvBatch(C.Structure):  # llmint8_kv_batch_t
+    _fields_ = [("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("slots", C.c_void_p),
+                ("status", C.c_void_p), ("n_seqs", C.c_int), ("n_rows", C.c_int), ("page_stride", C.c_int),
+                ("max_rows", C.c_int), ("max_len", C.c_int)]
 
 
 class Llmint8Error(RuntimeError):
@@ -105,6 +118,21 @@ def lib():
     L.llmint8_debug_weight_reads_for.argtypes = [i32, i32, i32]
     L.llmint8_debug_decode_shape.restype = i32
     L.llmint8_debug_decode_shape.argtypes = [i32]
+    i64, cache, batch = C.c_int64, C.POINTER(_KvCache), C.POINTER(_KvBatch)
+    L.llmint8_kv_codes_bytes.restype = sz
+    L.llmint8_kv_codes_bytes.argtypes = [i32, i32, i32, i32]
+    L.llmint8_kv_consts_bytes.restype = sz
+    L.llmint8_kv_consts_bytes.argtypes = [i32, i32, i32]
+    L.llmint8_kv_ring_bytes.restype = sz
+    L.llmint8_kv_ring_bytes.argtypes = [i32, i32, i32]
+    L.llmint8_kv_append.restype = i32
+    L.llmint8_kv_append.argtypes = [cache, batch, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i32, i32, vp]
+    L.llmint8_kv_attention_workspace_bytes.restype = sz
+    L.llmint8_kv_attention_workspace_bytes.argtypes = [batch, i32, i32, i32]
+    L.llmint8_kv_attention.restype = i32
+    L.llmint8_kv_attention.argtypes = [cache, batch, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp]
+    L.llmint8_kv_read.restype = i32
+    L.llmint8_kv_read.argtypes = [cache, batch, vp, vp, vp]
     _lib = L
     return L
 
@@ -432,6 +460,140 @@ def zp_linear(X, qw, alpha, outl, rows, ws, out=None):
                                    _ptr(outl.idx), outl.cap, _ptr(outl.count), _ptr(outl.status), _ptr(rows.Xq),
                                    _ptr(rows.zc), _ptr(rows.Xo), _ptr(out), _ptr(ws.buf), ws.nbytes, _stream()))
     return out
+
+
+# ---- 8-bit key/value cache and its attention ----------------------------------------
+
+KV_BLOCK, KV_RING, KV_MAX_D = 32, 64, 256  # LLMINT8_KV_BLOCK / _RING / _MAX_D
+KV_BAD_BATCH, KV_BAD_PAGE, KV_NOT_FINITE = 1, 2, 4  # bits of a batch's status word
+
+
+@dataclass(frozen=True)
+class KvCache:
+    """Keys and values of a layer (llmint8_kv_cache_t; include/llmint8.h has the layout).  Holds the tensors it is made of."""
+    codes: object   # int8 device tensor [n_pages, heads, page_tokens / 32, 2, 32 * dpad]
+    consts: object  # fp16 [n_pages, heads, page_tokens / 32, 2]
+    ring: object    # fp16 [n_slots, heads, 2, 64, d]
+    page_tokens: int
+    d: int
+
+    def __post_init__(self):
+        torch = _torch()
+        dpad = (self.d + 31) // 32 * 32
+        n_pages, heads, blocks = self.codes.shape[:3]
+        assert self.codes.dtype == torch.int8 and self.consts.dtype == self.ring.dtype == torch.float16
+        assert self.page_tokens == blocks * KV_BLOCK and 1 <= self.d <= KV_MAX_D
+        assert tuple(self.codes.shape) == (n_pages, heads, blocks, 2, KV_BLOCK * dpad)
+        assert tuple(self.consts.shape) == (n_pages, heads, blocks, 2)
+        assert tuple(self.ring.shape) == (self.ring.shape[0], heads, 2, KV_RING, self.d)
+        for t in (self.codes, self.consts, self.ring):
+            assert t.is_cuda and t.is_contiguous() and t.device == self.codes.device
+        c = _KvCache(_ptr(self.codes), _ptr(self.consts), _ptr(self.ring), n_pages, self.page_tokens, self.ring.shape[0],
+                     heads, self.d)
+        object.__setattr__(self, "_c", c)
+
+    @property
+    def heads(self):
+        return self.codes.shape[1]
+
+    @staticmethod
+    def allocate(n_pages, page_tokens, n_slots, heads, d, device="cuda"):
+        torch = _torch()
+        assert page_tokens % KV_BLOCK == 0
+        dpad, blocks = (d + 31) // 32 * 32, page_tokens // KV_BLOCK
+        return KvCache(torch.empty((n_pages, heads, blocks, 2, KV_BLOCK * dpad), dtype=torch.int8, device=device),
+                       torch.empty((n_pages, heads, blocks, 2), dtype=torch.float16, device=device),
+                       torch.empty((n_slots, heads, 2, KV_RING, d), dtype=torch.float16, device=device), page_tokens, d)
+
+
+@dataclass(frozen=True)
+class KvBatch:
+    """Which rows of a call belong to which sequence, and where these are in the cache (llmint8_kv_batch_t).  The tensors'
+    contents may change from call to call, within max_rows and max_len."""
+    row_start: object  # int32 [n_seqs + 1]
+    kv_len: object     # int32 [n_seqs], the call's own tokens included
+    pages: object      # int32 [n_seqs, most pages of a sequence]
+    slots: object      # int32 [n_seqs], or None: sequence b has slot b
+    n_rows: int
+    max_rows: int
+    max_len: int
+    status: object = None  # int32 [1], or None
+
+    def __post_init__(self):
+        torch = _torch()
+        n = self.kv_len.numel()
+        given = [t for t in (self.row_start, self.kv_len, self.pages, self.slots, self.status) if t is not None]
+        assert all(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() for t in given)
+        assert all(t.device == self.kv_len.device for t in given)
+        assert self.row_start.numel() == n + 1 and self.pages.dim() == 2 and self.pages.shape[0] == n
+        assert self.slots is None or self.slots.numel() == n
+        c = _KvBatch(_ptr(self.row_start), _ptr(self.kv_len), _ptr(self.pages), _ptr(self.slots), _ptr(self.status), n,
+                     self.n_rows, self.pages.shape[1], self.max_rows, self.max_len)
+        object.__setattr__(self, "_c", c)
+
+
+def _head_rows(t, n_rows, d):
+    """Row stride of fp16 rows [n_rows, heads, d] whose heads lie one after the other."""
+    assert t.is_cuda and t.dtype == _torch().float16 and t.dim() == 3 and t.shape[0] == n_rows and t.shape[2] == d
+    rows, heads, one = t.stride()
+    assert (one == 1 or d == 1) and (heads == d or t.shape[1] == 1)
+    return rows if n_rows > 1 else max(rows, t.shape[1] * d)
+
+
+def kv_append(cache, batch, k, v, q=None, q_out=None, cos=None, sin=None, pairs=False):
+    """llmint8_kv_append: k, v [n_rows, heads, d] fp16 (rows may be slices of wider ones) into the cache; q [n_rows, heads_q, d],
+    if given, rotated like the keys into q_out, which is returned (made if not given; may be q).  cos, sin: fp32
+    [positions, rotated features / 2], or None: no rotation."""
+    torch = _torch()
+    n, d = batch.n_rows, cache.d
+    assert k.shape[1] == v.shape[1] == cache.heads
+    rot = n_pos = ld_q = ld_out = heads_q = 0
+    if cos is not None:
+        assert cos.is_cuda and sin.is_cuda and cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape
+        assert cos.dim() == 2 and cos.is_contiguous() and sin.is_contiguous()
+        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+    if q is not None:
+        heads_q = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((n, heads_q, d), dtype=torch.float16, device=q.device)
+        assert q_out.shape == q.shape
+        ld_q, ld_out = _head_rows(q, n, d), _head_rows(q_out, n, d)
+    _check(lib().llmint8_kv_append(C.byref(cache._c), C.byref(batch._c), _ptr(k), _head_rows(k, n, d), _ptr(v),
+                                   _head_rows(v, n, d), _ptr(q), ld_q, _ptr(q_out) if q is not None else None, ld_out, heads_q, _ptr(cos),
+                                   _ptr(sin), n_pos, rot, int(pairs), _stream()))
+    return q_out
+
+
+def kv_attention_workspace(cache, batch, heads_q):
+    """Scratch of kv_attention for this batch's sizes: kept from call to call and layer to layer."""
+    n = lib().llmint8_kv_attention_workspace_bytes(C.byref(batch._c), heads_q, cache.heads, cache.d)
+    return Workspace(_torch().empty(n, dtype=_torch().uint8, device=cache.codes.device))
+
+
+def kv_attention(cache, batch, q, scale=None, causal=True, window=0, ws=None, out=None):
+    """llmint8_kv_attention: q [n_rows, heads_q, d] fp16 over the cache -> out, the same shape.  scale: 1 / sqrt(d) if None."""
+    n, d, heads_q = batch.n_rows, cache.d, q.shape[1]
+    if out is None:
+        out = _torch().empty((n, heads_q, d), dtype=_torch().float16, device=q.device)
+    assert out.shape == q.shape
+    if ws is None:
+        ws = kv_attention_workspace(cache, batch, heads_q)
+    _check(lib().llmint8_kv_attention(C.byref(cache._c), C.byref(batch._c), _ptr(q), _head_rows(q, n, d), heads_q,
+                                      d ** -0.5 if scale is None else scale, int(causal), window, _ptr(out),
+                                      _head_rows(out, n, d), _ptr(ws.buf), ws.nbytes, _stream()))
+    return out
+
+
+def kv_read(cache, batch, k=None, v=None):
+    """llmint8_kv_read: keys and values at the batch's rows' positions, fp16 [n_rows, heads, d] each."""
+    torch = _torch()
+    shape = (batch.n_rows, cache.heads, cache.d)
+    if k is None and v is None:
+        k, v = (torch.empty(shape, dtype=torch.float16, device=cache.codes.device) for _ in range(2))
+    for t in (k, v):
+        assert t is None or (t.is_cuda and t.dtype == torch.float16 and tuple(t.shape) == shape and t.is_contiguous())
+    _check(lib().llmint8_kv_read(C.byref(cache._c), C.byref(batch._c), _ptr(k), _ptr(v), _stream()))
+    return k, v
 
 
 def export_weight(qw):

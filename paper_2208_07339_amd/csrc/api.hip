@@ -6,6 +6,7 @@
 
 #include "../../include/llmint8.h"
 #include "common.h"
+#include "kv.h"
 
 using namespace llmint8;
 
@@ -572,6 +573,86 @@ int llmint8_export_rows(const int8_t* Xq, int s, int h, int8_t* X_i8_rowmajor, l
 {
     if (!Xq || !X_i8_rowmajor || s < 1 || h < 1 || misaligned(Xq, 16)) return LLMINT8_INVALID_ARG;
     return hip_status(launch_export_tiled(Xq, s, h, X_i8_rowmajor, 1, (hipStream_t)stream));
+}
+
+// ---- 8-bit key/value cache ----
+
+size_t llmint8_kv_codes_bytes(int n_pages, int page_tokens, int heads, int d)
+{
+    if (n_pages < 1 || page_tokens < 1 || page_tokens % KV_BLOCK || heads < 1 || d < 1 || d > KV_MAX_D) return 0;
+    return (size_t)n_pages * heads * page_tokens * 2 * kv_dpad(d);
+}
+
+size_t llmint8_kv_consts_bytes(int n_pages, int page_tokens, int heads)
+{
+    if (n_pages < 1 || page_tokens < 1 || page_tokens % KV_BLOCK || heads < 1) return 0;
+    return (size_t)n_pages * heads * (page_tokens / KV_BLOCK) * 4;
+}
+
+size_t llmint8_kv_ring_bytes(int n_slots, int heads, int d)
+{
+    if (n_slots < 1 || heads < 1 || d < 1 || d > KV_MAX_D) return 0;
+    return (size_t)n_slots * heads * 2 * KV_RING * d * 2;
+}
+
+int llmint8_kv_append(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* batch, const void* k_f16, int64_t ld_k,
+                      const void* v_f16, int64_t ld_v, const void* q_f16, int64_t ld_q, void* q_out_f16, int64_t ld_q_out,
+                      int heads_q, const float* cos, const float* sin, int n_pos, int rot, int pairs, llmint8_stream_t stream)
+{
+    const int bad = kv_check(cache, batch);
+    if (bad) return bad;
+    if (!k_f16 || !v_f16 || misaligned(k_f16, 2) || misaligned(v_f16, 2) || rot < 0 || rot % 2 || rot > cache->d)
+        return LLMINT8_INVALID_ARG;
+    const int64_t wide = (int64_t)cache->heads * cache->d;
+    if (ld_k < wide || ld_v < wide) return LLMINT8_INVALID_ARG;
+    if (rot && (!cos || !sin || misaligned(cos, 4) || misaligned(sin, 4) || n_pos < 1)) return LLMINT8_INVALID_ARG;
+    if (q_f16) {
+        if (heads_q < 1 || !q_out_f16 || misaligned(q_f16, 2) || misaligned(q_out_f16, 2) || ld_q < (int64_t)heads_q * cache->d ||
+            ld_q_out < (int64_t)heads_q * cache->d || (q_f16 == q_out_f16 && ld_q != ld_q_out))
+            return LLMINT8_INVALID_ARG;
+        if (heads_q > 65535 - cache->heads) return LLMINT8_SHAPE;
+    }
+    KvAppend a = {k_f16, v_f16, q_f16, q_out_f16, ld_k, ld_v, ld_q, ld_q_out, heads_q, cos, sin, n_pos, rot, pairs != 0};
+    return hip_status(launch_kv_append(kv_args(cache, batch), a, (hipStream_t)stream));
+}
+
+size_t llmint8_kv_attention_workspace_bytes(const llmint8_kv_batch_t* batch, int heads_q, int heads, int d)
+{
+    if (!batch || batch->n_seqs < 1 || batch->n_rows < 1 || batch->max_rows < 1 || batch->max_len < 0 || heads < 1 || heads_q < heads ||
+        heads_q % heads || d < 1 || d > KV_MAX_D)
+        return 0;
+    Kv p = {};
+    p.heads = heads, p.d = d, p.n_seqs = batch->n_seqs, p.n_rows = batch->n_rows, p.max_len = batch->max_len;
+    p.max_rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
+    return kv_attention_ws(kv_plan(p, heads_q), p.n_rows, heads_q, d);
+}
+
+int llmint8_kv_attention(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* batch, const void* q_f16, int64_t ld_q,
+                         int heads_q, float scale, int causal, int window, void* out_f16, int64_t ld_out, void* ws,
+                         size_t ws_bytes, llmint8_stream_t stream)
+{
+    const int bad = kv_check(cache, batch);
+    if (bad) return bad;
+    if (!q_f16 || !out_f16 || misaligned(q_f16, 2) || misaligned(out_f16, 2) || heads_q < 1 || heads_q % cache->heads ||
+        !std::isfinite(scale) || scale < 0.0f || window < 0 || (window && !causal))
+        return LLMINT8_INVALID_ARG;
+    if (ld_q < (int64_t)heads_q * cache->d || ld_out < (int64_t)heads_q * cache->d) return LLMINT8_INVALID_ARG;
+    if ((int64_t)heads_q * batch->n_rows > KV_MAX_LEN || (int64_t)cache->heads * batch->n_seqs > KV_MAX_LEN) return LLMINT8_SHAPE;
+    const Kv p = kv_args(cache, batch);
+    const KvPlan plan = kv_plan(p, heads_q);
+    const size_t need = kv_attention_ws(plan, p.n_rows, heads_q, p.d);
+    if (need && (!ws || ws_bytes < need)) return LLMINT8_WORKSPACE;
+    KvAttend a = {q_f16, out_f16, ld_q, ld_out, heads_q, scale, causal != 0, window};
+    return hip_status(launch_kv_attention(p, a, plan, need ? ws_base(ws) : nullptr, (hipStream_t)stream));
+}
+
+int llmint8_kv_read(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* batch, void* k_out_f16, void* v_out_f16,
+                    llmint8_stream_t stream)
+{
+    const int bad = kv_check(cache, batch);
+    if (bad) return bad;
+    if ((!k_out_f16 && !v_out_f16) || misaligned(k_out_f16, 2) || misaligned(v_out_f16, 2)) return LLMINT8_INVALID_ARG;
+    return hip_status(launch_kv_read(kv_args(cache, batch), k_out_f16, v_out_f16, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,679 @@
+// Attention over the 8-bit key/value cache (layout: kv.h).
+//
+// With codes k, v, constants c_k, c_v of a block, x_j = scale c_k / 127 (q . k_j), w_j = exp(x_j - m) / l over the positions j that
+// a row sees, m = max x_j, l = sum exp(x_j - m):  out = sum_j w_j c_v / 127 v_j.  One pass over the positions with a running
+// m and l; what has been summed is scaled by exp(m_old - m_new) when the maximum grows.  Exponentials are taken to base 2, log2(e)
+// being in the scale.
+//
+// Both products are fp16 MFMAs (32 x 32 x 16) with fp32 sums.  Codes are exact in fp16: 0x6400 + u is the fp16 number 1024 + u, so a
+// byte permutation and a packed subtraction make two values of two codes.  Rows of queries are the N side of both products, S^T = K
+// Q^T and O^T = V^T P^T: a lane has one row of queries, so maximum, sum and scaling need one exchange between the lane's two halves,
+// and the scores a lane has computed are the operand of the second product as they are (kv.h).
+#include "kv.h"
+
+namespace llmint8 {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOWEST = -3.0e38f;  // below every score, finite: exp2(-inf - LOWEST) is 0, where -inf - -inf would be NaN
+
+__device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// eight codes as fp16
+__device__ __forceinline__ h8 codes8(unsigned a, unsigned b)
+{
+    const h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    a ^= 0x80808080u, b ^= 0x80808080u;
+    auto two = [&](unsigned w, unsigned sel) { return __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, sel)) - off; };
+    const h2 p = two(a, 0x04010400u), q = two(a, 0x04030402u), r = two(b, 0x04010400u), t = two(b, 0x04030402u);
+    return h8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
+}
+
+__device__ __forceinline__ h8 pack8(const float* p, float f)
+{
+    h8 r;
+#pragma unroll
+    for (int e = 0; e < 8; e++) r[e] = (_Float16)(p[e] * f);
+    return r;
+}
+
+struct AttendArgs {
+    Kv kv;
+    const _Float16* q;
+    _Float16* out;
+    long long ld_q, ld_out;
+    int heads_q, group;  // group: query heads to a key head
+    float scale;         // log2(e) included
+    int causal, window;
+    int splits;
+    float* part;   // [split][row * heads_q + head][d] sums, not divided
+    float2* stat;  // [split][row * heads_q + head] (m, l)
+    bool vec;      // d and the rows of q allow 16-byte accesses
+};
+
+// features f .. f + 7 of a row of d
+__device__ __forceinline__ h8 q8(const _Float16* row, int f, int d, bool vec)
+{
+    if (vec) return f < d ? *(const h8*)(row + f) : h8{};
+    h8 r;
+#pragma unroll
+    for (int e = 0; e < 8; e++) r[e] = f + e < d ? row[f + e] : (_Float16)0.0f;
+    return r;
+}
+
+// Operand B of the score product for one row of queries: features 32 g + 16 (lane / 32) + 8 t .. of step 2 g + t
+template <int DP>
+__device__ __forceinline__ void load_q(const AttendArgs& a, const KvSeq& s, int head, int r, int hh, h8 (&qf)[DP / 16])
+{
+    if (r < s.n * a.group) {
+        const _Float16* row = a.q + (s.row0 + r / a.group) * a.ld_q + (long long)(head * a.group + r % a.group) * a.kv.d;
+#pragma unroll
+        for (int t = 0; t < DP / 16; t++) qf[t] = q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), a.kv.d, a.vec);
+    } else {
+#pragma unroll
+        for (int t = 0; t < DP / 16; t++) qf[t] = h8{};
+    }
+}
+
+// Positions that a row at `pos` sees: lo .. hi - 1 (none if hi <= lo)
+__device__ __forceinline__ void seen(const AttendArgs& a, int len, int pos, int& lo, int& hi)
+{
+    hi = !a.causal ? len : pos < 0 ? 0 : pos + 1;
+    lo = a.window && pos >= a.window ? pos - a.window + 1 : 0;
+}
+
+// A power of two that is at least x > 0 (fp32)
+__device__ __forceinline__ float power_above(float x)
+{
+    const unsigned b = __builtin_bit_cast(unsigned, x);
+    return __builtin_bit_cast(float, (b + 0x007fffffu) & 0xff800000u);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
+// every wave blocks of its own; sums meet in LDS.  Bound by HBM.  The values' codes stay exact, their constant is a factor of the
+// weights: relative to `ref`, a power of two that is at least every constant so far, so that the products keep the
+// precision of fp16 whatever the values' size.
+// ---------------------------------------------------------------------------------------------------------------------------
+template <int DP>
+__global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
+{
+    constexpr int NT = DP / 32;
+    __shared__ float s_o[4][32][33];
+    __shared__ float s_m[4][32], s_l[4][32];
+    const Kv& p = a.kv;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
+    const int head = blockIdx.x % p.heads, b = blockIdx.x / p.heads, split = blockIdx.y;
+    KvSeq s;
+    const bool ok = kv_seq(p, b, s);
+    if (!ok && tid == 0) kv_flag(p, LLMINT8_KV_BAD_BATCH);
+    const int rows = s.n * a.group;  // <= 32
+    if (rows == 0) return;
+
+    // blocks that some row sees, and this workgroup's part of them
+    int lo, hi, first, end, x0, x1;
+    seen(a, s.len, s.len - 1, x0, hi);
+    seen(a, s.len, s.len - s.n, lo, x1);
+    first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
+    const int chunk = (end - first + a.splits - 1) / a.splits;
+    const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
+    const int closed = s.len / KV_BLOCK;  // blocks held as codes
+    const int k1 = c1 < closed ? c1 : closed;
+
+    h8 qf[DP / 16];
+    load_q<DP>(a, s, head, qr, hh, qf);
+    int rlo, rhi;  // what this lane's row sees
+    seen(a, s.len, s.len - s.n + qr / a.group, rlo, rhi);
+    // blocks before / behind which a mask is needed: that of the last row's start, of the first row's end
+    int all_lo, all_hi;
+    seen(a, s.len, s.len - 1, all_lo, x1);
+    seen(a, s.len, s.len - s.n, x0, all_hi);
+
+    f16v o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) o[t] = f16v{};
+    float m = LOWEST, l = 0.0f, ref = 0.0f;
+
+    auto rescale = [&](float f) {
+#pragma unroll
+        for (int t = 0; t < NT; t++) o[t] *= f;
+    };
+    auto new_ref = [&](float c) {
+        const float r = power_above(c);
+        if (ref > 0.0f) rescale(ref / r);
+        ref = r;
+    };
+    // weights of a block from its scores, as the two operands of the second product, times f
+    auto weights = [&](f16v sc, float ks, int blk, float f, h8 (&pf)[2]) {
+        float x[16], mx = LOWEST;
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = sc[i] * ks;
+        if (blk * KV_BLOCK < all_lo || blk * KV_BLOCK + KV_BLOCK > all_hi) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int pos = blk * KV_BLOCK + 8 * (i >> 2) + 4 * hh + (i & 3);
+                if (pos < rlo || pos >= rhi) x[i] = -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) mx = fmaxf(mx, x[i]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__any(mx > m)) {
+            const float n = fmaxf(m, mx), f = exp2_(m - n);
+            l *= f;
+            rescale(f);
+            m = n;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            x[i] = exp2_(x[i] - m);
+            l += x[i];
+        }
+        pf[0] = pack8(x, f), pf[1] = pack8(x + 8, f);
+    };
+
+    // The wave's blocks: c0 + w, c0 + w + 4, ...  Lane i looks up the i-th of the next 64.
+    const int nb = k1 > c0 + w ? (k1 - c0 - w + 3) / 4 : 0;
+    u4 kc[NT], vc[NT], kn[NT], vn[NT];
+    long long at = -1;
+    unsigned cc = 0;
+    auto look_up = [&](int i0) {
+        const int i = i0 + lane;
+        at = -1, cc = 0;
+        if (i < nb) {
+            at = kv_block(p, b, head, c0 + w + 4 * i);
+            if (at >= 0) cc = p.consts[at];
+            else kv_flag(p, LLMINT8_KV_BAD_PAGE);
+        }
+    };
+    auto at_of = [&](int i) {
+        return (long long)__builtin_amdgcn_readlane((int)(at >> 32), i & 63) << 32 |
+               (unsigned)__builtin_amdgcn_readlane((int)at, i & 63);
+    };
+    auto request = [&](long long n, u4 (&k)[NT], u4 (&v)[NT]) {
+        if (n < 0) return;
+        const u4* src = (const u4*)(p.codes + n * (2 * KV_BLOCK * DP)) + lane;
+#pragma unroll
+        for (int t = 0; t < NT; t++) k[t] = __builtin_nontemporal_load(src + 64 * t);
+#pragma unroll
+        for (int t = 0; t < NT; t++) v[t] = __builtin_nontemporal_load(src + 64 * (NT + t));
+    };
+    long long next = -1;
+    if (nb > 0) {
+        look_up(0);
+        next = at_of(0);
+        request(next, kn, vn);
+    }
+    for (int i = 0; i < nb; i++) {
+        const bool there = next >= 0;
+        const unsigned c = __builtin_amdgcn_readlane((int)cc, i & 63);
+#pragma unroll
+        for (int t = 0; t < NT; t++) kc[t] = kn[t], vc[t] = vn[t];
+        if (i + 1 < nb) {
+            if (((i + 1) & 63) == 0) look_up(i + 1);
+            next = at_of(i + 1);
+            request(next, kn, vn);
+        }
+        if (!there) continue;
+        const float ck = f16_bits_to_float((unsigned short)(c & 0xffffu)), cv = f16_bits_to_float((unsigned short)(c >> 16));
+        f16v sc = {};
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            sc = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc);
+            sc = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc);
+        }
+        if (cv > ref) new_ref(cv);
+        h8 pf[2];
+        weights(sc, ck * (1.0f / 127.0f) * a.scale, c0 + w + 4 * i, ref > 0.0f ? cv / ref : 0.0f, pf);
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0], o[t]);
+            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[1], o[t]);
+        }
+    }
+    // The open block, fp16: by the wave whose turn it is.  Values in units of ref / 128, weights times 127 / 128, as if they were codes.
+    if (closed >= c0 && closed < c1 && ((closed - c0) & 3) == w) {
+        const int d = p.d, base = closed * KV_BLOCK;
+        f16v sc = {};
+        const bool there = base + qr < s.len;
+        const _Float16* row = (const _Float16*)kv_ring_row(p, s.slot, head, 0, base + qr);
+#pragma unroll
+        for (int t = 0; t < DP / 16; t++)
+            sc = mfma(there ? q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), d, d % 8 == 0) : h8{}, qf[t], sc);
+        unsigned short v[NT][16], big = 0;
+        const unsigned short* vals = kv_ring_row(p, s.slot, head, 1, base);
+#pragma unroll
+        for (int t = 0; t < NT; t++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int r = 8 * (i >> 2) + 4 * hh + (i & 3), f = 32 * t + qr;
+                v[t][i] = base + r < s.len && f < d ? vals[r * d + f] : (unsigned short)0;
+                const unsigned short y = v[t][i] & 0x7fffu;
+                big = y > big ? y : big;
+            }
+        int top = big;
+#pragma unroll
+        for (int x = 32; x; x >>= 1) {
+            const int y = __shfl_xor(top, x);
+            top = y > top ? y : top;
+        }
+        const float cv = f16_bits_to_float((unsigned short)top);
+        if (cv > ref) new_ref(cv);
+        if (ref == 0.0f) ref = 1.0f;
+        const float unit = 128.0f / ref;
+        h8 pf[2];
+        weights(sc, a.scale, closed, 127.0f / 128.0f, pf);
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            float y[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) y[i] = f16_bits_to_float(v[t][i]);
+            o[t] = mfma(pack8(y, unit), pf[0], o[t]);
+            o[t] = mfma(pack8(y + 8, unit), pf[1], o[t]);
+        }
+    }
+
+    // ---- join the four waves
+    l += __shfl_xor(l, 32);
+    if (hh == 0) s_m[w][qr] = m, s_l[w][qr] = l;
+    __syncthreads();
+    {
+        const float top = fmaxf(fmaxf(s_m[0][qr], s_m[1][qr]), fmaxf(s_m[2][qr], s_m[3][qr]));
+        rescale(exp2_(m - top) * ref * (1.0f / 127.0f));
+    }
+    const long long total = (long long)p.n_rows * a.heads_q;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        if (qr < rows)
+#pragma unroll
+            for (int i = 0; i < 16; i++) s_o[w][8 * (i >> 2) + 4 * hh + (i & 3)][qr] = o[t][i];
+        __syncthreads();
+        for (int x = tid; x < 32 * rows; x += 256) {
+            const int f = x & 31, r = x >> 5;
+            const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+            float sum = 0.0f, den = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                sum += s_o[q][f][r];
+                den += s_l[q][r] * exp2_(s_m[q][r] - top);
+            }
+            const long long row = s.row0 + r / a.group;
+            const int g = head * a.group + r % a.group;
+            if (32 * t + f < p.d) {
+                if (a.splits == 1)
+                    a.out[row * a.ld_out + (long long)g * p.d + 32 * t + f] = (_Float16)(den != 0.0f ? sum / den : 0.0f);
+                else if (den != 0.0f)
+                    a.part[((long long)split * total + row * a.heads_q + g) * p.d + 32 * t + f] = sum;
+            }
+            if (t == 0 && f == 0 && a.splits > 1) a.stat[split * total + row * a.heads_q + g] = make_float2(top, den);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// Many rows: a workgroup takes a tile of 4 x 32 QT rows (tokens, and for each the query heads that share its keys), its waves the
+// same blocks of the cache two at a time from LDS, where they lie as fp16 in operand order: codes are converted once for all rows.
+// The values there are whole (code c_v / 127 rounded to fp16, as llmint8_kv_read gives them), the keys codes, their constant a factor of
+// the scores.  Bound by the matrix units and by what makes scores weights.
+// ---------------------------------------------------------------------------------------------------------------------------
+template <int DP, int QT>
+__global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
+{
+    constexpr int NT = DP / 32, ROWS = 128 * QT;
+    constexpr int PER = DP * 8 / 256;                           // 16-byte pieces of two blocks' codes to a thread
+    extern __shared__ __align__(16) _Float16 lds[];             // [2][keys, values][2 blocks][DP * 32]
+    constexpr int BUF = 2 * 2 * DP * 32;
+    __shared__ float s_ks[2][2];
+    const Kv& p = a.kv;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
+    const int head = blockIdx.x % p.heads, split = blockIdx.y;  // the heads of a tile one after the other: with a multiple of 8
+                                                                // heads, a head's tiles all run on one XCD and share its L2
+    bool wrong = false;
+    auto tiles = [&](int q) {
+        KvSeq s;
+        if (!kv_seq(p, q, s)) wrong = true;
+        return (s.n * a.group + ROWS - 1) / ROWS;
+    };
+    int b, tile;
+    const bool found = kv_find(p.n_seqs, blockIdx.x / p.heads, tiles, b, tile);
+    if (wrong) kv_flag(p, LLMINT8_KV_BAD_BATCH);
+    if (!found) return;
+    KvSeq s;
+    kv_seq(p, b, s);
+    const int rows = s.n * a.group, old = s.len - s.n;
+    tile = (rows + ROWS - 1) / ROWS - 1 - tile;  // those that see most first
+    const int r0 = tile * ROWS, r1 = r0 + ROWS < rows ? r0 + ROWS : rows;
+    const int w0 = r0 + w * 32 * QT, w1 = w0 + 32 * QT < r1 ? w0 + 32 * QT : r1;  // this wave's rows
+
+    int lo, hi, x0, x1;
+    seen(a, s.len, old + r0 / a.group, lo, x1);
+    seen(a, s.len, old + (r1 - 1) / a.group, x0, hi);
+    const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
+    const int chunk = ((end - first + a.splits - 1) / a.splits + 1) & ~1;
+    const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
+    const int closed = s.len / KV_BLOCK;
+    // what the wave's rows see: some of them, and all of them
+    int some_lo = 0, some_hi = 0, all_lo = 0, all_hi = 0;
+    if (w0 < w1) {
+        seen(a, s.len, old + w0 / a.group, some_lo, all_hi);
+        seen(a, s.len, old + (w1 - 1) / a.group, all_lo, some_hi);
+    }
+
+    h8 qf[QT][DP / 16];
+    int rlo[QT], rhi[QT];
+#pragma unroll
+    for (int t = 0; t < QT; t++) {
+        const int r = w0 + 32 * t + qr;
+        load_q<DP>(a, s, head, r, hh, qf[t]);
+        seen(a, s.len, old + r / a.group, rlo[t], rhi[t]);
+    }
+    f16v o[QT][NT];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int t = 0; t < QT; t++) {
+        m[t] = LOWEST, l[t] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < NT; x++) o[t][x] = f16v{};
+    }
+
+    // ---- two blocks from the cache: requested as 16-byte pieces of codes, later converted into LDS
+    u4 piece[PER];
+    float pc[PER];  // constant of a piece's block
+    // numbers of the stage's two blocks in codes; -1: none, or none held as codes
+    auto blocks_of = [&](int blk, long long (&at)[2]) {
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+            at[x] = -1;
+            if (blk + x < c1 && blk + x < closed) {
+                at[x] = kv_block(p, b, head, blk + x);
+                if (at[x] < 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
+            }
+        }
+    };
+    float ks_next[2];
+    auto request = [&](int blk) {
+        long long at[2];
+        blocks_of(blk, at);
+        float cv[2];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+            const unsigned c = at[x] >= 0 ? p.consts[at[x]] : 0u;
+            ks_next[x] = at[x] >= 0 ? f16_bits_to_float((unsigned short)(c & 0xffffu)) * (1.0f / 127.0f) * a.scale : -1.0f;
+            cv[x] = f16_bits_to_float((unsigned short)(c >> 16)) * (1.0f / 127.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < PER; j++) {
+            const int t = tid + 256 * j, x = t >= DP * 4, u = t - x * DP * 4;
+            pc[j] = cv[x];
+            piece[j] = u4{0x0u, 0x0u, 0x0u, 0x0u};
+            if (at[x] >= 0) piece[j] = *((const u4*)(p.codes + at[x] * (2 * KV_BLOCK * DP)) + u);
+        }
+    };
+    auto deposit = [&](int buf, int blk) {
+        _Float16* const base = lds + buf * BUF;
+#pragma unroll
+        for (int j = 0; j < PER; j++) {
+            const int t = tid + 256 * j, x = t >= DP * 4, u = t - x * DP * 4;
+            const bool value = u >= DP * 2;
+            const int g = (value ? u - DP * 2 : u) >> 6, ln = u & 63;
+            h8 y[2];
+            if (blk + x == closed && blk + x < c1) {  // the open block: fp16 from the ring
+                const int d = p.d, r = ln & 31, h2_ = ln >> 5, base_pos = closed * KV_BLOCK;
+                if (!value) {
+                    const _Float16* row = (const _Float16*)kv_ring_row(p, s.slot, head, 0, base_pos + r);
+                    const bool there = base_pos + r < s.len;
+                    y[0] = there ? q8(row, 32 * g + 16 * h2_, d, d % 8 == 0) : h8{};
+                    y[1] = there ? q8(row, 32 * g + 16 * h2_ + 8, d, d % 8 == 0) : h8{};
+                } else {
+                    const _Float16* vals = (const _Float16*)kv_ring_row(p, s.slot, head, 1, base_pos);
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const int q = 8 * (i >> 2) + 4 * h2_ + (i & 3), f = 32 * g + r;
+                        y[i >> 3][i & 7] = base_pos + q < s.len && f < d ? vals[q * d + f] : (_Float16)0.0f;
+                    }
+                }
+            } else if (!value) {
+                y[0] = codes8(piece[j][0], piece[j][1]), y[1] = codes8(piece[j][2], piece[j][3]);
+            } else {
+                float f[16];
+#pragma unroll
+                for (int i = 0; i < 16; i++) f[i] = (float)(int8_t)(piece[j][i >> 2] >> (8 * (i & 3)));
+                y[0] = pack8(f, pc[j]), y[1] = pack8(f + 8, pc[j]);
+            }
+            h8* dst = (h8*)(base + (value ? 2 * DP * 32 : 0) + x * DP * 32) + 2 * g * 64 + ln;
+            dst[0] = y[0], dst[64] = y[1];
+        }
+        if (tid < 2) s_ks[buf][tid] = blk + tid == closed && blk + tid < c1 ? a.scale : tid ? ks_next[1] : ks_next[0];
+    };
+
+    const int stages = c1 > c0 ? (c1 - c0 + 1) / 2 : 0;
+    if (stages) {
+        request(c0);
+        deposit(0, c0);
+        if (stages > 1) request(c0 + 2);
+        __syncthreads();
+    }
+    for (int st = 0; st < stages; st++) {
+        const int blk = c0 + 2 * st, buf = st & 1;
+        const _Float16* const base = lds + buf * BUF;
+        if (blk * KV_BLOCK < some_hi && (blk + 2) * KV_BLOCK > some_lo) {
+            f16v sc[QT][2];
+#pragma unroll
+            for (int t = 0; t < QT; t++) sc[t][0] = sc[t][1] = f16v{};
+#pragma unroll
+            for (int x = 0; x < 2; x++)
+#pragma unroll
+                for (int g = 0; g < DP / 16; g++) {
+                    const h8 k = *((const h8*)(base + x * DP * 32) + g * 64 + lane);
+#pragma unroll
+                    for (int t = 0; t < QT; t++) sc[t][x] = mfma(k, qf[t][g], sc[t][x]);
+                }
+            const float ks[2] = {s_ks[buf][0], s_ks[buf][1]};
+            const bool mask = blk * KV_BLOCK < all_lo || (blk + 2) * KV_BLOCK > all_hi || ks[0] < 0.0f || ks[1] < 0.0f;
+            h8 pf[QT][2][2];
+#pragma unroll
+            for (int t = 0; t < QT; t++) {
+                float x[2][16], mx = LOWEST;
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[y][i] = sc[t][y][i] * ks[y];
+                    if (mask)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            const int pos = (blk + y) * KV_BLOCK + 8 * (i >> 2) + 4 * hh + (i & 3);
+                            if (pos < rlo[t] || pos >= rhi[t] || ks[y] < 0.0f) x[y][i] = -__builtin_inff();
+                        }
+#pragma unroll
+                    for (int i = 0; i < 16; i++) mx = fmaxf(mx, x[y][i]);
+                }
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                if (__any(mx > m[t])) {
+                    const float n = fmaxf(m[t], mx), f = exp2_(m[t] - n);
+                    l[t] *= f;
+                    m[t] = n;
+#pragma unroll
+                    for (int q = 0; q < NT; q++) o[t][q] *= f;
+                }
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        x[y][i] = exp2_(x[y][i] - m[t]);
+                        l[t] += x[y][i];
+                    }
+                    pf[t][y][0] = pack8(x[y], 1.0f), pf[t][y][1] = pack8(x[y] + 8, 1.0f);
+                }
+            }
+            const h8* const vb = (const h8*)(base + 2 * DP * 32) + lane;
+#pragma unroll
+            for (int x = 0; x < 2; x++)
+#pragma unroll
+                for (int q = 0; q < NT; q++)
+#pragma unroll
+                    for (int y = 0; y < 2; y++) {
+                        const h8 v = vb[x * DP * 4 + (2 * q + y) * 64];
+#pragma unroll
+                        for (int t = 0; t < QT; t++) o[t][q] = mfma(v, pf[t][x][y], o[t][q]);
+                    }
+        }
+        if (st + 1 < stages) {
+            deposit(buf ^ 1, blk + 2);
+            if (st + 2 < stages) request(blk + 4);
+        }
+        __syncthreads();
+    }
+
+    const long long total = (long long)p.n_rows * a.heads_q;
+#pragma unroll
+    for (int t = 0; t < QT; t++) {
+        const float den = l[t] + __shfl_xor(l[t], 32);
+        const int r = w0 + 32 * t + qr;
+        if (r >= r1) continue;
+        const long long row = s.row0 + r / a.group;
+        const int g = head * a.group + r % a.group;
+        if (a.splits > 1) {
+            if (hh == 0) a.stat[split * total + row * a.heads_q + g] = make_float2(m[t], den);
+            if (den != 0.0f) {
+                float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
+#pragma unroll
+                for (int q = 0; q < NT; q++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const int f = 32 * q + 8 * (i >> 2) + 4 * hh + (i & 3);
+                        if (f < p.d) dst[f] = o[t][q][i];
+                    }
+            }
+        } else {
+            _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d;
+            const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+#pragma unroll
+            for (int q = 0; q < NT; q++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const int f = 32 * q + 8 * j + 4 * hh;
+                    h4 y;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) y[e] = (_Float16)(o[t][q][4 * j + e] * inv);
+                    if (a.vec) {
+                        if (f < p.d) *(h4*)(dst + f) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (f + e < p.d) dst[f + e] = y[e];
+                    }
+                }
+        }
+    }
+}
+
+// Joins the splits: one wave to a row and head.
+__global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
+{
+    const long long total = (long long)a.kv.n_rows * a.heads_q, x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (x >= total) return;
+    const int lane = threadIdx.x & 63, d = a.kv.d;
+    float top = LOWEST;
+    for (int s = 0; s < a.splits; s++) {
+        const float2 t = a.stat[s * total + x];
+        if (t.y != 0.0f) top = fmaxf(top, t.x);
+    }
+    float sum[KV_MAX_D / 64] = {}, den = 0.0f;
+    for (int s = 0; s < a.splits; s++) {
+        const float2 t = a.stat[s * total + x];
+        if (t.y == 0.0f) continue;
+        const float f = exp2_(t.x - top);
+        den += f * t.y;
+        const float* src = a.part + (s * total + x) * d;
+#pragma unroll
+        for (int q = 0; q < KV_MAX_D / 64; q++)
+            if (lane + 64 * q < d) sum[q] += f * src[lane + 64 * q];
+    }
+    _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d;
+#pragma unroll
+    for (int q = 0; q < KV_MAX_D / 64; q++)
+        if (lane + 64 * q < d) dst[lane + 64 * q] = (_Float16)(den != 0.0f ? sum[q] / den : 0.0f);
+}
+
+template <int DP>
+hipError_t launch_step(const AttendArgs& a, hipStream_t st)
+{
+    kv_step_kernel<DP><<<dim3(a.kv.heads * a.kv.n_seqs, a.splits), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int DP, int QT>
+hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
+{
+    constexpr int bytes = 2 * 2 * 2 * DP * 32 * 2;
+    if (bytes + sizeof(float) * 4 > 65536) {  // with the static part
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, QT>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    kv_prompt_kernel<DP, QT><<<dim3(tiles * a.kv.heads, a.splits), 256, bytes, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+constexpr int KV_STEP_ROWS = 32;
+
+KvPlan kv_plan(const Kv& p, int heads_q)
+{
+    KvPlan r;
+    const long long group = heads_q / p.heads, rows = p.max_rows * group;
+    const int blocks = (p.max_len + KV_BLOCK - 1) / KV_BLOCK;
+    long long units;
+    if (rows <= KV_STEP_ROWS) {
+        r.tile = KV_STEP_ROWS, r.tiles = 0;
+        units = (long long)p.n_seqs * p.heads;
+    } else {
+        r.tile = 128;
+        const long long x = ((long long)p.n_rows * group + (long long)p.n_seqs * (r.tile - 1)) / r.tile, y = p.n_seqs * ((rows + r.tile - 1) / r.tile);
+        r.tiles = (int)(x < y ? x : y);
+        units = (long long)r.tiles * p.heads;
+    }
+    const long long want = 1024 / units, most = blocks / 8;
+    r.splits = (int)(want < most ? want : most);
+    if (r.splits < 1) r.splits = 1;
+    return r;
+}
+
+size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d)
+{
+    return plan.splits > 1 ? (size_t)plan.splits * n_rows * heads_q * (4 * (size_t)d + 8) + 512 : 0;
+}
+
+hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& plan, void* ws, hipStream_t st)
+{
+    AttendArgs a;
+    a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
+    a.group = c.heads_q / p.heads, a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = plan.splits;
+    const size_t total = (size_t)p.n_rows * c.heads_q;
+    a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));
+    a.vec = p.d % 8 == 0 && ((((uintptr_t)c.q | (uintptr_t)c.out) & 15) | (c.ld_q & 7) | (c.ld_out & 7)) == 0;
+    const int dp = kv_dpad(p.d);
+    hipError_t e;
+    auto pick = [&](auto w) {
+        constexpr int DP = decltype(w)::value;
+        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st) : launch_prompt<DP, 1>(a, plan.tiles, st);
+    };
+    switch (dp) {
+        case 32: e = pick(std::integral_constant<int, 32>()); break;
+        case 64: e = pick(std::integral_constant<int, 64>()); break;
+        case 96: e = pick(std::integral_constant<int, 96>()); break;
+        case 128: e = pick(std::integral_constant<int, 128>()); break;
+        case 160: e = pick(std::integral_constant<int, 160>()); break;
+        case 192: e = pick(std::integral_constant<int, 192>()); break;
+        case 224: e = pick(std::integral_constant<int, 224>()); break;
+        default: e = pick(std::integral_constant<int, 256>()); break;
+    }
+    if (e != hipSuccess || plan.splits == 1) return e;
+    kv_join_kernel<<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace llmint8
