@@ -1,9 +1,11 @@
 // Attention over the 8-bit key/value cache (layout: kv.h).
 //
 // With codes k, v, constants c_k, c_v of a block, x_j = scale c_k / 127 (q . k_j), w_j = exp(x_j - m) / l over the positions j that
-// a row sees, m = max x_j, l = sum exp(x_j - m):  out = sum_j w_j c_v / 127 v_j.  One pass over the positions with a running
-// m and l; what has been summed is scaled by exp(m_old - m_new) when the maximum grows.  Exponentials are taken to base 2, log2(e)
-// being in the scale.
+// a row sees, l = sum exp(x_j - m):  out = sum_j w_j c_v / 127 v_j.  One pass over the positions.  The values' constants go into the
+// exponents: with y_j = x_j + log c_v the weight that is multiplied by a code is p_j = exp(y_j - M), M the running maximum of y, so
+// that fp16 weights have their full precision where they count whatever the values' size, and a block's share of l is
+// (sum p_j) / c_v.  What has been summed is scaled by exp(M_old - M_new) when M has to grow, which it does only by more than
+// 2^GROW: until then weights up to 2^GROW are as good.  Exponentials are to base 2, log2(e) being in the scale.
 //
 // Both products are fp16 MFMAs (32 x 32 x 16) with fp32 sums.  Codes are exact in fp16: 0x6400 + u is the fp16 number 1024 + u, so a
 // byte permutation and a packed subtraction make two values of two codes.  Rows of queries are the N side of both products, S^T = K
@@ -17,6 +19,7 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LOWEST = -3.0e38f;  // below every score, finite: exp2(-inf - LOWEST) is 0, where -inf - -inf would be NaN
+constexpr float GROW = 8.0f;
 
 __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -31,12 +34,81 @@ __device__ __forceinline__ h8 codes8(unsigned a, unsigned b)
     return h8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
 }
 
-__device__ __forceinline__ h8 pack8(const float* p, float f)
+__device__ __forceinline__ h8 pack8(const float* p)
 {
     h8 r;
 #pragma unroll
-    for (int e = 0; e < 8; e++) r[e] = (_Float16)(p[e] * f);
+    for (int e = 0; e < 8; e++) r[e] = (_Float16)p[e];
     return r;
+}
+
+// What a block's scores and weights are taken by.  A block that is not there: weights of 0.
+struct Factors {
+    float ks;   // of the scores; above 0, so that a masked -inf stays one
+    float lcv;  // log2 of the values' constant.  A block of zeros counts as 2^-24, the smallest constant: its weights count in l
+    float inv;  // 1 / the values' constant
+};
+__device__ __forceinline__ Factors factors(bool there, float ck, float cv, float scale)
+{
+    cv = fmaxf(cv, 0x1p-24f);
+    return {fmaxf(ck * scale, 1e-30f), there ? __builtin_amdgcn_logf(cv) : -__builtin_inff(), there ? 1.0f / cv : 0.0f};
+}
+__device__ __forceinline__ Factors factors(bool there, unsigned c, float scale)
+{
+    return factors(there, f16_bits_to_float((unsigned short)(c & 0xffffu)) * (1.0f / 127.0f), f16_bits_to_float((unsigned short)(c >> 16)), scale);
+}
+
+// the larger of what the two halves of a wave hold for a row
+__device__ __forceinline__ float halves_max(float x)
+{
+    float y = x;
+    // upper half of the one with lower half of the other; two wait states behind what wrote the operands
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return fmaxf(x, y);
+}
+
+// Weights of N blocks from their raw scores: sc[y][i] is at position pos0 + 32 y + 8 (i / 4) + 4 hh + i % 4.  lo .. hi - 1: what the lane's
+// row sees, looked at if mask.  grown(f): M grew, sums are to be scaled by f.
+template <int N, class G>
+__device__ __forceinline__ void weights(f16v (&sc)[N], const Factors (&fa)[N], bool mask, int pos0, int hh, int lo, int hi, float& M, float& l,
+                                        h8 (&pf)[N][2], G grown)
+{
+    if (mask) {
+#pragma unroll
+        for (int y = 0; y < N; y++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int pos = pos0 + 32 * y + 8 * (i >> 2) + 4 * hh + (i & 3);
+                if (pos < lo || pos >= hi) sc[y][i] = -__builtin_inff();
+            }
+    }
+    float top = LOWEST;
+#pragma unroll
+    for (int y = 0; y < N; y++) {
+        float mx = sc[y][0];
+#pragma unroll
+        for (int i = 1; i < 16; i++) mx = fmaxf(mx, sc[y][i]);
+        top = fmaxf(top, __builtin_fmaf(mx, fa[y].ks, fa[y].lcv));
+    }
+    top = halves_max(top);
+    if (__any(top > M + GROW)) {
+        const float n = fmaxf(M, top), f = exp2_(M - n);
+        l *= f;
+        M = n;
+        grown(f);
+    }
+#pragma unroll
+    for (int y = 0; y < N; y++) {
+        const float off = fa[y].lcv - M;
+        float p[16], sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            p[i] = exp2_(__builtin_fmaf(sc[y][i], fa[y].ks, off));
+            sum += p[i];
+        }
+        l = __builtin_fmaf(sum, fa[y].inv, l);
+        pf[y][0] = pack8(p), pf[y][1] = pack8(p + 8);
+    }
 }
 
 struct AttendArgs {
@@ -84,21 +156,19 @@ __device__ __forceinline__ void seen(const AttendArgs& a, int len, int pos, int&
     lo = a.window && pos >= a.window ? pos - a.window + 1 : 0;
 }
 
-// A power of two that is at least x > 0 (fp32)
-__device__ __forceinline__ float power_above(float x)
+// The open block's values are taken in units of this power of two, so that the largest (fp16 bits) is at most 128 of them
+__device__ __forceinline__ float open_unit(unsigned largest)
 {
-    const unsigned b = __builtin_bit_cast(unsigned, x);
-    return __builtin_bit_cast(float, (b + 0x007fffffu) & 0xff800000u);
+    const unsigned b = __builtin_bit_cast(unsigned, fmaxf(f16_bits_to_float((unsigned short)largest), 0x1p-24f));
+    return __builtin_bit_cast(float, (b + 0x007fffffu) & 0xff800000u) * (1.0f / 128.0f);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
-// every wave blocks of its own; sums meet in LDS.  Bound by HBM.  The values' codes stay exact, their constant is a factor of the
-// weights: relative to `ref`, a power of two that is at least every constant so far, so that the products keep the
-// precision of fp16 whatever the values' size.
+// every wave blocks of its own; sums meet in LDS.  Bound by HBM.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <int DP>
-__global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const AttendArgs a)
 {
     constexpr int NT = DP / 32;
     __shared__ float s_o[4][32][33];
@@ -134,44 +204,10 @@ __global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
     f16v o[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) o[t] = f16v{};
-    float m = LOWEST, l = 0.0f, ref = 0.0f;
-
+    float m = LOWEST, l = 0.0f;
     auto rescale = [&](float f) {
 #pragma unroll
         for (int t = 0; t < NT; t++) o[t] *= f;
-    };
-    auto new_ref = [&](float c) {
-        const float r = power_above(c);
-        if (ref > 0.0f) rescale(ref / r);
-        ref = r;
-    };
-    // weights of a block from its scores, as the two operands of the second product, times f
-    auto weights = [&](f16v sc, float ks, int blk, float f, h8 (&pf)[2]) {
-        float x[16], mx = LOWEST;
-#pragma unroll
-        for (int i = 0; i < 16; i++) x[i] = sc[i] * ks;
-        if (blk * KV_BLOCK < all_lo || blk * KV_BLOCK + KV_BLOCK > all_hi) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const int pos = blk * KV_BLOCK + 8 * (i >> 2) + 4 * hh + (i & 3);
-                if (pos < rlo || pos >= rhi) x[i] = -__builtin_inff();
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) mx = fmaxf(mx, x[i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (__any(mx > m)) {
-            const float n = fmaxf(m, mx), f = exp2_(m - n);
-            l *= f;
-            rescale(f);
-            m = n;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            x[i] = exp2_(x[i] - m);
-            l += x[i];
-        }
-        pf[0] = pack8(x, f), pf[1] = pack8(x + 8, f);
     };
 
     // The wave's blocks: c0 + w, c0 + w + 4, ...  Lane i looks up the i-th of the next 64.
@@ -217,31 +253,31 @@ __global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
             request(next, kn, vn);
         }
         if (!there) continue;
-        const float ck = f16_bits_to_float((unsigned short)(c & 0xffffu)), cv = f16_bits_to_float((unsigned short)(c >> 16));
-        f16v sc = {};
+        f16v sc[1] = {};
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            sc = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc);
-            sc = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc);
+            sc[0] = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc[0]);
+            sc[0] = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc[0]);
         }
-        if (cv > ref) new_ref(cv);
-        h8 pf[2];
-        weights(sc, ck * (1.0f / 127.0f) * a.scale, c0 + w + 4 * i, ref > 0.0f ? cv / ref : 0.0f, pf);
+        const Factors fa[1] = {factors(true, c, a.scale)};
+        const int pos0 = (c0 + w + 4 * i) * KV_BLOCK;
+        h8 pf[1][2];
+        weights<1>(sc, fa, pos0 < all_lo || pos0 + KV_BLOCK > all_hi, pos0, hh, rlo, rhi, m, l, pf, rescale);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0], o[t]);
-            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[1], o[t]);
+            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0][0], o[t]);
+            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[0][1], o[t]);
         }
     }
-    // The open block, fp16: by the wave whose turn it is.  Values in units of ref / 128, weights times 127 / 128, as if they were codes.
+    // The open block, fp16: by the wave whose turn it is.  Its values are scaled by a power of two to what codes are, at most 128.
     if (closed >= c0 && closed < c1 && ((closed - c0) & 3) == w) {
         const int d = p.d, base = closed * KV_BLOCK;
-        f16v sc = {};
+        f16v sc[1] = {};
         const bool there = base + qr < s.len;
         const _Float16* row = (const _Float16*)kv_ring_row(p, s.slot, head, 0, base + qr);
 #pragma unroll
         for (int t = 0; t < DP / 16; t++)
-            sc = mfma(there ? q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), d, d % 8 == 0) : h8{}, qf[t], sc);
+            sc[0] = mfma(there ? q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), d, d % 8 == 0) : h8{}, qf[t], sc[0]);
         unsigned short v[NT][16], big = 0;
         const unsigned short* vals = kv_ring_row(p, s.slot, head, 1, base);
 #pragma unroll
@@ -259,19 +295,17 @@ __global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
             const int y = __shfl_xor(top, x);
             top = y > top ? y : top;
         }
-        const float cv = f16_bits_to_float((unsigned short)top);
-        if (cv > ref) new_ref(cv);
-        if (ref == 0.0f) ref = 1.0f;
-        const float unit = 128.0f / ref;
-        h8 pf[2];
-        weights(sc, a.scale, closed, 127.0f / 128.0f, pf);
+        const float unit = open_unit(top);
+        const Factors fa[1] = {factors(true, 1.0f, 127.0f * unit, a.scale)};
+        h8 pf[1][2];
+        weights<1>(sc, fa, true, base, hh, rlo, rhi, m, l, pf, rescale);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             float y[16];
 #pragma unroll
-            for (int i = 0; i < 16; i++) y[i] = f16_bits_to_float(v[t][i]);
-            o[t] = mfma(pack8(y, unit), pf[0], o[t]);
-            o[t] = mfma(pack8(y + 8, unit), pf[1], o[t]);
+            for (int i = 0; i < 16; i++) y[i] = f16_bits_to_float(v[t][i]) * (1.0f / unit);
+            o[t] = mfma(pack8(y), pf[0][0], o[t]);
+            o[t] = mfma(pack8(y + 8), pf[0][1], o[t]);
         }
     }
 
@@ -281,7 +315,7 @@ __global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
     __syncthreads();
     {
         const float top = fmaxf(fmaxf(s_m[0][qr], s_m[1][qr]), fmaxf(s_m[2][qr], s_m[3][qr]));
-        rescale(exp2_(m - top) * ref * (1.0f / 127.0f));
+        rescale(exp2_(m - top) * (1.0f / 127.0f));
     }
     const long long total = (long long)p.n_rows * a.heads_q;
 #pragma unroll
@@ -314,19 +348,19 @@ __global__ void __launch_bounds__(256) kv_step_kernel(const AttendArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Many rows: a workgroup takes a tile of 4 x 32 QT rows (tokens, and for each the query heads that share its keys), its waves the
-// same blocks of the cache two at a time from LDS, where they lie as fp16 in operand order: codes are converted once for all rows.
-// The values there are whole (code c_v / 127 rounded to fp16, as llmint8_kv_read gives them), the keys codes, their constant a factor of
-// the scores.  Bound by the matrix units and by what makes scores weights.
+// Many rows: a workgroup takes a tile of 32 QT rows a wave (tokens, and for each the query heads that share its keys), its waves the
+// same blocks of the cache two at a time from LDS, where the codes lie as fp16 in operand order: they are converted once for all
+// rows.  Bound by the matrix units and by what makes scores weights.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DP, int QT>
-__global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
+template <int DP, int QT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP * QT <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
 {
-    constexpr int NT = DP / 32, ROWS = 128 * QT;
-    constexpr int PER = DP * 8 / 256;                           // 16-byte pieces of two blocks' codes to a thread
-    extern __shared__ __align__(16) _Float16 lds[];             // [2][keys, values][2 blocks][DP * 32]
+    constexpr int NT = DP / 32, ROWS = 32 * QT * WAVES, THREADS = 64 * WAVES;
+    constexpr int PIECES = DP * 8, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' codes; to a thread
+    extern __shared__ __align__(16) _Float16 lds[];  // [2][keys, values][2 blocks][DP * 32]
     constexpr int BUF = 2 * 2 * DP * 32;
-    __shared__ float s_ks[2][2];
+    __shared__ Factors s_f[2][2];
+    __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
     const int head = blockIdx.x % p.heads, split = blockIdx.y;  // the heads of a tile one after the other: with a multiple of 8
@@ -381,9 +415,9 @@ __global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
 
     // ---- two blocks from the cache: requested as 16-byte pieces of codes, later converted into LDS
     u4 piece[PER];
-    float pc[PER];  // constant of a piece's block
-    // numbers of the stage's two blocks in codes; -1: none, or none held as codes
-    auto blocks_of = [&](int blk, long long (&at)[2]) {
+    Factors next[2];
+    auto request = [&](int blk) {
+        long long at[2];
 #pragma unroll
         for (int x = 0; x < 2; x++) {
             at[x] = -1;
@@ -391,62 +425,69 @@ __global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
                 at[x] = kv_block(p, b, head, blk + x);
                 if (at[x] < 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
             }
-        }
-    };
-    float ks_next[2];
-    auto request = [&](int blk) {
-        long long at[2];
-        blocks_of(blk, at);
-        float cv[2];
-#pragma unroll
-        for (int x = 0; x < 2; x++) {
-            const unsigned c = at[x] >= 0 ? p.consts[at[x]] : 0u;
-            ks_next[x] = at[x] >= 0 ? f16_bits_to_float((unsigned short)(c & 0xffffu)) * (1.0f / 127.0f) * a.scale : -1.0f;
-            cv[x] = f16_bits_to_float((unsigned short)(c >> 16)) * (1.0f / 127.0f);
+            next[x] = factors(at[x] >= 0, at[x] >= 0 ? p.consts[at[x]] : 0u, a.scale);
         }
 #pragma unroll
         for (int j = 0; j < PER; j++) {
-            const int t = tid + 256 * j, x = t >= DP * 4, u = t - x * DP * 4;
-            pc[j] = cv[x];
-            piece[j] = u4{0x0u, 0x0u, 0x0u, 0x0u};
+            const int t = tid + THREADS * j, x = t >= DP * 4, u = t - x * DP * 4;
+            piece[j] = u4{};
+            if (PIECES % THREADS && t >= PIECES) break;
             if (at[x] >= 0) piece[j] = *((const u4*)(p.codes + at[x] * (2 * KV_BLOCK * DP)) + u);
         }
     };
     auto deposit = [&](int buf, int blk) {
         _Float16* const base = lds + buf * BUF;
+        const int open = closed - blk;  // which of the two is the open block, if any
+        const bool has_open = (open == 0 || open == 1) && closed < c1;
+        if (has_open) {  // fp16 from the ring, in place of that block's pieces
+            const int d = p.d, pos0 = closed * KV_BLOCK;
+            const unsigned short* const vals = kv_ring_row(p, s.slot, head, 1, pos0);
+            int big = 0;
+            for (int t = tid; t < KV_BLOCK * d; t += THREADS)
+                if (pos0 + t / d < s.len) {
+                    const int y = vals[t] & 0x7fff;
+                    big = y > big ? y : big;
+                }
 #pragma unroll
-        for (int j = 0; j < PER; j++) {
-            const int t = tid + 256 * j, x = t >= DP * 4, u = t - x * DP * 4;
-            const bool value = u >= DP * 2;
-            const int g = (value ? u - DP * 2 : u) >> 6, ln = u & 63;
-            h8 y[2];
-            if (blk + x == closed && blk + x < c1) {  // the open block: fp16 from the ring
-                const int d = p.d, r = ln & 31, h2_ = ln >> 5, base_pos = closed * KV_BLOCK;
+            for (int x = 32; x; x >>= 1) {
+                const int y = __shfl_xor(big, x);
+                big = y > big ? y : big;
+            }
+            if (lane == 0) s_big[w] = big;
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
+            const float unit = open_unit(big);
+            next[open] = factors(true, 1.0f, 127.0f * unit, a.scale);
+            for (int t = tid; t < 2 * KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's values each
+                const bool value = t >= KV_BLOCK * DP / 8;
+                const int u = value ? t - KV_BLOCK * DP / 8 : t, step = u >> 6, ln = u & 63, r = ln & 31, h = ln >> 5;
+                h8 y = {};
                 if (!value) {
-                    const _Float16* row = (const _Float16*)kv_ring_row(p, s.slot, head, 0, base_pos + r);
-                    const bool there = base_pos + r < s.len;
-                    y[0] = there ? q8(row, 32 * g + 16 * h2_, d, d % 8 == 0) : h8{};
-                    y[1] = there ? q8(row, 32 * g + 16 * h2_ + 8, d, d % 8 == 0) : h8{};
+                    if (pos0 + r < s.len)
+                        y = q8((const _Float16*)kv_ring_row(p, s.slot, head, 0, pos0 + r), 32 * (step >> 1) + 16 * h + 8 * (step & 1), d, d % 8 == 0);
                 } else {
-                    const _Float16* vals = (const _Float16*)kv_ring_row(p, s.slot, head, 1, base_pos);
+                    const int f = 32 * (step >> 1) + r;
 #pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const int q = 8 * (i >> 2) + 4 * h2_ + (i & 3), f = 32 * g + r;
-                        y[i >> 3][i & 7] = base_pos + q < s.len && f < d ? vals[q * d + f] : (_Float16)0.0f;
+                    for (int i = 0; i < 8; i++) {
+                        const int q = 16 * (step & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
+                        if (pos0 + q < s.len && f < d) y[i] = (_Float16)(f16_bits_to_float(vals[q * d + f]) * (1.0f / unit));
                     }
                 }
-            } else if (!value) {
-                y[0] = codes8(piece[j][0], piece[j][1]), y[1] = codes8(piece[j][2], piece[j][3]);
-            } else {
-                float f[16];
-#pragma unroll
-                for (int i = 0; i < 16; i++) f[i] = (float)(int8_t)(piece[j][i >> 2] >> (8 * (i & 3)));
-                y[0] = pack8(f, pc[j]), y[1] = pack8(f + 8, pc[j]);
+                *((h8*)(base + (value ? 2 * DP * 32 : 0) + open * DP * 32) + u) = y;
             }
-            h8* dst = (h8*)(base + (value ? 2 * DP * 32 : 0) + x * DP * 32) + 2 * g * 64 + ln;
-            dst[0] = y[0], dst[64] = y[1];
         }
-        if (tid < 2) s_ks[buf][tid] = blk + tid == closed && blk + tid < c1 ? a.scale : tid ? ks_next[1] : ks_next[0];
+#pragma unroll
+        for (int j = 0; j < PER; j++) {
+            const int t = tid + THREADS * j, x = t >= DP * 4, u = t - x * DP * 4;
+            if (PIECES % THREADS && t >= PIECES) break;
+            if (has_open && x == open) continue;
+            const bool value = u >= DP * 2;
+            const int g = (value ? u - DP * 2 : u) >> 6, ln = u & 63;
+            h8* dst = (h8*)(base + (value ? 2 * DP * 32 : 0) + x * DP * 32) + 2 * g * 64 + ln;
+            dst[0] = codes8(piece[j][0], piece[j][1]), dst[64] = codes8(piece[j][2], piece[j][3]);
+        }
+        if (tid == 0) s_f[buf][0] = next[0], s_f[buf][1] = next[1];
     };
 
     const int stages = c1 > c0 ? (c1 - c0 + 1) / 2 : 0;
@@ -464,57 +505,29 @@ __global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
 #pragma unroll
             for (int t = 0; t < QT; t++) sc[t][0] = sc[t][1] = f16v{};
 #pragma unroll
-            for (int x = 0; x < 2; x++)
+            for (int g = 0; g < DP / 16; g++)
 #pragma unroll
-                for (int g = 0; g < DP / 16; g++) {
+                for (int x = 0; x < 2; x++) {
                     const h8 k = *((const h8*)(base + x * DP * 32) + g * 64 + lane);
 #pragma unroll
                     for (int t = 0; t < QT; t++) sc[t][x] = mfma(k, qf[t][g], sc[t][x]);
                 }
-            const float ks[2] = {s_ks[buf][0], s_ks[buf][1]};
-            const bool mask = blk * KV_BLOCK < all_lo || (blk + 2) * KV_BLOCK > all_hi || ks[0] < 0.0f || ks[1] < 0.0f;
+            const Factors fa[2] = {s_f[buf][0], s_f[buf][1]};
+            const bool mask = blk * KV_BLOCK < all_lo || (blk + 2) * KV_BLOCK > all_hi;
             h8 pf[QT][2][2];
 #pragma unroll
-            for (int t = 0; t < QT; t++) {
-                float x[2][16], mx = LOWEST;
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) x[y][i] = sc[t][y][i] * ks[y];
-                    if (mask)
-#pragma unroll
-                        for (int i = 0; i < 16; i++) {
-                            const int pos = (blk + y) * KV_BLOCK + 8 * (i >> 2) + 4 * hh + (i & 3);
-                            if (pos < rlo[t] || pos >= rhi[t] || ks[y] < 0.0f) x[y][i] = -__builtin_inff();
-                        }
-#pragma unroll
-                    for (int i = 0; i < 16; i++) mx = fmaxf(mx, x[y][i]);
-                }
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                if (__any(mx > m[t])) {
-                    const float n = fmaxf(m[t], mx), f = exp2_(m[t] - n);
-                    l[t] *= f;
-                    m[t] = n;
+            for (int t = 0; t < QT; t++)
+                weights<2>(sc[t], fa, mask, blk * KV_BLOCK, hh, rlo[t], rhi[t], m[t], l[t], pf[t], [&](float f) {
 #pragma unroll
                     for (int q = 0; q < NT; q++) o[t][q] *= f;
-                }
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        x[y][i] = exp2_(x[y][i] - m[t]);
-                        l[t] += x[y][i];
-                    }
-                    pf[t][y][0] = pack8(x[y], 1.0f), pf[t][y][1] = pack8(x[y] + 8, 1.0f);
-                }
-            }
+                });
             const h8* const vb = (const h8*)(base + 2 * DP * 32) + lane;
 #pragma unroll
             for (int x = 0; x < 2; x++)
 #pragma unroll
-                for (int q = 0; q < NT; q++)
+                for (int y = 0; y < 2; y++)
 #pragma unroll
-                    for (int y = 0; y < 2; y++) {
+                    for (int q = 0; q < NT; q++) {
                         const h8 v = vb[x * DP * 4 + (2 * q + y) * 64];
 #pragma unroll
                         for (int t = 0; t < QT; t++) o[t][q] = mfma(v, pf[t][x][y], o[t][q]);
@@ -544,12 +557,12 @@ __global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
                         const int f = 32 * q + 8 * (i >> 2) + 4 * hh + (i & 3);
-                        if (f < p.d) dst[f] = o[t][q][i];
+                        if (f < p.d) dst[f] = o[t][q][i] * (1.0f / 127.0f);
                     }
             }
         } else {
             _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d;
-            const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+            const float inv = den != 0.0f ? (1.0f / 127.0f) / den : 0.0f;
 #pragma unroll
             for (int q = 0; q < NT; q++)
 #pragma unroll
@@ -570,32 +583,92 @@ __global__ void __launch_bounds__(256) kv_prompt_kernel(const AttendArgs a)
     }
 }
 
-// Joins the splits: one wave to a row and head.
+// Joins the splits: WAVES waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the splits dealt
+// out over the waves and their quarters, four in flight each.
+template <int WAVES>
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 {
-    const long long total = (long long)a.kv.n_rows * a.heads_q, x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int NQ = KV_MAX_D / 64;
+    __shared__ f4 s_sum[WAVES > 1 ? WAVES : 1][NQ][16];
+    __shared__ float s_den[WAVES > 1 ? WAVES : 1];
+    const int tid = threadIdx.x, lane = tid & 63, d = a.kv.d, w = WAVES > 1 ? tid >> 6 : 0;
+    const long long total = (long long)a.kv.n_rows * a.heads_q, x = WAVES > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + (tid >> 6);
     if (x >= total) return;
-    const int lane = threadIdx.x & 63, d = a.kv.d;
     float top = LOWEST;
-    for (int s = 0; s < a.splits; s++) {
+    for (int s = lane; s < a.splits; s += 64) {
         const float2 t = a.stat[s * total + x];
         if (t.y != 0.0f) top = fmaxf(top, t.x);
     }
-    float sum[KV_MAX_D / 64] = {}, den = 0.0f;
-    for (int s = 0; s < a.splits; s++) {
-        const float2 t = a.stat[s * total + x];
-        if (t.y == 0.0f) continue;
-        const float f = exp2_(t.x - top);
-        den += f * t.y;
-        const float* src = a.part + (s * total + x) * d;
 #pragma unroll
-        for (int q = 0; q < KV_MAX_D / 64; q++)
-            if (lane + 64 * q < d) sum[q] += f * src[lane + 64 * q];
+    for (int y = 32; y; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
+    const int part = lane >> 4, f0 = 4 * (lane & 15);
+    f4 sum[NQ] = {};
+    float den = 0.0f;
+    for (int s0 = 4 * w + part; s0 < a.splits; s0 += 16 * WAVES) {
+        f4 v[4][NQ];
+        float f[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int s = s0 + 4 * WAVES * u;
+            const float2 t = s < a.splits ? a.stat[s * total + x] : make_float2(0.0f, 0.0f);
+            f[u] = t.y != 0.0f ? exp2_(t.x - top) : 0.0f;
+            den += f[u] * t.y;
+            const float* src = a.part + (s * total + x) * d + f0;
+#pragma unroll
+            for (int q = 0; q < NQ; q++) {
+                v[u][q] = f4{};
+                if (t.y != 0.0f && f0 + 64 * q < d) {
+                    if (d % 4 == 0) {
+                        v[u][q] = *(const f4*)(src + 64 * q);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (f0 + 64 * q + e < d) v[u][q][e] = src[64 * q + e];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+            for (int q = 0; q < NQ; q++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum[q][e] += f[u] * v[u][q][e];
     }
-    _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d;
 #pragma unroll
-    for (int q = 0; q < KV_MAX_D / 64; q++)
-        if (lane + 64 * q < d) dst[lane + 64 * q] = (_Float16)(den != 0.0f ? sum[q] / den : 0.0f);
+    for (int y = 16; y < 64; y <<= 1) {
+        den += __shfl_xor(den, y);
+#pragma unroll
+        for (int q = 0; q < NQ; q++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[q][e] += __shfl_xor(sum[q][e], y);
+    }
+    if (WAVES > 1) {
+        if (lane < 16)
+#pragma unroll
+            for (int q = 0; q < NQ; q++) s_sum[w][q][lane] = sum[q];
+        if (lane == 0) s_den[w] = den;
+        __syncthreads();
+        if (w) return;
+        den = 0.0f;
+#pragma unroll
+        for (int y = 0; y < WAVES; y++) den += s_den[y];
+#pragma unroll
+        for (int q = 0; q < NQ; q++) {
+            sum[q] = f4{};
+#pragma unroll
+            for (int y = 0; y < WAVES; y++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum[q][e] += s_sum[y][q][lane & 15][e];
+        }
+    }
+    if (lane >= 16) return;
+    _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d + f0;
+#pragma unroll
+    for (int q = 0; q < NQ; q++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (f0 + 64 * q + e < d) dst[64 * q + e] = (_Float16)(den != 0.0f ? sum[q][e] / den : 0.0f);
 }
 
 template <int DP>
@@ -605,15 +678,15 @@ hipError_t launch_step(const AttendArgs& a, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DP, int QT>
+template <int DP, int WAVES>
 hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 {
     constexpr int bytes = 2 * 2 * 2 * DP * 32 * 2;
-    if (bytes + sizeof(float) * 4 > 65536) {  // with the static part
-        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, QT>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (bytes + 256 > 65536) {  // with the static part
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, 1, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    kv_prompt_kernel<DP, QT><<<dim3(tiles * a.kv.heads, a.splits), 256, bytes, st>>>(a);
+    kv_prompt_kernel<DP, 1, WAVES><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES, bytes, st>>>(a);
     return hipGetLastError();
 }
 
@@ -631,12 +704,12 @@ KvPlan kv_plan(const Kv& p, int heads_q)
         r.tile = KV_STEP_ROWS, r.tiles = 0;
         units = (long long)p.n_seqs * p.heads;
     } else {
-        r.tile = 128;
+        r.tile = rows > 128 && kv_dpad(p.d) <= 192 ? 256 : 128;
         const long long x = ((long long)p.n_rows * group + (long long)p.n_seqs * (r.tile - 1)) / r.tile, y = p.n_seqs * ((rows + r.tile - 1) / r.tile);
         r.tiles = (int)(x < y ? x : y);
         units = (long long)r.tiles * p.heads;
     }
-    const long long want = 1024 / units, most = blocks / 8;
+    const long long want = (r.tile == KV_STEP_ROWS ? 1024 : r.tile == 128 ? 512 : 256) / units, most = blocks / 8;
     r.splits = (int)(want < most ? want : most);
     if (r.splits < 1) r.splits = 1;
     return r;
@@ -659,7 +732,8 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     hipError_t e;
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
-        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st) : launch_prompt<DP, 1>(a, plan.tiles, st);
+        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st) : plan.tile == 128 ? launch_prompt<DP, 4>(a, plan.tiles, st)
+                                                                                   : launch_prompt<(DP > 192 ? 192 : DP), 8>(a, plan.tiles, st);
     };
     switch (dp) {
         case 32: e = pick(std::integral_constant<int, 32>()); break;
@@ -672,7 +746,10 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
         default: e = pick(std::integral_constant<int, 256>()); break;
     }
     if (e != hipSuccess || plan.splits == 1) return e;
-    kv_join_kernel<<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a);
+    if (plan.splits > 8)
+        kv_join_kernel<4><<<(unsigned)total, 256, 0, st>>>(a);
+    else
+        kv_join_kernel<1><<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
