@@ -67,21 +67,25 @@ __device__ __forceinline__ float halves_max(float x)
     return fmaxf(x, y);
 }
 
-// Weights of N blocks from their raw scores: sc[y][i] is at position pos0 + 32 y + 8 (i / 4) + 4 hh + i % 4.  lo .. hi - 1: what the lane's
-// row sees, looked at if mask.  grown(f): M grew, sums are to be scaled by f.
-template <int N, class G>
-__device__ __forceinline__ void weights(f16v (&sc)[N], const Factors (&fa)[N], bool mask, int pos0, int hh, int lo, int hi, float& M, float& l,
-                                        h8 (&pf)[N][2], G grown)
+// Scores of N blocks of which the lane's row does not see all: those at positions outside lo .. hi - 1 out.  sc[y][i] is at position
+// pos0 + 32 y + 8 (i / 4) + 4 hh + i % 4.
+template <int N>
+__device__ __forceinline__ void hide(f16v (&sc)[N], int pos0, int hh, int lo, int hi)
 {
-    if (mask) {
+    const int l = lo - pos0 - 4 * hh, h = hi - pos0 - 4 * hh;
 #pragma unroll
-        for (int y = 0; y < N; y++)
+    for (int y = 0; y < N; y++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const int pos = pos0 + 32 * y + 8 * (i >> 2) + 4 * hh + (i & 3);
-                if (pos < lo || pos >= hi) sc[y][i] = -__builtin_inff();
-            }
-    }
+        for (int i = 0; i < 16; i++) {
+            const int at = 32 * y + 8 * (i >> 2) + (i & 3);
+            if (at < l || at >= h) sc[y][i] = -__builtin_inff();
+        }
+}
+
+// The running maximum with N blocks' raw scores; grown(f): M grew, sums are to be scaled by f.
+template <int N, class G>
+__device__ __forceinline__ void peak(const f16v (&sc)[N], const Factors (&fa)[N], float& M, float& l, G grown)
+{
     float top = LOWEST;
 #pragma unroll
     for (int y = 0; y < N; y++) {
@@ -97,18 +101,21 @@ __device__ __forceinline__ void weights(f16v (&sc)[N], const Factors (&fa)[N], b
         M = n;
         grown(f);
     }
+}
+
+// Weights of a block as the operands of the second product, and their share of l: by their fp32 values, since those of a block whose
+// values are small may be nothing in fp16.
+__device__ __forceinline__ void expo(const f16v& sc, const Factors& fa, float M, float& l, h8 (&pf)[2])
+{
+    const float off = fa.lcv - M;
+    float p[16], sum = 0.0f;
 #pragma unroll
-    for (int y = 0; y < N; y++) {
-        const float off = fa[y].lcv - M;
-        float p[16], sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            p[i] = exp2_(__builtin_fmaf(sc[y][i], fa[y].ks, off));
-            sum += p[i];
-        }
-        l = __builtin_fmaf(sum, fa[y].inv, l);
-        pf[y][0] = pack8(p), pf[y][1] = pack8(p + 8);
+    for (int i = 0; i < 16; i++) {
+        p[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off));
+        sum += p[i];
     }
+    pf[0] = pack8(p), pf[1] = pack8(p + 8);
+    l = __builtin_fmaf(sum, fa.inv, l);
 }
 
 struct AttendArgs {
@@ -262,7 +269,9 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         const Factors fa[1] = {factors(true, c, a.scale)};
         const int pos0 = (c0 + w + 4 * i) * KV_BLOCK;
         h8 pf[1][2];
-        weights<1>(sc, fa, pos0 < all_lo || pos0 + KV_BLOCK > all_hi, pos0, hh, rlo, rhi, m, l, pf, rescale);
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide<1>(sc, pos0, hh, rlo, rhi);
+        peak<1>(sc, fa, m, l, rescale);
+        expo(sc[0], fa[0], m, l, pf[0]);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0][0], o[t]);
@@ -298,7 +307,9 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         const float unit = open_unit(top);
         const Factors fa[1] = {factors(true, 1.0f, 127.0f * unit, a.scale)};
         h8 pf[1][2];
-        weights<1>(sc, fa, true, base, hh, rlo, rhi, m, l, pf, rescale);
+        hide<1>(sc, base, hh, rlo, rhi);
+        peak<1>(sc, fa, m, l, rescale);
+        expo(sc[0], fa[0], m, l, pf[0]);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             float y[16];
@@ -348,18 +359,17 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Many rows: a workgroup takes a tile of 32 QT rows a wave (tokens, and for each the query heads that share its keys), its waves the
-// same blocks of the cache two at a time from LDS, where the codes lie as fp16 in operand order: they are converted once for all
-// rows.  Bound by the matrix units and by what makes scores weights.
+// Many rows: a workgroup takes a tile of 32 rows a wave (tokens, and for each the query heads that share its keys), its waves the
+// same blocks of the cache two at a time (a stage) from LDS, where the codes lie as fp16 in operand order: they are converted once
+// for all rows.  Bound by the matrix units and by what makes scores weights, which are kept busy at the same time: the scores of the
+// next stage are computed while the weights of this one are.  So LDS holds keys one stage ahead of values.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DP, int QT, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP * QT <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
+template <int DP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
 {
-    constexpr int NT = DP / 32, ROWS = 32 * QT * WAVES, THREADS = 64 * WAVES;
-    constexpr int PIECES = DP * 8, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' codes; to a thread
-    extern __shared__ __align__(16) _Float16 lds[];  // [2][keys, values][2 blocks][DP * 32]
-    constexpr int BUF = 2 * 2 * DP * 32;
-    __shared__ Factors s_f[2][2];
+    constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+    constexpr int PIECES = DP * 4, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' keys, or values; to a thread
+    extern __shared__ __align__(16) _Float16 lds[];                         // [keys, values][4 blocks][DP * 32]
     __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
@@ -380,7 +390,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP * QT <= 128 ? 2 :
     const int rows = s.n * a.group, old = s.len - s.n;
     tile = (rows + ROWS - 1) / ROWS - 1 - tile;  // those that see most first
     const int r0 = tile * ROWS, r1 = r0 + ROWS < rows ? r0 + ROWS : rows;
-    const int w0 = r0 + w * 32 * QT, w1 = w0 + 32 * QT < r1 ? w0 + 32 * QT : r1;  // this wave's rows
+    const int w0 = r0 + w * 32, w1 = w0 + 32 < r1 ? w0 + 32 : r1;  // this wave's rows
 
     int lo, hi, x0, x1;
     seen(a, s.len, old + r0 / a.group, lo, x1);
@@ -388,198 +398,275 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP * QT <= 128 ? 2 :
     const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
     const int chunk = ((end - first + a.splits - 1) / a.splits + 1) & ~1;
     const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
-    const int closed = s.len / KV_BLOCK;
-    // what the wave's rows see: some of them, and all of them
+    const int closed = s.len / KV_BLOCK, k1 = c1 < closed ? c1 : closed;
+    const int stages = k1 > c0 ? (k1 - c0 + 1) / 2 : 0;
+    // what all of the wave's rows see, and the stages in which some see anything
     int some_lo = 0, some_hi = 0, all_lo = 0, all_hi = 0;
     if (w0 < w1) {
         seen(a, s.len, old + w0 / a.group, some_lo, all_hi);
         seen(a, s.len, old + (w1 - 1) / a.group, all_lo, some_hi);
     }
+    auto clip = [&](int x) { return x < 0 ? 0 : x > stages ? stages : x; };
+    const int sa = clip((some_lo / KV_BLOCK - c0) >> 1), sb = clip(((some_hi + KV_BLOCK - 1) / KV_BLOCK - c0 + 1) >> 1);
 
-    h8 qf[QT][DP / 16];
-    int rlo[QT], rhi[QT];
+    h8 qf[DP / 16];
+    load_q<DP>(a, s, head, w0 + qr, hh, qf);
+    int rlo, rhi;
+    seen(a, s.len, old + (w0 + qr) / a.group, rlo, rhi);
+    if (rhi > k1 * KV_BLOCK) rhi = k1 * KV_BLOCK;  // behind that there is nothing of this workgroup's but the open block
+    if (all_hi > k1 * KV_BLOCK) all_hi = k1 * KV_BLOCK;
+    f16v o[NT];
+    float m = LOWEST, l = 0.0f;
 #pragma unroll
-    for (int t = 0; t < QT; t++) {
-        const int r = w0 + 32 * t + qr;
-        load_q<DP>(a, s, head, r, hh, qf[t]);
-        seen(a, s.len, old + r / a.group, rlo[t], rhi[t]);
-    }
-    f16v o[QT][NT];
-    float m[QT], l[QT];
-#pragma unroll
-    for (int t = 0; t < QT; t++) {
-        m[t] = LOWEST, l[t] = 0.0f;
-#pragma unroll
-        for (int x = 0; x < NT; x++) o[t][x] = f16v{};
-    }
+    for (int x = 0; x < NT; x++) o[x] = f16v{};
 
-    // ---- two blocks from the cache: requested as 16-byte pieces of codes, later converted into LDS
-    u4 piece[PER];
-    Factors next[2];
-    auto request = [&](int blk) {
-        long long at[2];
+    // where a block's keys and values lie in LDS
+    auto keys = [&](int j) { return (h8*)(lds + (j & 3) * (DP * 32)) + lane; };
+    auto values = [&](int j) { return (h8*)(lds + (4 + (j & 3)) * (DP * 32)) + lane; };
+    auto scores = [&](int j, f16v& sc) {
+        const h8* const kb = keys(j);
+        sc = f16v{};
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
-            at[x] = -1;
-            if (blk + x < c1 && blk + x < closed) {
-                at[x] = kv_block(p, b, head, blk + x);
-                if (at[x] < 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
-            }
-            next[x] = factors(at[x] >= 0, at[x] >= 0 ? p.consts[at[x]] : 0u, a.scale);
-        }
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-            const int t = tid + THREADS * j, x = t >= DP * 4, u = t - x * DP * 4;
-            piece[j] = u4{};
-            if (PIECES % THREADS && t >= PIECES) break;
-            if (at[x] >= 0) piece[j] = *((const u4*)(p.codes + at[x] * (2 * KV_BLOCK * DP)) + u);
-        }
+        for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
     };
-    auto deposit = [&](int buf, int blk) {
-        _Float16* const base = lds + buf * BUF;
-        const int open = closed - blk;  // which of the two is the open block, if any
-        const bool has_open = (open == 0 || open == 1) && closed < c1;
-        if (has_open) {  // fp16 from the ring, in place of that block's pieces
-            const int d = p.d, pos0 = closed * KV_BLOCK;
-            const unsigned short* const vals = kv_ring_row(p, s.slot, head, 1, pos0);
-            int big = 0;
-            for (int t = tid; t < KV_BLOCK * d; t += THREADS)
-                if (pos0 + t / d < s.len) {
-                    const int y = vals[t] & 0x7fff;
-                    big = y > big ? y : big;
-                }
+    // Weights of block j from its scores, in slices between the products of the next block's scores, then its sums.  The order is
+    // fixed slice by slice: operands are read from LDS one slice ahead and no further, or registers run out.
+    auto step = [&](int j, const f16v& sc, const Factors& fa, f16v& next) {
+        constexpr int S = DP / 16;
+        const h8 *const kb = keys(j + 1), *const vb = values(j);
+        const float off = fa.lcv - m;
+        float sum = 0.0f;
+        h8 pf[2], k = kb[0], v[NT];
+        next = f16v{};
 #pragma unroll
-            for (int x = 32; x; x >>= 1) {
-                const int y = __shfl_xor(big, x);
-                big = y > big ? y : big;
+        for (int g = 0; g < S; g++) {
+            const h8 t = k;
+            if (g + 1 < S) k = kb[(g + 1) * 64];
+            next = mfma(t, qf[g], next);
+            if (g + 1 == S)
+#pragma unroll
+                for (int q = 0; q < NT; q++) v[q] = vb[2 * q * 64];
+#pragma unroll
+            for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
+                const float p0 = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), p1 = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
+                pf[i >> 3][i & 7] = (_Float16)p0, pf[i >> 3][(i & 7) + 1] = (_Float16)p1;
+                sum += p0;
+                sum += p1;
             }
-            if (lane == 0) s_big[w] = big;
-            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l = __builtin_fmaf(sum, fa.inv, l);
 #pragma unroll
-            for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
-            const float unit = open_unit(big);
-            next[open] = factors(true, 1.0f, 127.0f * unit, a.scale);
-            for (int t = tid; t < 2 * KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's values each
-                const bool value = t >= KV_BLOCK * DP / 8;
-                const int u = value ? t - KV_BLOCK * DP / 8 : t, step = u >> 6, ln = u & 63, r = ln & 31, h = ln >> 5;
-                h8 y = {};
-                if (!value) {
-                    if (pos0 + r < s.len)
-                        y = q8((const _Float16*)kv_ring_row(p, s.slot, head, 0, pos0 + r), 32 * (step >> 1) + 16 * h + 8 * (step & 1), d, d % 8 == 0);
-                } else {
-                    const int f = 32 * (step >> 1) + r;
+        for (int y = 0; y < 2; y++)
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const int q = 16 * (step & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
-                        if (pos0 + q < s.len && f < d) y[i] = (_Float16)(f16_bits_to_float(vals[q * d + f]) * (1.0f / unit));
-                    }
-                }
-                *((h8*)(base + (value ? 2 * DP * 32 : 0) + open * DP * 32) + u) = y;
+            for (int q = 0; q < NT; q++) {
+                const h8 t = v[q];
+                if (y == 0) v[q] = vb[(2 * q + 1) * 64];
+                o[q] = mfma(t, pf[y], o[q]);
             }
-        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto look = [&](int pos0, f16v& sc, const Factors& fa) {
+        f16v(&one)[1] = reinterpret_cast<f16v(&)[1]>(sc);
+        const Factors f[1] = {fa};
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide<1>(one, pos0, hh, rlo, rhi);
+        peak<1>(one, f, m, l, [&](float x) {
 #pragma unroll
-        for (int j = 0; j < PER; j++) {
-            const int t = tid + THREADS * j, x = t >= DP * 4, u = t - x * DP * 4;
-            if (PIECES % THREADS && t >= PIECES) break;
-            if (has_open && x == open) continue;
-            const bool value = u >= DP * 2;
-            const int g = (value ? u - DP * 2 : u) >> 6, ln = u & 63;
-            h8* dst = (h8*)(base + (value ? 2 * DP * 32 : 0) + x * DP * 32) + 2 * g * 64 + ln;
-            dst[0] = codes8(piece[j][0], piece[j][1]), dst[64] = codes8(piece[j][2], piece[j][3]);
-        }
-        if (tid == 0) s_f[buf][0] = next[0], s_f[buf][1] = next[1];
+            for (int q = 0; q < NT; q++) o[q] *= x;
+        });
     };
 
-    const int stages = c1 > c0 ? (c1 - c0 + 1) / 2 : 0;
+    // ---- the open block, fp16 from the ring, before the others
+    if (closed >= c0 && closed < c1) {
+        const int d = p.d, pos0 = closed * KV_BLOCK;
+        const unsigned short *const krows = kv_ring_row(p, s.slot, head, 0, pos0), *const vrows = kv_ring_row(p, s.slot, head, 1, pos0);
+        int big = 0;
+        for (int t = tid; t < (s.len - pos0) * d; t += THREADS) {
+            const int y = vrows[t] & 0x7fff;
+            big = y > big ? y : big;
+        }
+#pragma unroll
+        for (int x = 32; x; x >>= 1) {
+            const int y = __shfl_xor(big, x);
+            big = y > big ? y : big;
+        }
+        if (lane == 0) s_big[w] = big;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
+        const float unit = open_unit(big);
+        for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
+            const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
+            h8 y = {}, z = {};
+            if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
+                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / unit));
+            }
+            *((h8*)lds + t) = y;
+            *((h8*)(lds + 4 * DP * 32) + t) = z;
+        }
+        __syncthreads();
+        if (pos0 < some_hi) {
+            f16v sc[1];
+            scores(0, sc[0]);
+            const Factors fa[1] = {factors(true, 1.0f, 127.0f * unit, a.scale)};
+            int olo, ohi;
+            seen(a, s.len, old + (w0 + qr) / a.group, olo, ohi);
+            hide<1>(sc, pos0, hh, olo, ohi < s.len ? ohi : s.len);
+            peak<1>(sc, fa, m, l, [](float) {});
+            h8 pf[2];
+            expo(sc[0], fa[0], m, l, pf);
+            const h8* const vb = values(0);
+#pragma unroll
+            for (int y = 0; y < 2; y++)
+#pragma unroll
+                for (int q = 0; q < NT; q++) o[q] = mfma(vb[(2 * q + y) * 64], pf[y], o[q]);
+        }
+        __syncthreads();
+    }
+
+    // ---- Lane i of every wave looks up the i-th of 64 blocks, so that a stage waits neither for the page table nor for constants:
+    // `ahead` are the 64 blocks behind those in use.
+    struct Looked {
+        int at[2];  // number in codes; -1: none
+        Factors f;
+    };
+    auto look_up = [&](int j) {
+        Looked r;
+        long long at = -1;
+        unsigned c = 0;
+        if (c0 + j + lane < k1) {
+            at = kv_block(p, b, head, c0 + j + lane);
+            if (at >= 0)
+                c = p.consts[at];
+            else
+                kv_flag(p, LLMINT8_KV_BAD_PAGE);
+        }
+        r.f = factors(at >= 0, c, a.scale);
+        at = at < 0 ? 0 : at;  // (weights of 0 for what is not there)
+        r.at[0] = (int)at, r.at[1] = (int)(at >> 32);
+        return r;
+    };
+    Looked use, ahead;
+    int j0 = 0;  // the first block of `use`
+    auto at_lane = [&](int x, int y, int j) {
+        const int i = j - j0, u = __builtin_amdgcn_readlane(x, i & 63), v = __builtin_amdgcn_readlane(y, i & 63);
+        return i < 64 ? u : v;
+    };
+    auto float_at = [&](float x, float y, int j) {
+        return __builtin_bit_cast(float, at_lane(__builtin_bit_cast(int, x), __builtin_bit_cast(int, y), j));
+    };
+    auto factors_of = [&](int j) {
+        return Factors{float_at(use.f.ks, ahead.f.ks, j), float_at(use.f.lcv, ahead.f.lcv, j), float_at(use.f.inv, ahead.f.inv, j)};
+    };
+    // this thread's 16-byte pieces of the keys (value 0) or values of blocks j and j + 1
+    auto request = [&](int j, int value, u4 (&piece)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;  // a wave's pieces are of one block
+            if (PIECES % THREADS && t >= PIECES) break;
+            const long long at = (long long)at_lane(use.at[1], ahead.at[1], j + x) << 32 | (unsigned)at_lane(use.at[0], ahead.at[0], j + x);
+            piece[i] = *((const u4*)(p.codes + at * (2 * KV_BLOCK * DP)) + value * DP * 2 + u + lane);
+        }
+    };
+    auto deposit = [&](int j, int value, const u4 (&piece)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;
+            if (PIECES % THREADS && t >= PIECES) break;
+            h8* dst = (value ? values(j + x) : keys(j + x)) + 2 * u;
+            dst[0] = codes8(piece[i][0], piece[i][1]), dst[64] = codes8(piece[i][2], piece[i][3]);
+        }
+    };
+
+    // ---- Stage st: blocks 2 st and 2 st + 1 (from c0 on): their weights and sums, and each time the scores of the block behind.  So keys
+    // go to LDS one block earlier than values: meanwhile those of 2 st + 3 and 2 st + 4, and the values of 2 st + 2 and 2 st + 3.
     if (stages) {
-        request(c0);
-        deposit(0, c0);
-        if (stages > 1) request(c0 + 2);
+        u4 pk[PER], pv[PER];
+        use = look_up(0), ahead = look_up(64);
+        request(0, 0, pk), request(0, 1, pv);
+        deposit(0, 0, pk), deposit(0, 1, pv);
+        request(1, 0, pk);
+        __syncthreads();  // (block 1's keys come twice)
+        deposit(1, 0, pk);
+        request(3, 0, pk), request(2, 1, pv);
         __syncthreads();
-    }
-    for (int st = 0; st < stages; st++) {
-        const int blk = c0 + 2 * st, buf = st & 1;
-        const _Float16* const base = lds + buf * BUF;
-        if (blk * KV_BLOCK < some_hi && (blk + 2) * KV_BLOCK > some_lo) {
-            f16v sc[QT][2];
-#pragma unroll
-            for (int t = 0; t < QT; t++) sc[t][0] = sc[t][1] = f16v{};
-#pragma unroll
-            for (int g = 0; g < DP / 16; g++)
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    const h8 k = *((const h8*)(base + x * DP * 32) + g * 64 + lane);
-#pragma unroll
-                    for (int t = 0; t < QT; t++) sc[t][x] = mfma(k, qf[t][g], sc[t][x]);
-                }
-            const Factors fa[2] = {s_f[buf][0], s_f[buf][1]};
-            const bool mask = blk * KV_BLOCK < all_lo || (blk + 2) * KV_BLOCK > all_hi;
-            h8 pf[QT][2][2];
-#pragma unroll
-            for (int t = 0; t < QT; t++)
-                weights<2>(sc[t], fa, mask, blk * KV_BLOCK, hh, rlo[t], rhi[t], m[t], l[t], pf[t], [&](float f) {
-#pragma unroll
-                    for (int q = 0; q < NT; q++) o[t][q] *= f;
-                });
-            const h8* const vb = (const h8*)(base + 2 * DP * 32) + lane;
-#pragma unroll
-            for (int x = 0; x < 2; x++)
-#pragma unroll
-                for (int y = 0; y < 2; y++)
-#pragma unroll
-                    for (int q = 0; q < NT; q++) {
-                        const h8 v = vb[x * DP * 4 + (2 * q + y) * 64];
-#pragma unroll
-                        for (int t = 0; t < QT; t++) o[t][q] = mfma(v, pf[t][x][y], o[t][q]);
-                    }
-        }
-        if (st + 1 < stages) {
-            deposit(buf ^ 1, blk + 2);
-            if (st + 2 < stages) request(blk + 4);
-        }
+        auto supply = [&](int st) {  // the end of a stage
+            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
+            if (2 * st + 2 == j0 + 64) {
+                use = ahead, j0 += 64;
+                ahead = look_up(j0 + 64);
+            }
+            request(2 * st + 5, 0, pk), request(2 * st + 4, 1, pv);
+            __syncthreads();
+        };
+        // The wave's first scores are computed in the stage before (its keys are overwritten in its own)
+        f16v s0, s1;
+        Factors f0;
+        auto enter = [&]() {
+            scores(2 * sa, s0);
+            f0 = factors_of(2 * sa);
+            look((c0 + 2 * sa) * KV_BLOCK, s0, f0);
+        };
+        if (sa == 0) enter();
         __syncthreads();
+        int st = 0;
+        for (; st < sa; st++) {
+            if (st + 1 == sa) enter();
+            supply(st);
+        }
+        for (; st < sb; st++) {
+            const int pos0 = (c0 + 2 * st) * KV_BLOCK;
+            step(2 * st, s0, f0, s1);
+            const Factors f1 = factors_of(2 * st + 1);
+            look(pos0 + KV_BLOCK, s1, f1);
+            step(2 * st + 1, s1, f1, s0);
+            f0 = factors_of(2 * st + 2);
+            look(pos0 + 2 * KV_BLOCK, s0, f0);
+            supply(st);
+        }
+        for (; st < stages; st++) supply(st);
     }
 
     const long long total = (long long)p.n_rows * a.heads_q;
-#pragma unroll
-    for (int t = 0; t < QT; t++) {
-        const float den = l[t] + __shfl_xor(l[t], 32);
-        const int r = w0 + 32 * t + qr;
-        if (r >= r1) continue;
-        const long long row = s.row0 + r / a.group;
-        const int g = head * a.group + r % a.group;
-        if (a.splits > 1) {
-            if (hh == 0) a.stat[split * total + row * a.heads_q + g] = make_float2(m[t], den);
-            if (den != 0.0f) {
-                float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
-#pragma unroll
-                for (int q = 0; q < NT; q++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const int f = 32 * q + 8 * (i >> 2) + 4 * hh + (i & 3);
-                        if (f < p.d) dst[f] = o[t][q][i] * (1.0f / 127.0f);
-                    }
-            }
-        } else {
-            _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d;
-            const float inv = den != 0.0f ? (1.0f / 127.0f) / den : 0.0f;
+    const float den = l + __shfl_xor(l, 32);
+    const int r = w0 + qr;
+    if (r >= r1) return;
+    const long long row = s.row0 + r / a.group;
+    const int g = head * a.group + r % a.group;
+    if (a.splits > 1) {
+        if (hh == 0) a.stat[split * total + row * a.heads_q + g] = make_float2(m, den);
+        if (den != 0.0f) {
+            float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
 #pragma unroll
             for (int q = 0; q < NT; q++)
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int f = 32 * q + 8 * j + 4 * hh;
-                    h4 y;
-#pragma unroll
-                    for (int e = 0; e < 4; e++) y[e] = (_Float16)(o[t][q][4 * j + e] * inv);
-                    if (a.vec) {
-                        if (f < p.d) *(h4*)(dst + f) = y;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (f + e < p.d) dst[f + e] = y[e];
-                    }
+                for (int i = 0; i < 16; i++) {
+                    const int f = 32 * q + 8 * (i >> 2) + 4 * hh + (i & 3);
+                    if (f < p.d) dst[f] = o[q][i] * (1.0f / 127.0f);
                 }
         }
+    } else {
+        _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d;
+        const float inv = den != 0.0f ? (1.0f / 127.0f) / den : 0.0f;
+#pragma unroll
+        for (int q = 0; q < NT; q++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int f = 32 * q + 8 * j + 4 * hh;
+                h4 y;
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = (_Float16)(o[q][4 * j + e] * inv);
+                if (a.vec) {
+                    if (f < p.d) *(h4*)(dst + f) = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (f + e < p.d) dst[f + e] = y[e];
+                }
+            }
     }
 }
 
@@ -683,10 +770,10 @@ hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 {
     constexpr int bytes = 2 * 2 * 2 * DP * 32 * 2;
     if (bytes + 256 > 65536) {  // with the static part
-        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, 1, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    kv_prompt_kernel<DP, 1, WAVES><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES, bytes, st>>>(a);
+    kv_prompt_kernel<DP, WAVES><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES, bytes, st>>>(a);
     return hipGetLastError();
 }
 
@@ -704,7 +791,7 @@ KvPlan kv_plan(const Kv& p, int heads_q)
         r.tile = KV_STEP_ROWS, r.tiles = 0;
         units = (long long)p.n_seqs * p.heads;
     } else {
-        r.tile = rows > 128 && kv_dpad(p.d) <= 192 ? 256 : 128;
+        r.tile = rows > 128 && kv_dpad(p.d) <= 128 ? 256 : 128;
         const long long x = ((long long)p.n_rows * group + (long long)p.n_seqs * (r.tile - 1)) / r.tile, y = p.n_seqs * ((rows + r.tile - 1) / r.tile);
         r.tiles = (int)(x < y ? x : y);
         units = (long long)r.tiles * p.heads;
@@ -733,7 +820,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
         return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st) : plan.tile == 128 ? launch_prompt<DP, 4>(a, plan.tiles, st)
-                                                                                   : launch_prompt<(DP > 192 ? 192 : DP), 8>(a, plan.tiles, st);
+                                                                                   : launch_prompt<(DP > 128 ? 128 : DP), 8>(a, plan.tiles, st);
     };
     switch (dp) {
         case 32: e = pick(std::integral_constant<int, 32>()); break;

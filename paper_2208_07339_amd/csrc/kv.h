@@ -88,12 +88,12 @@ __device__ __forceinline__ bool kv_find(int n_seqs, int x, F count, int& b, int&
         }
         const unsigned long long past = __ballot(base + incl > x);
         if (past) {
-            const int l = __ffsll(past) - 1;
-            b = b0 + l;
-            i = x - base - __shfl(incl - c, l);
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll(past) - 1);
+            b = b0 + l;  // (the same for all lanes, and the compiler is to know it: what hangs on it stays scalar)
+            i = __builtin_amdgcn_readfirstlane(x - base - __builtin_amdgcn_readlane(incl - c, l));
             return true;
         }
-        base += __shfl(incl, 63);
+        base += __builtin_amdgcn_readlane(incl, 63);
     }
     return false;
 }
