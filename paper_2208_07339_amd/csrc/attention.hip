@@ -67,34 +67,32 @@ __device__ __forceinline__ float halves_max(float x)
     return fmaxf(x, y);
 }
 
-// Scores of N blocks of which the lane's row does not see all: those at positions outside lo .. hi - 1 out.  sc[y][i] is at position
-// pos0 + 32 y + 8 (i / 4) + 4 hh + i % 4.
-template <int N>
-__device__ __forceinline__ void hide(f16v (&sc)[N], int pos0, int hh, int lo, int hi)
+// Scores of a block of which the lane's row does not see all: those at positions outside lo .. hi - 1 out.  sc[i] is at position
+// pos0 + 8 (i / 4) + 4 hh + i % 4.
+__device__ __forceinline__ void hide(f16v& sc, int pos0, int hh, int lo, int hi)
 {
     const int l = lo - pos0 - 4 * hh, h = hi - pos0 - 4 * hh;
 #pragma unroll
-    for (int y = 0; y < N; y++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const int at = 32 * y + 8 * (i >> 2) + (i & 3);
-            if (at < l || at >= h) sc[y][i] = -__builtin_inff();
-        }
+    for (int i = 0; i < 16; i++) {
+        const int at = 8 * (i >> 2) + (i & 3);
+        sc[i] = ((at < l) | (at >= h)) ? -__builtin_inff() : sc[i];
+    }
 }
 
-// The running maximum with N blocks' raw scores; grown(f): M grew, sums are to be scaled by f.
-template <int N, class G>
-__device__ __forceinline__ void peak(const f16v (&sc)[N], const Factors (&fa)[N], float& M, float& l, G grown)
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float largest(const f16v& sc)
 {
-    float top = LOWEST;
+    float r = max3(sc[0], sc[1], sc[2]);
 #pragma unroll
-    for (int y = 0; y < N; y++) {
-        float mx = sc[y][0];
-#pragma unroll
-        for (int i = 1; i < 16; i++) mx = fmaxf(mx, sc[y][i]);
-        top = fmaxf(top, __builtin_fmaf(mx, fa[y].ks, fa[y].lcv));
-    }
-    top = halves_max(top);
+    for (int i = 3; i < 15; i += 2) r = max3(r, sc[i], sc[i + 1]);
+    return fmaxf(r, sc[15]);
+}
+
+// The running maximum with a block whose largest raw score in this lane is mx; grown(f): M grew, sums are to be scaled by f.
+template <class G>
+__device__ __forceinline__ void peak(float mx, const Factors& fa, float& M, float& l, G grown)
+{
+    const float top = halves_max(fmaxf(__builtin_fmaf(mx, fa.ks, fa.lcv), LOWEST));
     if (__any(top > M + GROW)) {
         const float n = fmaxf(M, top), f = exp2_(M - n);
         l *= f;
@@ -260,33 +258,33 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
             request(next, kn, vn);
         }
         if (!there) continue;
-        f16v sc[1] = {};
+        f16v sc = {};
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            sc[0] = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc[0]);
-            sc[0] = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc[0]);
+            sc = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc);
+            sc = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc);
         }
-        const Factors fa[1] = {factors(true, c, a.scale)};
+        const Factors fa = factors(true, c, a.scale);
         const int pos0 = (c0 + w + 4 * i) * KV_BLOCK;
-        h8 pf[1][2];
-        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide<1>(sc, pos0, hh, rlo, rhi);
-        peak<1>(sc, fa, m, l, rescale);
-        expo(sc[0], fa[0], m, l, pf[0]);
+        h8 pf[2];
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
+        peak(largest(sc), fa, m, l, rescale);
+        expo(sc, fa, m, l, pf);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0][0], o[t]);
-            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[0][1], o[t]);
+            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0], o[t]);
+            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[1], o[t]);
         }
     }
     // The open block, fp16: by the wave whose turn it is.  Its values are scaled by a power of two to what codes are, at most 128.
     if (closed >= c0 && closed < c1 && ((closed - c0) & 3) == w) {
         const int d = p.d, base = closed * KV_BLOCK;
-        f16v sc[1] = {};
+        f16v sc = {};
         const bool there = base + qr < s.len;
         const _Float16* row = (const _Float16*)kv_ring_row(p, s.slot, head, 0, base + qr);
 #pragma unroll
         for (int t = 0; t < DP / 16; t++)
-            sc[0] = mfma(there ? q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), d, d % 8 == 0) : h8{}, qf[t], sc[0]);
+            sc = mfma(there ? q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), d, d % 8 == 0) : h8{}, qf[t], sc);
         unsigned short v[NT][16], big = 0;
         const unsigned short* vals = kv_ring_row(p, s.slot, head, 1, base);
 #pragma unroll
@@ -305,18 +303,18 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
             top = y > top ? y : top;
         }
         const float unit = open_unit(top);
-        const Factors fa[1] = {factors(true, 1.0f, 127.0f * unit, a.scale)};
-        h8 pf[1][2];
-        hide<1>(sc, base, hh, rlo, rhi);
-        peak<1>(sc, fa, m, l, rescale);
-        expo(sc[0], fa[0], m, l, pf[0]);
+        const Factors fa = factors(true, 1.0f, 127.0f * unit, a.scale);
+        h8 pf[2];
+        hide(sc, base, hh, rlo, rhi);
+        peak(largest(sc), fa, m, l, rescale);
+        expo(sc, fa, m, l, pf);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             float y[16];
 #pragma unroll
             for (int i = 0; i < 16; i++) y[i] = f16_bits_to_float(v[t][i]) * (1.0f / unit);
-            o[t] = mfma(pack8(y), pf[0][0], o[t]);
-            o[t] = mfma(pack8(y + 8), pf[0][1], o[t]);
+            o[t] = mfma(pack8(y), pf[0], o[t]);
+            o[t] = mfma(pack8(y + 8), pf[1], o[t]);
         }
     }
 
@@ -373,8 +371,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
-    const int head = blockIdx.x % p.heads, split = blockIdx.y;  // the heads of a tile one after the other: with a multiple of 8
-                                                                // heads, a head's tiles all run on one XCD and share its L2
+    // the heads of a tile one after the other: with a multiple of 8 heads, a head's tiles all run on one XCD and share its L2
+    const int head = blockIdx.x % p.heads;
+    const int split = blockIdx.y;
     bool wrong = false;
     auto tiles = [&](int q) {
         KvSeq s;
@@ -429,48 +428,63 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
 #pragma unroll
         for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
     };
-    // Weights of block j from its scores, in slices between the products of the next block's scores, then its sums.  The order is
-    // fixed slice by slice: operands are read from LDS one slice ahead and no further, or registers run out.
-    auto step = [&](int j, const f16v& sc, const Factors& fa, f16v& next) {
-        constexpr int S = DP / 16;
+    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums, and between these
+    // products the weights' own sum and the next scores' maximum (returned; of scores of which some may have to be hidden).  other(x),
+    // x = 0 .. 3: a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS four slices
+    // ahead (its latency) and no further, or registers run out.
+    constexpr int S = DP / 16, AHEAD = S < 4 ? S : 4;
+    auto first_keys = [&](int j, h8 (&k)[AHEAD]) {
+        const h8* const kb = keys(j);
+#pragma unroll
+        for (int g = 0; g < AHEAD; g++) k[g] = kb[g * 64];
+    };
+    auto step = [&](int j, f16v& sc, const Factors& fa, f16v& next, h8 (&k)[AHEAD], auto other) {
         const h8 *const kb = keys(j + 1), *const vb = values(j);
         const float off = fa.lcv - m;
-        float sum = 0.0f;
-        h8 pf[2], k = kb[0], v[NT];
+        float sum = 0.0f, mx = 0.0f;
+        h8 pf[2], v[NT];
         next = f16v{};
 #pragma unroll
         for (int g = 0; g < S; g++) {
-            const h8 t = k;
-            if (g + 1 < S) k = kb[(g + 1) * 64];
-            next = mfma(t, qf[g], next);
-            if (g + 1 == S)
+            const h8 t = k[g % AHEAD];
+            if (g + AHEAD < S) k[g % AHEAD] = kb[(g + AHEAD) * 64];
 #pragma unroll
-                for (int q = 0; q < NT; q++) v[q] = vb[2 * q * 64];
+            for (int q = 0; q < NT; q++)  // the values' first operands over the last slices
+                if (g == S - AHEAD + q * AHEAD / NT) v[q] = vb[2 * q * 64];
+            next = mfma(t, qf[g], next);
 #pragma unroll
             for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
-                const float p0 = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), p1 = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
-                pf[i >> 3][i & 7] = (_Float16)p0, pf[i >> 3][(i & 7) + 1] = (_Float16)p1;
-                sum += p0;
-                sum += p1;
+                sc[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), sc[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
+                pf[i >> 3][i & 7] = (_Float16)sc[i], pf[i >> 3][(i & 7) + 1] = (_Float16)sc[i + 1];
+            }
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                if (g == x * S / 4) other(x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int u = 0; u < 2 * NT; u++) {
+            const int y = u / NT, q = u % NT;
+            const h8 t = v[q];
+            if (y == 0) v[q] = vb[(2 * q + 1) * 64];
+            o[q] = mfma(t, pf[y], o[q]);
+#pragma unroll
+            for (int i = 16 * u / (2 * NT); i < 16 * (u + 1) / (2 * NT); i++) {
+                sum += sc[i];
+                if (i == 8) mx = max3(next[0], next[1], next[2]);  // (the scores' last product is done by now)
+                if (i > 8) mx = max3(mx, next[2 * i - 15], next[2 * i - 14]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
         l = __builtin_fmaf(sum, fa.inv, l);
-#pragma unroll
-        for (int y = 0; y < 2; y++)
-#pragma unroll
-            for (int q = 0; q < NT; q++) {
-                const h8 t = v[q];
-                if (y == 0) v[q] = vb[(2 * q + 1) * 64];
-                o[q] = mfma(t, pf[y], o[q]);
-            }
-        __builtin_amdgcn_sched_barrier(0);
+        return max3(mx, next[15], next[15]);
     };
-    auto look = [&](int pos0, f16v& sc, const Factors& fa) {
-        f16v(&one)[1] = reinterpret_cast<f16v(&)[1]>(sc);
-        const Factors f[1] = {fa};
-        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide<1>(one, pos0, hh, rlo, rhi);
-        peak<1>(one, f, m, l, [&](float x) {
+    auto look = [&](int pos0, f16v& sc, float mx, const Factors& fa) {
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) {
+            hide(sc, pos0, hh, rlo, rhi);
+            mx = largest(sc);
+        }
+        peak(mx, fa, m, l, [&](float x) {
 #pragma unroll
             for (int q = 0; q < NT; q++) o[q] *= x;
         });
@@ -494,7 +508,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
-        const float unit = open_unit(big);
+        const float scale = open_unit(big);
         for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
             const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
             h8 y = {}, z = {};
@@ -502,22 +516,22 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
-                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / unit));
+                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / scale));
             }
             *((h8*)lds + t) = y;
             *((h8*)(lds + 4 * DP * 32) + t) = z;
         }
         __syncthreads();
         if (pos0 < some_hi) {
-            f16v sc[1];
-            scores(0, sc[0]);
-            const Factors fa[1] = {factors(true, 1.0f, 127.0f * unit, a.scale)};
+            f16v sc;
+            scores(0, sc);
+            const Factors fa = factors(true, 1.0f, 127.0f * scale, a.scale);
             int olo, ohi;
             seen(a, s.len, old + (w0 + qr) / a.group, olo, ohi);
-            hide<1>(sc, pos0, hh, olo, ohi < s.len ? ohi : s.len);
-            peak<1>(sc, fa, m, l, [](float) {});
+            hide(sc, pos0, hh, olo, ohi < s.len ? ohi : s.len);
+            peak(largest(sc), fa, m, l, [](float) {});
             h8 pf[2];
-            expo(sc[0], fa[0], m, l, pf);
+            expo(sc, fa, m, l, pf);
             const h8* const vb = values(0);
 #pragma unroll
             for (int y = 0; y < 2; y++)
@@ -527,10 +541,11 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         __syncthreads();
     }
 
-    // ---- Lane i of every wave looks up the i-th of 64 blocks, so that a stage waits neither for the page table nor for constants:
-    // `ahead` are the 64 blocks behind those in use.
+    // ---- Lane i of every wave looks up the i-th of 64 blocks, so that a stage waits neither for the page table nor for constants.
+    // `ahead` are 64 blocks from PERIOD behind the first of those in use on.
+    constexpr int PERIOD = 56;
     struct Looked {
-        int at[2];  // number in codes; -1: none
+        int at[2];  // number in codes
         Factors f;
     };
     auto look_up = [&](int j) {
@@ -551,41 +566,34 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     };
     Looked use, ahead;
     int j0 = 0;  // the first block of `use`
-    auto at_lane = [&](int x, int y, int j) {
-        const int i = j - j0, u = __builtin_amdgcn_readlane(x, i & 63), v = __builtin_amdgcn_readlane(y, i & 63);
-        return i < 64 ? u : v;
-    };
-    auto float_at = [&](float x, float y, int j) {
-        return __builtin_bit_cast(float, at_lane(__builtin_bit_cast(int, x), __builtin_bit_cast(int, y), j));
-    };
-    auto factors_of = [&](int j) {
-        return Factors{float_at(use.f.ks, ahead.f.ks, j), float_at(use.f.lcv, ahead.f.lcv, j), float_at(use.f.inv, ahead.f.inv, j)};
-    };
+    auto float_at = [&](float x, int j) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), j - j0)); };
+    auto factors_of = [&](int j) { return Factors{float_at(use.f.ks, j), float_at(use.f.lcv, j), float_at(use.f.inv, j)}; };
     // this thread's 16-byte pieces of the keys (value 0) or values of blocks j and j + 1
     auto request = [&](int j, int value, u4 (&piece)[PER]) {
 #pragma unroll
         for (int i = 0; i < PER; i++) {
             const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;  // a wave's pieces are of one block
             if (PIECES % THREADS && t >= PIECES) break;
-            const long long at = (long long)at_lane(use.at[1], ahead.at[1], j + x) << 32 | (unsigned)at_lane(use.at[0], ahead.at[0], j + x);
+            const long long at = (long long)__builtin_amdgcn_readlane(use.at[1], j + x - j0) << 32 |
+                                 (unsigned)__builtin_amdgcn_readlane(use.at[0], j + x - j0);
             piece[i] = *((const u4*)(p.codes + at * (2 * KV_BLOCK * DP)) + value * DP * 2 + u + lane);
         }
     };
-    auto deposit = [&](int j, int value, const u4 (&piece)[PER]) {
+    auto deposit_half = [&](int j, int value, const u4 (&piece)[PER], int half) {
 #pragma unroll
         for (int i = 0; i < PER; i++) {
             const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;
             if (PIECES % THREADS && t >= PIECES) break;
-            h8* dst = (value ? values(j + x) : keys(j + x)) + 2 * u;
-            dst[0] = codes8(piece[i][0], piece[i][1]), dst[64] = codes8(piece[i][2], piece[i][3]);
+            ((value ? values(j + x) : keys(j + x)) + 2 * u)[64 * half] = codes8(piece[i][2 * half], piece[i][2 * half + 1]);
         }
     };
+    auto deposit = [&](int j, int value, const u4 (&piece)[PER]) { deposit_half(j, value, piece, 0), deposit_half(j, value, piece, 1); };
 
     // ---- Stage st: blocks 2 st and 2 st + 1 (from c0 on): their weights and sums, and each time the scores of the block behind.  So keys
     // go to LDS one block earlier than values: meanwhile those of 2 st + 3 and 2 st + 4, and the values of 2 st + 2 and 2 st + 3.
     if (stages) {
         u4 pk[PER], pv[PER];
-        use = look_up(0), ahead = look_up(64);
+        use = look_up(0), ahead = look_up(PERIOD);
         request(0, 0, pk), request(0, 1, pv);
         deposit(0, 0, pk), deposit(0, 1, pv);
         request(1, 0, pk);
@@ -593,11 +601,10 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         deposit(1, 0, pk);
         request(3, 0, pk), request(2, 1, pv);
         __syncthreads();
-        auto supply = [&](int st) {  // the end of a stage
-            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
-            if (2 * st + 2 == j0 + 64) {
-                use = ahead, j0 += 64;
-                ahead = look_up(j0 + 64);
+        auto more = [&](int st) {  // the end of a stage
+            if (2 * st + 2 == j0 + PERIOD) {
+                use = ahead, j0 += PERIOD;
+                ahead = look_up(j0 + PERIOD);
             }
             request(2 * st + 5, 0, pk), request(2 * st + 4, 1, pv);
             __syncthreads();
@@ -608,26 +615,38 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         auto enter = [&]() {
             scores(2 * sa, s0);
             f0 = factors_of(2 * sa);
-            look((c0 + 2 * sa) * KV_BLOCK, s0, f0);
+            look((c0 + 2 * sa) * KV_BLOCK, s0, largest(s0), f0);
         };
         if (sa == 0) enter();
         __syncthreads();
         int st = 0;
         for (; st < sa; st++) {
             if (st + 1 == sa) enter();
-            supply(st);
+            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
+            more(st);
         }
         for (; st < sb; st++) {
             const int pos0 = (c0 + 2 * st) * KV_BLOCK;
-            step(2 * st, s0, f0, s1);
+            h8 k[AHEAD];
+            first_keys(2 * st + 1, k);
+            float mx = step(2 * st, s0, f0, s1, k, [&](int x) {
+                if (x & 1) deposit_half(2 * st + 3, 0, pk, x >> 1);
+            });
+            first_keys(2 * st + 2, k);
             const Factors f1 = factors_of(2 * st + 1);
-            look(pos0 + KV_BLOCK, s1, f1);
-            step(2 * st + 1, s1, f1, s0);
+            look(pos0 + KV_BLOCK, s1, mx, f1);
+            mx = step(2 * st + 1, s1, f1, s0, k, [&](int x) {
+                if (x & 1) deposit_half(2 * st + 2, 1, pv, x >> 1);
+            });
             f0 = factors_of(2 * st + 2);
-            look(pos0 + 2 * KV_BLOCK, s0, f0);
-            supply(st);
+            if (w < 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
+            more(st);
+            if (w >= 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
         }
-        for (; st < stages; st++) supply(st);
+        for (; st < stages; st++) {
+            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
+            more(st);
+        }
     }
 
     const long long total = (long long)p.n_rows * a.heads_q;
