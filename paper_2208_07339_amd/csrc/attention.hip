@@ -629,14 +629,12 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             const int pos0 = (c0 + 2 * st) * KV_BLOCK;
             h8 k[AHEAD];
             first_keys(2 * st + 1, k);
-            float mx = step(2 * st, s0, f0, s1, k, [&](int x) {
-                if (x & 1) deposit_half(2 * st + 3, 0, pk, x >> 1);
-            });
+            float mx = step(2 * st, s0, f0, s1, k, [](int) {});
             first_keys(2 * st + 2, k);
             const Factors f1 = factors_of(2 * st + 1);
             look(pos0 + KV_BLOCK, s1, mx, f1);
             mx = step(2 * st + 1, s1, f1, s0, k, [&](int x) {
-                if (x & 1) deposit_half(2 * st + 2, 1, pv, x >> 1);
+                deposit_half(2 * st + (x < 2 ? 3 : 2), x >> 1, x < 2 ? pk : pv, x & 1);
             });
             f0 = factors_of(2 * st + 2);
             if (w < 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
