@@ -124,7 +124,7 @@ struct AttendArgs {
     int heads_q, group;  // group: query heads to a key head
     float scale;         // log2(e) included
     int causal, window;
-    int splits;
+    int splits, tiles;  // tiles: of 32 rows to a sequence, few rows
     float* part;   // [split][row * heads_q + head][d] sums, not divided
     float2* stat;  // [split][row * heads_q + head] (m, l)
     bool vec;      // d and the rows of q allow 16-byte accesses
@@ -161,6 +161,15 @@ __device__ __forceinline__ void seen(const AttendArgs& a, int len, int pos, int&
     lo = a.window && pos >= a.window ? pos - a.window + 1 : 0;
 }
 
+// Blocks to a part where `blocks` are cut into at most `parts`, a multiple of `step`: not fewer than 8, so that short sequences are not
+// cut into parts that cost more than they have to do
+__host__ __device__ inline int chunk_of(int blocks, int parts, int step)
+{
+    int c = (blocks + parts - 1) / parts;
+    if (parts > 1 && c < 8) c = 8;
+    return (c + step - 1) / step * step;
+}
+
 // The open block's values are taken in units of this power of two, so that the largest (fp16 bits) is at most 128 of them
 __device__ __forceinline__ float open_unit(unsigned largest)
 {
@@ -172,39 +181,49 @@ __device__ __forceinline__ float open_unit(unsigned largest)
 // Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
 // every wave blocks of its own; sums meet in LDS.  Bound by HBM.
 // ---------------------------------------------------------------------------------------------------------------------------
+constexpr int JOIN_FLOATS = 32 * 36;  // for a wave's sums in LDS: 32 rows of 32 features, or fewer of more
+
 template <int DP>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const AttendArgs a)
 {
     constexpr int NT = DP / 32;
-    __shared__ float s_o[4][32][33];
+    __shared__ __align__(16) float s_o[4 * JOIN_FLOATS];
     __shared__ float s_m[4][32], s_l[4][32];
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
-    const int head = blockIdx.x % p.heads, b = blockIdx.x / p.heads, split = blockIdx.y;
+    // Workgroups go to the eight XCDs in turn: the row tiles of one part of one sequence's positions run on one XCD, one after the
+    // other, and find the codes in its L2.
+    const int turn = blockIdx.x / 8, unit = turn / a.tiles * 8 + blockIdx.x % 8, tile = turn % a.tiles;
+    const int split = unit % a.splits, head = unit / a.splits % p.heads, b = unit / a.splits / p.heads;
+    if (b >= p.n_seqs) return;
     KvSeq s;
     const bool ok = kv_seq(p, b, s);
     if (!ok && tid == 0) kv_flag(p, LLMINT8_KV_BAD_BATCH);
-    const int rows = s.n * a.group;  // <= 32
-    if (rows == 0) return;
+    const int r0 = 32 * tile, rows = s.n * a.group - r0 < 32 ? s.n * a.group - r0 : 32;  // this tile's
+    if (rows <= 0) return;
+    const int top_pos = s.len - s.n + (r0 + rows - 1) / a.group, low_pos = s.len - s.n + r0 / a.group;
 
     // blocks that some row sees, and this workgroup's part of them
-    int lo, hi, first, end, x0, x1;
-    seen(a, s.len, s.len - 1, x0, hi);
-    seen(a, s.len, s.len - s.n, lo, x1);
-    first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
-    const int chunk = (end - first + a.splits - 1) / a.splits;
+    // (lo, all_hi: of the first row; all_lo, hi: of the last.  Blocks before all_lo or behind all_hi need a mask.)
+    int lo, hi, all_lo, all_hi;
+    seen(a, s.len, top_pos, all_lo, hi);
+    seen(a, s.len, low_pos, lo, all_hi);
+    const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
+    const int chunk = chunk_of(end - first, a.splits, 1);
     const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
     const int closed = s.len / KV_BLOCK;  // blocks held as codes
+    const long long total = (long long)p.n_rows * a.heads_q;
+    if (split && c0 >= c1) {  // nothing left for this part
+        if (tid < rows)
+            a.stat[split * total + (s.row0 + (r0 + tid) / a.group) * (long long)a.heads_q + head * a.group + (r0 + tid) % a.group] = make_float2(LOWEST, 0.0f);
+        return;
+    }
     const int k1 = c1 < closed ? c1 : closed;
 
     h8 qf[DP / 16];
-    load_q<DP>(a, s, head, qr, hh, qf);
+    load_q<DP>(a, s, head, r0 + qr, hh, qf);
     int rlo, rhi;  // what this lane's row sees
-    seen(a, s.len, s.len - s.n + qr / a.group, rlo, rhi);
-    // blocks before / behind which a mask is needed: that of the last row's start, of the first row's end
-    int all_lo, all_hi;
-    seen(a, s.len, s.len - 1, all_lo, x1);
-    seen(a, s.len, s.len - s.n, x0, all_hi);
+    seen(a, s.len, s.len - s.n + (r0 + qr) / a.group, rlo, rhi);
 
     f16v o[NT];
 #pragma unroll
@@ -326,33 +345,58 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         const float top = fmaxf(fmaxf(s_m[0][qr], s_m[1][qr]), fmaxf(s_m[2][qr], s_m[3][qr]));
         rescale(exp2_(m - top) * (1.0f / 127.0f));
     }
-    const long long total = (long long)p.n_rows * a.heads_q;
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
+    // as many tiles of 32 features at a time as LDS has room for; rows are 4 floats longer than their data, for the banks
+    const int fit = (JOIN_FLOATS / rows - 4) / 32, nt = fit < NT ? fit : NT, pitch = 32 * nt + 4;
+    for (int t0 = 0; t0 < NT; t0 += nt) {
+        if (t0) __syncthreads();
         if (qr < rows)
 #pragma unroll
-            for (int i = 0; i < 16; i++) s_o[w][8 * (i >> 2) + 4 * hh + (i & 3)][qr] = o[t][i];
+            for (int t = 0; t < NT; t++)
+                if (t >= t0 && t < t0 + nt)
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        *(f4*)(s_o + (w * rows + qr) * pitch + 32 * (t - t0) + 8 * j + 4 * hh) =
+                            f4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
         __syncthreads();
-        for (int x = tid; x < 32 * rows; x += 256) {
-            const int f = x & 31, r = x >> 5;
+        const int quads = 8 * nt;  // of features
+        for (int x = tid; x < quads * rows; x += 256) {
+            const int f = 4 * (x % quads), r = x / quads, at = 32 * t0 + f;
+            if (at >= p.d) continue;
             const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
-            float sum = 0.0f, den = 0.0f;
+            f4 sum = {};
+            float den = 0.0f;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                sum += s_o[q][f][r];
+                const f4 y = *(const f4*)(s_o + (q * rows + r) * pitch + f);
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum[e] += y[e];
                 den += s_l[q][r] * exp2_(s_m[q][r] - top);
             }
-            const long long row = s.row0 + r / a.group;
-            const int g = head * a.group + r % a.group;
-            if (32 * t + f < p.d) {
-                if (a.splits == 1)
-                    a.out[row * a.ld_out + (long long)g * p.d + 32 * t + f] = (_Float16)(den != 0.0f ? sum / den : 0.0f);
-                else if (den != 0.0f)
-                    a.part[((long long)split * total + row * a.heads_q + g) * p.d + 32 * t + f] = sum;
+            const long long row = s.row0 + (r0 + r) / a.group;
+            const int g = head * a.group + (r0 + r) % a.group;
+            const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+            if (a.splits > 1) {
+                const long long at_row = split * total + row * a.heads_q + g;
+                if (at == 0) a.stat[at_row] = make_float2(top, den);
+                float* dst = a.part + at_row * p.d + at;
+                if (p.d % 4 == 0) {
+                    *(f4*)dst = sum;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (at + e < p.d) dst[e] = sum[e];
+                }
+            } else {
+                _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d + at;
+                if (a.vec) {
+                    *(h4*)dst = h4{(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv), (_Float16)(sum[3] * inv)};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (at + e < p.d) dst[e] = (_Float16)(sum[e] * inv);
+                }
             }
-            if (t == 0 && f == 0 && a.splits > 1) a.stat[split * total + row * a.heads_q + g] = make_float2(top, den);
         }
-        __syncthreads();
     }
 }
 
@@ -362,15 +406,17 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 // for all rows.  Bound by the matrix units and by what makes scores weights, which are kept busy at the same time: the scores of the
 // next stage are computed while the weights of this one are.  So LDS holds keys one stage ahead of values.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
+template <int DP, int WAVES, int GROUPS>
+__global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
 {
-    constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+    constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;  // of a group
     constexpr int PIECES = DP * 4, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' keys, or values; to a thread
-    extern __shared__ __align__(16) _Float16 lds[];                         // [keys, values][4 blocks][DP * 32]
+    extern __shared__ __align__(16) _Float16 all_lds[];                     // [group][keys, values][4 blocks][DP * 32]
     __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = GROUPS > 1 ? wave / WAVES : 0;
+    const int tid = threadIdx.x % THREADS, lane = tid & 63, w = wave % WAVES, qr = lane & 31, hh = lane >> 5;
+    _Float16* const lds = all_lds + group * (8 * DP * 32);
     // the heads of a tile one after the other: with a multiple of 8 heads, a head's tiles all run on one XCD and share its L2
     const int head = blockIdx.x % p.heads;
     const int split = blockIdx.y;
@@ -395,10 +441,25 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     seen(a, s.len, old + r0 / a.group, lo, x1);
     seen(a, s.len, old + (r1 - 1) / a.group, x0, hi);
     const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
-    const int chunk = ((end - first + a.splits - 1) / a.splits + 1) & ~1;
-    const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
+    const int chunk = chunk_of(end - first, a.splits, 2 * GROUPS);
+    const int b0 = first + split * chunk, b1 = b0 + chunk < end ? b0 + chunk : end;
+    const int part = GROUPS > 1 ? chunk_of(b1 - b0, GROUPS, 2) : chunk;  // a group's
+    const int c0 = b0 + group * part, c1 = c0 + part < b1 ? c0 + part : b1;
     const int closed = s.len / KV_BLOCK, k1 = c1 < closed ? c1 : closed;
     const int stages = k1 > c0 ? (k1 - c0 + 1) / 2 : 0;
+    // the most that a group has (the first one's): all take part in as many barriers
+    int most = stages;
+    if (GROUPS > 1) {
+        int e = b0 + part < b1 ? b0 + part : b1;
+        e = e < closed ? e : closed;
+        most = e > b0 ? (e - b0 + 1) / 2 : 0;
+    }
+    const long long total = (long long)p.n_rows * a.heads_q;
+    if (split && b0 >= b1) {  // nothing left for this part
+        for (int r = r0 + (int)threadIdx.x; r < r1; r += THREADS * GROUPS)
+            a.stat[split * total + (s.row0 + r / a.group) * (long long)a.heads_q + head * a.group + r % a.group] = make_float2(LOWEST, 0.0f);
+        return;
+    }
     // what all of the wave's rows see, and the stages in which some see anything
     int some_lo = 0, some_hi = 0, all_lo = 0, all_hi = 0;
     if (w0 < w1) {
@@ -490,12 +551,13 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         });
     };
 
-    // ---- the open block, fp16 from the ring, before the others
-    if (closed >= c0 && closed < c1) {
+    // ---- the open block, fp16 from the ring, before the others: the last group's
+    const bool mine = GROUPS == 1 || group == GROUPS - 1;
+    if (closed >= b0 && closed < b1) {
         const int d = p.d, pos0 = closed * KV_BLOCK;
         const unsigned short *const krows = kv_ring_row(p, s.slot, head, 0, pos0), *const vrows = kv_ring_row(p, s.slot, head, 1, pos0);
         int big = 0;
-        for (int t = tid; t < (s.len - pos0) * d; t += THREADS) {
+        for (int t = tid; mine && t < (s.len - pos0) * d; t += THREADS) {
             const int y = vrows[t] & 0x7fff;
             big = y > big ? y : big;
         }
@@ -504,12 +566,12 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             const int y = __shfl_xor(big, x);
             big = y > big ? y : big;
         }
-        if (lane == 0) s_big[w] = big;
+        if (mine && lane == 0) s_big[w] = big;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
         const float scale = open_unit(big);
-        for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
+        for (int t = tid; mine && t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
             const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
             h8 y = {}, z = {};
             if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
@@ -522,7 +584,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             *((h8*)(lds + 4 * DP * 32) + t) = z;
         }
         __syncthreads();
-        if (pos0 < some_hi) {
+        if (mine && pos0 < some_hi) {
             f16v sc;
             scores(0, sc);
             const Factors fa = factors(true, 1.0f, 127.0f * scale, a.scale);
@@ -591,15 +653,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
 
     // ---- Stage st: blocks 2 st and 2 st + 1 (from c0 on): their weights and sums, and each time the scores of the block behind.  So keys
     // go to LDS one block earlier than values: meanwhile those of 2 st + 3 and 2 st + 4, and the values of 2 st + 2 and 2 st + 3.
-    if (stages) {
+    if (most > 0) {
         u4 pk[PER], pv[PER];
         use = look_up(0), ahead = look_up(PERIOD);
-        request(0, 0, pk), request(0, 1, pv);
-        deposit(0, 0, pk), deposit(0, 1, pv);
-        request(1, 0, pk);
-        __syncthreads();  // (block 1's keys come twice)
-        deposit(1, 0, pk);
-        request(3, 0, pk), request(2, 1, pv);
+        {
+            u4 k0[PER], k1[PER], v0[PER];
+            request(0, 0, k0), request(1, 0, k1), request(0, 1, v0), request(3, 0, pk), request(2, 1, pv);
+            deposit(0, 0, k0);
+            __syncthreads();  // (block 1's keys come twice)
+            deposit(1, 0, k1), deposit(0, 1, v0);
+        }
         __syncthreads();
         auto more = [&](int st) {  // the end of a stage
             if (2 * st + 2 == j0 + PERIOD) {
@@ -637,34 +700,67 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
                 deposit_half(2 * st + (x < 2 ? 3 : 2), x >> 1, x < 2 ? pk : pv, x & 1);
             });
             f0 = factors_of(2 * st + 2);
-            if (w < 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
+            // Four of the eight waves (two to a SIMD) do this behind the barrier: the two are then not at the same place.
+            if (wave < 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
             more(st);
-            if (w >= 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
+            if (wave >= 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
         }
         for (; st < stages; st++) {
             deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
             more(st);
         }
+        if (GROUPS > 1)
+            for (; st < most; st++) __syncthreads();
     }
 
-    const long long total = (long long)p.n_rows * a.heads_q;
-    const float den = l + __shfl_xor(l, 32);
+    float den = l + __shfl_xor(l, 32);
+    if (GROUPS > 1) {  // the second group's sums to the first, through LDS, 32 features at a time a wave
+        float* const mine_m = (float*)all_lds + w * 64 + lane;
+        f4* const mine_o = (f4*)((float*)all_lds + 2 * THREADS) + w * 64 + lane;
+        __syncthreads();
+        if (group) mine_m[0] = m, mine_m[THREADS] = den;
+        if (group)
+#pragma unroll
+            for (int q = 0; q < NT; q++)
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    mine_o[(4 * q + j) * THREADS] = f4{o[q][4 * j], o[q][4 * j + 1], o[q][4 * j + 2], o[q][4 * j + 3]};
+        __syncthreads();
+        if (group) return;
+        const float m2 = mine_m[0], n = fmaxf(m, m2), f = exp2_(m - n), f2 = exp2_(m2 - n);
+        den = den * f + mine_m[THREADS] * f2;
+        m = n;
+#pragma unroll
+        for (int q = 0; q < NT; q++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const f4 y = mine_o[(4 * q + j) * THREADS];
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[q][4 * j + e] = o[q][4 * j + e] * f + y[e] * f2;
+            }
+    }
     const int r = w0 + qr;
     if (r >= r1) return;
     const long long row = s.row0 + r / a.group;
     const int g = head * a.group + r % a.group;
     if (a.splits > 1) {
         if (hh == 0) a.stat[split * total + row * a.heads_q + g] = make_float2(m, den);
-        if (den != 0.0f) {
-            float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
+        float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
 #pragma unroll
-            for (int q = 0; q < NT; q++)
+        for (int q = 0; q < NT; q++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const int f = 32 * q + 8 * (i >> 2) + 4 * hh + (i & 3);
-                    if (f < p.d) dst[f] = o[q][i] * (1.0f / 127.0f);
+            for (int j = 0; j < 4; j++) {
+                const int f = 32 * q + 8 * j + 4 * hh;
+                const float u = 1.0f / 127.0f;
+                const f4 y = {o[q][4 * j] * u, o[q][4 * j + 1] * u, o[q][4 * j + 2] * u, o[q][4 * j + 3] * u};
+                if (p.d % 4 == 0) {
+                    if (f < p.d) *(f4*)(dst + f) = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (f + e < p.d) dst[f + e] = y[e];
                 }
-        }
+            }
     } else {
         _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d;
         const float inv = den != 0.0f ? (1.0f / 127.0f) / den : 0.0f;
@@ -687,17 +783,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     }
 }
 
-// Joins the splits: WAVES waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the splits dealt
-// out over the waves and their quarters, four in flight each.
-template <int WAVES>
+// Joins the splits, many of them: four waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the
+// splits dealt out over the waves and their quarters, four in flight each.  A part that had nothing to do has l = 0, and its sums
+// were not written.
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 {
     constexpr int NQ = KV_MAX_D / 64;
-    __shared__ f4 s_sum[WAVES > 1 ? WAVES : 1][NQ][16];
-    __shared__ float s_den[WAVES > 1 ? WAVES : 1];
-    const int tid = threadIdx.x, lane = tid & 63, d = a.kv.d, w = WAVES > 1 ? tid >> 6 : 0;
-    const long long total = (long long)a.kv.n_rows * a.heads_q, x = WAVES > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + (tid >> 6);
-    if (x >= total) return;
+    __shared__ f4 s_sum[4][NQ][16];
+    __shared__ float s_den[4];
+    const int tid = threadIdx.x, lane = tid & 63, d = a.kv.d, w = tid >> 6;
+    const long long total = (long long)a.kv.n_rows * a.heads_q, x = blockIdx.x;
     float top = LOWEST;
     for (int s = lane; s < a.splits; s += 64) {
         const float2 t = a.stat[s * total + x];
@@ -708,20 +803,21 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
     const int part = lane >> 4, f0 = 4 * (lane & 15);
     f4 sum[NQ] = {};
     float den = 0.0f;
-    for (int s0 = 4 * w + part; s0 < a.splits; s0 += 16 * WAVES) {
+    for (int s0 = 4 * w + part; s0 < a.splits; s0 += 64) {
         f4 v[4][NQ];
         float f[4];
 #pragma unroll
         for (int u = 0; u < 4; u++) {
-            const int s = s0 + 4 * WAVES * u;
-            const float2 t = s < a.splits ? a.stat[s * total + x] : make_float2(0.0f, 0.0f);
+            const int s = s0 + 16 * u;
+            const bool there = s < a.splits;
+            const float2 t = there ? a.stat[s * total + x] : make_float2(0.0f, 0.0f);
+            const float* src = a.part + (s * total + x) * d + f0;
             f[u] = t.y != 0.0f ? exp2_(t.x - top) : 0.0f;
             den += f[u] * t.y;
-            const float* src = a.part + (s * total + x) * d + f0;
 #pragma unroll
             for (int q = 0; q < NQ; q++) {
                 v[u][q] = f4{};
-                if (t.y != 0.0f && f0 + 64 * q < d) {
+                if (there && f0 + 64 * q < d) {
                     if (d % 4 == 0) {
                         v[u][q] = *(const f4*)(src + 64 * q);
                     } else {
@@ -734,10 +830,11 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
         }
 #pragma unroll
         for (int u = 0; u < 4; u++)
+            if (f[u] != 0.0f)
 #pragma unroll
-            for (int q = 0; q < NQ; q++)
+                for (int q = 0; q < NQ; q++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) sum[q][e] += f[u] * v[u][q][e];
+                    for (int e = 0; e < 4; e++) sum[q][e] += f[u] * v[u][q][e];
     }
 #pragma unroll
     for (int y = 16; y < 64; y <<= 1) {
@@ -747,50 +844,89 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 #pragma unroll
             for (int e = 0; e < 4; e++) sum[q][e] += __shfl_xor(sum[q][e], y);
     }
-    if (WAVES > 1) {
-        if (lane < 16)
+    if (lane < 16)
 #pragma unroll
-            for (int q = 0; q < NQ; q++) s_sum[w][q][lane] = sum[q];
-        if (lane == 0) s_den[w] = den;
-        __syncthreads();
-        if (w) return;
-        den = 0.0f;
-#pragma unroll
-        for (int y = 0; y < WAVES; y++) den += s_den[y];
-#pragma unroll
-        for (int q = 0; q < NQ; q++) {
-            sum[q] = f4{};
-#pragma unroll
-            for (int y = 0; y < WAVES; y++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) sum[q][e] += s_sum[y][q][lane & 15][e];
-        }
-    }
-    if (lane >= 16) return;
+        for (int q = 0; q < NQ; q++) s_sum[w][q][lane] = sum[q];
+    if (lane == 0) s_den[w] = den;
+    __syncthreads();
+    if (w || lane >= 16) return;
+    den = s_den[0] + s_den[1] + s_den[2] + s_den[3];
     _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d + f0;
 #pragma unroll
     for (int q = 0; q < NQ; q++)
 #pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float y = s_sum[0][q][lane][e] + s_sum[1][q][lane][e] + s_sum[2][q][lane][e] + s_sum[3][q][lane][e];
+            if (f0 + 64 * q + e < d) dst[64 * q + e] = (_Float16)(den != 0.0f ? y / den : 0.0f);
+        }
+}
+
+// The same for up to eight: a thread to four features of a row and head.
+constexpr int FEW = 8;
+__global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
+{
+    const int d = a.kv.d, quads = (d + 3) / 4;
+    const long long total = (long long)a.kv.n_rows * a.heads_q, t = (long long)blockIdx.x * 256 + threadIdx.x, x = t / quads;
+    if (x >= total) return;
+    const int f0 = 4 * (int)(t - x * quads);
+    float2 st[FEW];
+    f4 v[FEW];
+#pragma unroll
+    for (int s = 0; s < FEW; s++) {
+        st[s] = s < a.splits ? a.stat[s * total + x] : make_float2(LOWEST, 0.0f);
+        v[s] = f4{};
+        if (s < a.splits) {
+            const float* src = a.part + (s * total + x) * d + f0;
+            if (d % 4 == 0) {
+                v[s] = *(const f4*)src;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (f0 + e < d) v[s][e] = src[e];
+            }
+        }
+    }
+    float top = LOWEST, den = 0.0f;
+#pragma unroll
+    for (int s = 0; s < FEW; s++)
+        if (st[s].y != 0.0f) top = fmaxf(top, st[s].x);
+    f4 sum = {};
+#pragma unroll
+    for (int s = 0; s < FEW; s++)
+        if (st[s].y != 0.0f) {
+            const float f = exp2_(st[s].x - top);
+            den += f * st[s].y;
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += f * v[s][e];
+        }
+    const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+    _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d + f0;
+    if (a.vec) {
+        *(h4*)dst = h4{(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv), (_Float16)(sum[3] * inv)};
+    } else {
+#pragma unroll
         for (int e = 0; e < 4; e++)
-            if (f0 + 64 * q + e < d) dst[64 * q + e] = (_Float16)(den != 0.0f ? sum[q][e] / den : 0.0f);
+            if (f0 + e < d) dst[e] = (_Float16)(sum[e] * inv);
+    }
 }
 
 template <int DP>
 hipError_t launch_step(const AttendArgs& a, hipStream_t st)
 {
-    kv_step_kernel<DP><<<dim3(a.kv.heads * a.kv.n_seqs, a.splits), 256, 0, st>>>(a);
+    const long long units = (long long)a.kv.heads * a.kv.n_seqs * a.splits;
+    kv_step_kernel<DP><<<(unsigned)((units + 7) / 8 * 8 * a.tiles), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-template <int DP, int WAVES>
+template <int DP, int WAVES, int GROUPS>
 hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 {
-    constexpr int bytes = 2 * 2 * 2 * DP * 32 * 2;
+    constexpr int bytes = GROUPS * 8 * DP * 32 * 2;
     if (bytes + 256 > 65536) {  // with the static part
-        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES, GROUPS>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    kv_prompt_kernel<DP, WAVES><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES, bytes, st>>>(a);
+    kv_prompt_kernel<DP, WAVES, GROUPS><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES * GROUPS, bytes, st>>>(a);
     return hipGetLastError();
 }
 
@@ -801,19 +937,22 @@ constexpr int KV_STEP_ROWS = 32;
 KvPlan kv_plan(const Kv& p, int heads_q)
 {
     KvPlan r;
-    const long long group = heads_q / p.heads, rows = p.max_rows * group;
+    const long long group = heads_q / p.heads, rows = p.max_rows * group, all = p.n_rows * group;
     const int blocks = (p.max_len + KV_BLOCK - 1) / KV_BLOCK;
+    const bool wide = kv_dpad(p.d) > 128;
+    auto tiles = [&](long long t) {  // of t rows, that all sequences have together, at most
+        const long long x = (all + p.n_seqs * (t - 1)) / t, y = p.n_seqs * ((rows + t - 1) / t);
+        return x < y ? x : y;
+    };
     long long units;
     if (rows <= KV_STEP_ROWS) {
-        r.tile = KV_STEP_ROWS, r.tiles = 0;
+        r.tile = KV_STEP_ROWS, r.groups = 1, r.tiles = 1;
         units = (long long)p.n_seqs * p.heads;
     } else {
-        r.tile = rows > 128 && kv_dpad(p.d) <= 128 ? 256 : 128;
-        const long long x = ((long long)p.n_rows * group + (long long)p.n_seqs * (r.tile - 1)) / r.tile, y = p.n_seqs * ((rows + r.tile - 1) / r.tile);
-        r.tiles = (int)(x < y ? x : y);
-        units = (long long)r.tiles * p.heads;
+        r.tile = rows > 128 && !wide ? 256 : 128, r.groups = 1;
+        units = (r.tiles = (int)tiles(r.tile)) * p.heads;
     }
-    const long long want = (r.tile == KV_STEP_ROWS ? 1024 : r.tile == 128 ? 512 : 256) / units, most = blocks / 8;
+    const long long want = (r.tile == KV_STEP_ROWS || r.tile * r.groups == 128 ? 512 : 256) / units, most = (blocks + 7) / 8;
     r.splits = (int)(want < most ? want : most);
     if (r.splits < 1) r.splits = 1;
     return r;
@@ -828,7 +967,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
 {
     AttendArgs a;
     a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
-    a.group = c.heads_q / p.heads, a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = plan.splits;
+    a.group = c.heads_q / p.heads, a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = plan.splits, a.tiles = plan.tiles;
     const size_t total = (size_t)p.n_rows * c.heads_q;
     a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));
     a.vec = p.d % 8 == 0 && ((((uintptr_t)c.q | (uintptr_t)c.out) & 15) | (c.ld_q & 7) | (c.ld_out & 7)) == 0;
@@ -836,8 +975,11 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     hipError_t e;
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
-        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st) : plan.tile == 128 ? launch_prompt<DP, 4>(a, plan.tiles, st)
-                                                                                   : launch_prompt<(DP > 128 ? 128 : DP), 8>(a, plan.tiles, st);
+        constexpr int NARROW = DP > 128 ? 128 : DP;  // what kv_plan gives the two others
+        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st)
+               : plan.tile == 256        ? launch_prompt<NARROW, 8, 1>(a, plan.tiles, st)
+               : plan.groups == 2        ? launch_prompt<NARROW, 4, 2>(a, plan.tiles, st)
+                                         : launch_prompt<DP, 4, 1>(a, plan.tiles, st);
     };
     switch (dp) {
         case 32: e = pick(std::integral_constant<int, 32>()); break;
@@ -850,10 +992,10 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
         default: e = pick(std::integral_constant<int, 256>()); break;
     }
     if (e != hipSuccess || plan.splits == 1) return e;
-    if (plan.splits > 8)
-        kv_join_kernel<4><<<(unsigned)total, 256, 0, st>>>(a);
+    if (plan.splits > FEW)
+        kv_join_kernel<<<(unsigned)total, 256, 0, st>>>(a);
     else
-        kv_join_kernel<1><<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a);
+        kv_join_few_kernel<<<(unsigned)((total * ((p.d + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -137,7 +137,8 @@ struct KvAttend {  // the rest of llmint8_kv_attention's arguments
 // How a call's work is cut up: host arithmetic on the sizes alone.
 struct KvPlan {
     int tile;    // rows (of all query heads that share keys) to a workgroup
-    int tiles;   // tiles that the sequences have together, at most (tile > KV_STEP_ROWS)
+    int tiles;   // tiles that a sequence has at most (tile = KV_STEP_ROWS), or that all have together
+    int groups;  // of four waves in a workgroup of 128 rows, that share its positions
     int splits;  // parts of the positions, joined by a kernel of their own if more than one
 };
 KvPlan kv_plan(const Kv& p, int heads_q);
