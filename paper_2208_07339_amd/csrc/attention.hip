@@ -71,12 +71,10 @@ __device__ __forceinline__ float halves_max(float x)
 // pos0 + 8 (i / 4) + 4 hh + i % 4.
 __device__ __forceinline__ void hide(f16v& sc, int pos0, int hh, int lo, int hi)
 {
-    const int l = lo - pos0 - 4 * hh, h = hi - pos0 - 4 * hh;
+    const int from = lo - pos0 - 4 * hh, n = hi - lo;  // of the block's positions: from .. from + n - 1
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int at = 8 * (i >> 2) + (i & 3);
-        sc[i] = ((at < l) | (at >= h)) ? -__builtin_inff() : sc[i];
-    }
+    for (int i = 0; i < 16; i++)
+        if ((unsigned)(8 * (i >> 2) + (i & 3) - from) >= (unsigned)(n < 0 ? 0 : n)) sc[i] = -__builtin_inff();
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
@@ -88,11 +86,16 @@ __device__ __forceinline__ float largest(const f16v& sc)
     return fmaxf(r, sc[15]);
 }
 
-// The running maximum with a block whose largest raw score in this lane is mx; grown(f): M grew, sums are to be scaled by f.
-template <class G>
-__device__ __forceinline__ void peak(float mx, const Factors& fa, float& M, float& l, G grown)
+// the largest y of a row in a block, both halves
+__device__ __forceinline__ float top_of(const f16v& sc, const Factors& fa)
 {
-    const float top = halves_max(fmaxf(__builtin_fmaf(mx, fa.ks, fa.lcv), LOWEST));
+    return halves_max(fmaxf(__builtin_fmaf(largest(sc), fa.ks, fa.lcv), LOWEST));
+}
+
+// The running maximum with a block's `top`; grown(f): M grew, sums are to be scaled by f.
+template <class G>
+__device__ __forceinline__ void peak(float top, float& M, float& l, G grown)
+{
     if (__any(top > M + GROW)) {
         const float n = fmaxf(M, top), f = exp2_(M - n);
         l *= f;
@@ -121,10 +124,11 @@ struct AttendArgs {
     const _Float16* q;
     _Float16* out;
     long long ld_q, ld_out;
-    int heads_q, group;  // group: query heads to a key head
+    int heads_q;
+    Div group, heads;    // query heads to a key head; key heads
     float scale;         // log2(e) included
     int causal, window;
-    int splits, tiles;  // tiles: of 32 rows to a sequence, few rows
+    Div splits, tiles;  // tiles: of 32 rows to a sequence, few rows
     float* part;   // [split][row * heads_q + head][d] sums, not divided
     float2* stat;  // [split][row * heads_q + head] (m, l)
     bool vec;      // d and the rows of q allow 16-byte accesses
@@ -144,8 +148,10 @@ __device__ __forceinline__ h8 q8(const _Float16* row, int f, int d, bool vec)
 template <int DP>
 __device__ __forceinline__ void load_q(const AttendArgs& a, const KvSeq& s, int head, int r, int hh, h8 (&qf)[DP / 16])
 {
-    if (r < s.n * a.group) {
-        const _Float16* row = a.q + (s.row0 + r / a.group) * a.ld_q + (long long)(head * a.group + r % a.group) * a.kv.d;
+    const int g = (int)a.group.d;
+    if (r < s.n * g) {
+        const int i = a.group.quot(r);
+        const _Float16* row = a.q + (s.row0 + i) * a.ld_q + (long long)(head * g + r - i * g) * a.kv.d;
 #pragma unroll
         for (int t = 0; t < DP / 16; t++) qf[t] = q8(row, 32 * (t >> 1) + 16 * hh + 8 * (t & 1), a.kv.d, a.vec);
     } else {
@@ -193,15 +199,16 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
     // Workgroups go to the eight XCDs in turn: the row tiles of one part of one sequence's positions run on one XCD, one after the
     // other, and find the codes in its L2.
-    const int turn = blockIdx.x / 8, unit = turn / a.tiles * 8 + blockIdx.x % 8, tile = turn % a.tiles;
-    const int split = unit % a.splits, head = unit / a.splits % p.heads, b = unit / a.splits / p.heads;
+    const int turn = blockIdx.x / 8, tile = a.tiles.rem(turn), unit = a.tiles.quot(turn) * 8 + blockIdx.x % 8;
+    const int who = a.splits.quot(unit), split = a.splits.rem(unit), head = a.heads.rem(who), b = a.heads.quot(who), splits = (int)a.splits.d;
+    const int g_ = (int)a.group.d;
     if (b >= p.n_seqs) return;
     KvSeq s;
     const bool ok = kv_seq(p, b, s);
     if (!ok && tid == 0) kv_flag(p, LLMINT8_KV_BAD_BATCH);
-    const int r0 = 32 * tile, rows = s.n * a.group - r0 < 32 ? s.n * a.group - r0 : 32;  // this tile's
+    const int r0 = 32 * tile, rows = s.n * g_ - r0 < 32 ? s.n * g_ - r0 : 32;  // this tile's
     if (rows <= 0) return;
-    const int top_pos = s.len - s.n + (r0 + rows - 1) / a.group, low_pos = s.len - s.n + r0 / a.group;
+    const int top_pos = s.len - s.n + a.group.quot(r0 + rows - 1), low_pos = s.len - s.n + a.group.quot(r0);
 
     // blocks that some row sees, and this workgroup's part of them
     // (lo, all_hi: of the first row; all_lo, hi: of the last.  Blocks before all_lo or behind all_hi need a mask.)
@@ -209,13 +216,13 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     seen(a, s.len, top_pos, all_lo, hi);
     seen(a, s.len, low_pos, lo, all_hi);
     const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
-    const int chunk = chunk_of(end - first, a.splits, 1);
+    const int chunk = chunk_of(end - first, splits, 1);
     const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
     const int closed = s.len / KV_BLOCK;  // blocks held as codes
     const long long total = (long long)p.n_rows * a.heads_q;
     if (split && c0 >= c1) {  // nothing left for this part
         if (tid < rows)
-            a.stat[split * total + (s.row0 + (r0 + tid) / a.group) * (long long)a.heads_q + head * a.group + (r0 + tid) % a.group] = make_float2(LOWEST, 0.0f);
+            a.stat[split * total + (s.row0 + a.group.quot(r0 + tid)) * (long long)a.heads_q + head * g_ + a.group.rem(r0 + tid)] = make_float2(LOWEST, 0.0f);
         return;
     }
     const int k1 = c1 < closed ? c1 : closed;
@@ -223,7 +230,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     h8 qf[DP / 16];
     load_q<DP>(a, s, head, r0 + qr, hh, qf);
     int rlo, rhi;  // what this lane's row sees
-    seen(a, s.len, s.len - s.n + (r0 + qr) / a.group, rlo, rhi);
+    seen(a, s.len, s.len - s.n + a.group.quot(r0 + qr), rlo, rhi);
 
     f16v o[NT];
 #pragma unroll
@@ -234,65 +241,72 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         for (int t = 0; t < NT; t++) o[t] *= f;
     };
 
-    // The wave's blocks: c0 + w, c0 + w + 4, ...  Lane i looks up the i-th of the next 64.
+    // The wave's blocks: c0 + w, c0 + w + 4, ...  Lane i looks up the i-th of the next 64; two blocks are on their way at any time, a
+    // block's registers being requested again as soon as they have been converted.
     const int nb = k1 > c0 + w ? (k1 - c0 - w + 3) / 4 : 0;
-    u4 kc[NT], vc[NT], kn[NT], vn[NT];
-    long long at = -1;
-    unsigned cc = 0;
+    struct Block {
+        u4 k[NT], v[NT];
+        long long at;
+        Factors f;
+    };
+    long long at_ = 0;
+    Factors f_ = {};
     auto look_up = [&](int i0) {
-        const int i = i0 + lane;
-        at = -1, cc = 0;
-        if (i < nb) {
-            at = kv_block(p, b, head, c0 + w + 4 * i);
-            if (at >= 0) cc = p.consts[at];
-            else kv_flag(p, LLMINT8_KV_BAD_PAGE);
-        }
+        const int i = i0 + lane < nb ? i0 + lane : nb - 1;
+        at_ = kv_block(p, b, head, c0 + w + 4 * i);
+        const bool there = at_ >= 0;
+        if (!there) kv_flag(p, LLMINT8_KV_BAD_PAGE);
+        at_ = there ? at_ : 0;  // (weights of 0 for what is not there)
+        f_ = factors(there, p.consts[at_], a.scale);
     };
-    auto at_of = [&](int i) {
-        return (long long)__builtin_amdgcn_readlane((int)(at >> 32), i & 63) << 32 |
-               (unsigned)__builtin_amdgcn_readlane((int)at, i & 63);
+    auto uniform = [](float x, int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i)); };
+    auto name = [&](int i, Block& x) {  // the i-th block: where it is
+        if (i && (i & 63) == 0) look_up(i);
+        x.at = (long long)__builtin_amdgcn_readlane((int)(at_ >> 32), i & 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)at_, i & 63);
+        x.f = {uniform(f_.ks, i & 63), uniform(f_.lcv, i & 63), uniform(f_.inv, i & 63)};
     };
-    auto request = [&](long long n, u4 (&k)[NT], u4 (&v)[NT]) {
-        if (n < 0) return;
-        const u4* src = (const u4*)(p.codes + n * (2 * KV_BLOCK * DP)) + lane;
+    auto request = [&](const Block& x, u4 (&y)[NT], int value) {
+        const u4* src = (const u4*)(p.codes + x.at * (2 * KV_BLOCK * DP)) + lane + 64 * NT * value;
 #pragma unroll
-        for (int t = 0; t < NT; t++) k[t] = __builtin_nontemporal_load(src + 64 * t);
-#pragma unroll
-        for (int t = 0; t < NT; t++) v[t] = __builtin_nontemporal_load(src + 64 * (NT + t));
+        for (int t = 0; t < NT; t++) y[t] = __builtin_nontemporal_load(src + 64 * t);
     };
-    long long next = -1;
-    if (nb > 0) {
-        look_up(0);
-        next = at_of(0);
-        request(next, kn, vn);
-    }
-    for (int i = 0; i < nb; i++) {
-        const bool there = next >= 0;
-        const unsigned c = __builtin_amdgcn_readlane((int)cc, i & 63);
-#pragma unroll
-        for (int t = 0; t < NT; t++) kc[t] = kn[t], vc[t] = vn[t];
-        if (i + 1 < nb) {
-            if (((i + 1) & 63) == 0) look_up(i + 1);
-            next = at_of(i + 1);
-            request(next, kn, vn);
-        }
-        if (!there) continue;
+    auto take = [&](int i, Block& x) {
         f16v sc = {};
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            sc = mfma(codes8(kc[t][0], kc[t][1]), qf[2 * t], sc);
-            sc = mfma(codes8(kc[t][2], kc[t][3]), qf[2 * t + 1], sc);
+            sc = mfma(codes8(x.k[t][0], x.k[t][1]), qf[2 * t], sc);
+            sc = mfma(codes8(x.k[t][2], x.k[t][3]), qf[2 * t + 1], sc);
         }
-        const Factors fa = factors(true, c, a.scale);
+        const Factors fa = x.f;
+        const bool more = i + 2 < nb;
+        if (more) {
+            name(i + 2, x);
+            request(x, x.k, 0);
+        }
         const int pos0 = (c0 + w + 4 * i) * KV_BLOCK;
         h8 pf[2];
         if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
-        peak(largest(sc), fa, m, l, rescale);
+        peak(top_of(sc, fa), m, l, rescale);
         expo(sc, fa, m, l, pf);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            o[t] = mfma(codes8(vc[t][0], vc[t][1]), pf[0], o[t]);
-            o[t] = mfma(codes8(vc[t][2], vc[t][3]), pf[1], o[t]);
+            o[t] = mfma(codes8(x.v[t][0], x.v[t][1]), pf[0], o[t]);
+            o[t] = mfma(codes8(x.v[t][2], x.v[t][3]), pf[1], o[t]);
+        }
+        if (more) request(x, x.v, 1);
+    };
+    if (nb > 0) {
+        Block x, y;
+        look_up(0);
+        name(0, x);
+        request(x, x.k, 0), request(x, x.v, 1);
+        if (nb > 1) {
+            name(1, y);
+            request(y, y.k, 0), request(y, y.v, 1);
+        }
+        for (int i = 0; i < nb; i += 2) {
+            take(i, x);
+            if (i + 1 < nb) take(i + 1, y);
         }
     }
     // The open block, fp16: by the wave whose turn it is.  Its values are scaled by a power of two to what codes are, at most 128.
@@ -325,7 +339,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         const Factors fa = factors(true, 1.0f, 127.0f * unit, a.scale);
         h8 pf[2];
         hide(sc, base, hh, rlo, rhi);
-        peak(largest(sc), fa, m, l, rescale);
+        peak(top_of(sc, fa), m, l, rescale);
         expo(sc, fa, m, l, pf);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
@@ -372,10 +386,10 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
                 for (int e = 0; e < 4; e++) sum[e] += y[e];
                 den += s_l[q][r] * exp2_(s_m[q][r] - top);
             }
-            const long long row = s.row0 + (r0 + r) / a.group;
-            const int g = head * a.group + (r0 + r) % a.group;
+            const long long row = s.row0 + a.group.quot(r0 + r);
+            const int g = head * g_ + a.group.rem(r0 + r);
             const float inv = den != 0.0f ? 1.0f / den : 0.0f;
-            if (a.splits > 1) {
+            if (splits > 1) {
                 const long long at_row = split * total + row * a.heads_q + g;
                 if (at == 0) a.stat[at_row] = make_float2(top, den);
                 float* dst = a.part + at_row * p.d + at;
@@ -404,204 +418,52 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 // Many rows: a workgroup takes a tile of 32 rows a wave (tokens, and for each the query heads that share its keys), its waves the
 // same blocks of the cache two at a time (a stage) from LDS, where the codes lie as fp16 in operand order: they are converted once
 // for all rows.  Bound by the matrix units and by what makes scores weights, which are kept busy at the same time: the scores of the
-// next stage are computed while the weights of this one are.  So LDS holds keys one stage ahead of values.
+// next block are computed while the weights of this one are.  So LDS holds keys one block ahead of values.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DP, int WAVES, int GROUPS>
-__global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
+template <int DP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
 {
-    constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;  // of a group
+    constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int PIECES = DP * 4, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' keys, or values; to a thread
-    extern __shared__ __align__(16) _Float16 all_lds[];                     // [group][keys, values][4 blocks][DP * 32]
+    extern __shared__ __align__(16) _Float16 lds[];                         // [keys, values][4 blocks][DP * 32]
     __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = GROUPS > 1 ? wave / WAVES : 0;
-    const int tid = threadIdx.x % THREADS, lane = tid & 63, w = wave % WAVES, qr = lane & 31, hh = lane >> 5;
-    _Float16* const lds = all_lds + group * (8 * DP * 32);
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
     // the heads of a tile one after the other: with a multiple of 8 heads, a head's tiles all run on one XCD and share its L2
-    const int head = blockIdx.x % p.heads;
-    const int split = blockIdx.y;
+    const int head = a.heads.rem(blockIdx.x), split = blockIdx.y, splits = (int)a.splits.d, G = (int)a.group.d;
     bool wrong = false;
-    auto tiles = [&](int q) {
-        KvSeq s;
-        if (!kv_seq(p, q, s)) wrong = true;
-        return (s.n * a.group + ROWS - 1) / ROWS;
-    };
     int b, tile;
-    const bool found = kv_find(p.n_seqs, blockIdx.x / p.heads, tiles, b, tile);
+    KvSeq s;
+    const bool found = kv_find(p, a.heads.quot(blockIdx.x), [&](const KvSeq& t) { return (t.n * G + ROWS - 1) / ROWS; }, b, s, tile, wrong);
     if (wrong) kv_flag(p, LLMINT8_KV_BAD_BATCH);
     if (!found) return;
-    KvSeq s;
-    kv_seq(p, b, s);
-    const int rows = s.n * a.group, old = s.len - s.n;
+    const int rows = s.n * G, old = s.len - s.n;
     tile = (rows + ROWS - 1) / ROWS - 1 - tile;  // those that see most first
     const int r0 = tile * ROWS, r1 = r0 + ROWS < rows ? r0 + ROWS : rows;
     const int w0 = r0 + w * 32, w1 = w0 + 32 < r1 ? w0 + 32 : r1;  // this wave's rows
 
     int lo, hi, x0, x1;
-    seen(a, s.len, old + r0 / a.group, lo, x1);
-    seen(a, s.len, old + (r1 - 1) / a.group, x0, hi);
+    seen(a, s.len, old + a.group.quot(r0), lo, x1);
+    seen(a, s.len, old + a.group.quot(r1 - 1), x0, hi);
     const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
-    const int chunk = chunk_of(end - first, a.splits, 2 * GROUPS);
-    const int b0 = first + split * chunk, b1 = b0 + chunk < end ? b0 + chunk : end;
-    const int part = GROUPS > 1 ? chunk_of(b1 - b0, GROUPS, 2) : chunk;  // a group's
-    const int c0 = b0 + group * part, c1 = c0 + part < b1 ? c0 + part : b1;
+    const int chunk = chunk_of(end - first, splits, 2);
+    const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
     const int closed = s.len / KV_BLOCK, k1 = c1 < closed ? c1 : closed;
     const int stages = k1 > c0 ? (k1 - c0 + 1) / 2 : 0;
-    // the most that a group has (the first one's): all take part in as many barriers
-    int most = stages;
-    if (GROUPS > 1) {
-        int e = b0 + part < b1 ? b0 + part : b1;
-        e = e < closed ? e : closed;
-        most = e > b0 ? (e - b0 + 1) / 2 : 0;
-    }
     const long long total = (long long)p.n_rows * a.heads_q;
-    if (split && b0 >= b1) {  // nothing left for this part
-        for (int r = r0 + (int)threadIdx.x; r < r1; r += THREADS * GROUPS)
-            a.stat[split * total + (s.row0 + r / a.group) * (long long)a.heads_q + head * a.group + r % a.group] = make_float2(LOWEST, 0.0f);
+    if (split && c0 >= c1) {  // nothing left for this part
+        for (int r = r0 + tid; r < r1; r += THREADS)
+            a.stat[split * total + (s.row0 + a.group.quot(r)) * (long long)a.heads_q + head * G + a.group.rem(r)] = make_float2(LOWEST, 0.0f);
         return;
     }
     // what all of the wave's rows see, and the stages in which some see anything
     int some_lo = 0, some_hi = 0, all_lo = 0, all_hi = 0;
     if (w0 < w1) {
-        seen(a, s.len, old + w0 / a.group, some_lo, all_hi);
-        seen(a, s.len, old + (w1 - 1) / a.group, all_lo, some_hi);
+        seen(a, s.len, old + a.group.quot(w0), some_lo, all_hi);
+        seen(a, s.len, old + a.group.quot(w1 - 1), all_lo, some_hi);
     }
     auto clip = [&](int x) { return x < 0 ? 0 : x > stages ? stages : x; };
     const int sa = clip((some_lo / KV_BLOCK - c0) >> 1), sb = clip(((some_hi + KV_BLOCK - 1) / KV_BLOCK - c0 + 1) >> 1);
-
-    h8 qf[DP / 16];
-    load_q<DP>(a, s, head, w0 + qr, hh, qf);
-    int rlo, rhi;
-    seen(a, s.len, old + (w0 + qr) / a.group, rlo, rhi);
-    if (rhi > k1 * KV_BLOCK) rhi = k1 * KV_BLOCK;  // behind that there is nothing of this workgroup's but the open block
-    if (all_hi > k1 * KV_BLOCK) all_hi = k1 * KV_BLOCK;
-    f16v o[NT];
-    float m = LOWEST, l = 0.0f;
-#pragma unroll
-    for (int x = 0; x < NT; x++) o[x] = f16v{};
-
-    // where a block's keys and values lie in LDS
-    auto keys = [&](int j) { return (h8*)(lds + (j & 3) * (DP * 32)) + lane; };
-    auto values = [&](int j) { return (h8*)(lds + (4 + (j & 3)) * (DP * 32)) + lane; };
-    auto scores = [&](int j, f16v& sc) {
-        const h8* const kb = keys(j);
-        sc = f16v{};
-#pragma unroll
-        for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
-    };
-    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums, and between these
-    // products the weights' own sum and the next scores' maximum (returned; of scores of which some may have to be hidden).  other(x),
-    // x = 0 .. 3: a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS four slices
-    // ahead (its latency) and no further, or registers run out.
-    constexpr int S = DP / 16, AHEAD = S < 4 ? S : 4;
-    auto first_keys = [&](int j, h8 (&k)[AHEAD]) {
-        const h8* const kb = keys(j);
-#pragma unroll
-        for (int g = 0; g < AHEAD; g++) k[g] = kb[g * 64];
-    };
-    auto step = [&](int j, f16v& sc, const Factors& fa, f16v& next, h8 (&k)[AHEAD], auto other) {
-        const h8 *const kb = keys(j + 1), *const vb = values(j);
-        const float off = fa.lcv - m;
-        float sum = 0.0f, mx = 0.0f;
-        h8 pf[2], v[NT];
-        next = f16v{};
-#pragma unroll
-        for (int g = 0; g < S; g++) {
-            const h8 t = k[g % AHEAD];
-            if (g + AHEAD < S) k[g % AHEAD] = kb[(g + AHEAD) * 64];
-#pragma unroll
-            for (int q = 0; q < NT; q++)  // the values' first operands over the last slices
-                if (g == S - AHEAD + q * AHEAD / NT) v[q] = vb[2 * q * 64];
-            next = mfma(t, qf[g], next);
-#pragma unroll
-            for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
-                sc[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), sc[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
-                pf[i >> 3][i & 7] = (_Float16)sc[i], pf[i >> 3][(i & 7) + 1] = (_Float16)sc[i + 1];
-            }
-#pragma unroll
-            for (int x = 0; x < 4; x++)
-                if (g == x * S / 4) other(x);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int u = 0; u < 2 * NT; u++) {
-            const int y = u / NT, q = u % NT;
-            const h8 t = v[q];
-            if (y == 0) v[q] = vb[(2 * q + 1) * 64];
-            o[q] = mfma(t, pf[y], o[q]);
-#pragma unroll
-            for (int i = 16 * u / (2 * NT); i < 16 * (u + 1) / (2 * NT); i++) {
-                sum += sc[i];
-                if (i == 8) mx = max3(next[0], next[1], next[2]);  // (the scores' last product is done by now)
-                if (i > 8) mx = max3(mx, next[2 * i - 15], next[2 * i - 14]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        l = __builtin_fmaf(sum, fa.inv, l);
-        return max3(mx, next[15], next[15]);
-    };
-    auto look = [&](int pos0, f16v& sc, float mx, const Factors& fa) {
-        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) {
-            hide(sc, pos0, hh, rlo, rhi);
-            mx = largest(sc);
-        }
-        peak(mx, fa, m, l, [&](float x) {
-#pragma unroll
-            for (int q = 0; q < NT; q++) o[q] *= x;
-        });
-    };
-
-    // ---- the open block, fp16 from the ring, before the others: the last group's
-    const bool mine = GROUPS == 1 || group == GROUPS - 1;
-    if (closed >= b0 && closed < b1) {
-        const int d = p.d, pos0 = closed * KV_BLOCK;
-        const unsigned short *const krows = kv_ring_row(p, s.slot, head, 0, pos0), *const vrows = kv_ring_row(p, s.slot, head, 1, pos0);
-        int big = 0;
-        for (int t = tid; mine && t < (s.len - pos0) * d; t += THREADS) {
-            const int y = vrows[t] & 0x7fff;
-            big = y > big ? y : big;
-        }
-#pragma unroll
-        for (int x = 32; x; x >>= 1) {
-            const int y = __shfl_xor(big, x);
-            big = y > big ? y : big;
-        }
-        if (mine && lane == 0) s_big[w] = big;
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
-        const float scale = open_unit(big);
-        for (int t = tid; mine && t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
-            const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
-            h8 y = {}, z = {};
-            if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
-                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / scale));
-            }
-            *((h8*)lds + t) = y;
-            *((h8*)(lds + 4 * DP * 32) + t) = z;
-        }
-        __syncthreads();
-        if (mine && pos0 < some_hi) {
-            f16v sc;
-            scores(0, sc);
-            const Factors fa = factors(true, 1.0f, 127.0f * scale, a.scale);
-            int olo, ohi;
-            seen(a, s.len, old + (w0 + qr) / a.group, olo, ohi);
-            hide(sc, pos0, hh, olo, ohi < s.len ? ohi : s.len);
-            peak(largest(sc), fa, m, l, [](float) {});
-            h8 pf[2];
-            expo(sc, fa, m, l, pf);
-            const h8* const vb = values(0);
-#pragma unroll
-            for (int y = 0; y < 2; y++)
-#pragma unroll
-                for (int q = 0; q < NT; q++) o[q] = mfma(vb[(2 * q + y) * 64], pf[y], o[q]);
-        }
-        __syncthreads();
-    }
 
     // ---- Lane i of every wave looks up the i-th of 64 blocks, so that a stage waits neither for the page table nor for constants.
     // `ahead` are 64 blocks from PERIOD behind the first of those in use on.
@@ -612,17 +474,12 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
     };
     auto look_up = [&](int j) {
         Looked r;
-        long long at = -1;
-        unsigned c = 0;
-        if (c0 + j + lane < k1) {
-            at = kv_block(p, b, head, c0 + j + lane);
-            if (at >= 0)
-                c = p.consts[at];
-            else
-                kv_flag(p, LLMINT8_KV_BAD_PAGE);
-        }
-        r.f = factors(at >= 0, c, a.scale);
+        const int k = c0 + j + lane;
+        long long at = kv_block(p, b, head, k < k1 ? k : k1 - 1);
+        if (at < 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
+        const bool there = at >= 0 && k < k1;
         at = at < 0 ? 0 : at;  // (weights of 0 for what is not there)
+        r.f = factors(there, p.consts[at], a.scale);
         r.at[0] = (int)at, r.at[1] = (int)(at >> 32);
         return r;
     };
@@ -630,6 +487,9 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
     int j0 = 0;  // the first block of `use`
     auto float_at = [&](float x, int j) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), j - j0)); };
     auto factors_of = [&](int j) { return Factors{float_at(use.f.ks, j), float_at(use.f.lcv, j), float_at(use.f.inv, j)}; };
+    // where a block's keys and values lie in LDS
+    auto keys = [&](int j) { return (h8*)(lds + (j & 3) * (DP * 32)) + lane; };
+    auto values = [&](int j) { return (h8*)(lds + (4 + (j & 3)) * (DP * 32)) + lane; };
     // this thread's 16-byte pieces of the keys (value 0) or values of blocks j and j + 1
     auto request = [&](int j, int value, u4 (&piece)[PER]) {
 #pragma unroll
@@ -651,23 +511,166 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
     };
     auto deposit = [&](int j, int value, const u4 (&piece)[PER]) { deposit_half(j, value, piece, 0), deposit_half(j, value, piece, 1); };
 
+    // what the first stages need is requested before the rows of queries are
+    u4 pk[PER], pv[PER], k0[PER], k1_[PER], v0[PER];
+    if (stages) {
+        use = look_up(0);
+        request(0, 0, k0), request(1, 0, k1_), request(0, 1, v0), request(3, 0, pk), request(2, 1, pv);
+    }
+    h8 qf[DP / 16];
+    load_q<DP>(a, s, head, w0 + qr, hh, qf);
+    int rlo, rhi;
+    seen(a, s.len, old + a.group.quot(w0 + qr), rlo, rhi);
+    const int full_hi = rhi < s.len ? rhi : s.len;
+    if (rhi > k1 * KV_BLOCK) rhi = k1 * KV_BLOCK;  // behind that there is nothing of this workgroup's but the open block
+    if (all_hi > k1 * KV_BLOCK) all_hi = k1 * KV_BLOCK;
+    f16v o[NT];
+    float m = LOWEST, l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < NT; x++) o[x] = f16v{};
+    auto rescale = [&](float x) {
+#pragma unroll
+        for (int q = 0; q < NT; q++) o[q] *= x;
+    };
+    auto scores = [&](int j, f16v& sc) {
+        const h8* const kb = keys(j);
+        sc = f16v{};
+#pragma unroll
+        for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
+    };
+
+    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums, and between those
+    // products the next scores' maximum, which is returned (for both halves of a row; without what may have to be hidden).  other(x),
+    // x = 0 .. 3: a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS some slices
+    // ahead (its latency) and no further, or registers run out.  k: the next block's first keys; on return, if NEXT, those of
+    // the one behind.
+    constexpr int S = DP / 16, AHEAD = S < 4 ? S : 4, U = 2 * NT;
+    auto first_keys = [&](int j, h8 (&k)[AHEAD]) {
+        const h8* const kb = keys(j);
+#pragma unroll
+        for (int g = 0; g < AHEAD; g++) k[g] = kb[g * 64];
+    };
+    auto step = [&](auto with_next, int j, f16v& sc, const Factors& fa, f16v& next, const Factors& fb, h8 (&k)[AHEAD], auto other) {
+        constexpr bool NEXT = decltype(with_next)::value;
+        const h8 *const kb = keys(j + 1), *const kc = keys(j + 2), *const vb = values(j);
+        const float off = fa.lcv - m;
+        float sum = 0.0f, mx = 0.0f;
+        h8 pf[2], v[NT];
+        next = f16v{};
+#pragma unroll
+        for (int g = 0; g < S; g++) {
+            const h8 t = k[g % AHEAD];
+            if (g + AHEAD < S) k[g % AHEAD] = kb[(g + AHEAD) * 64];
+#pragma unroll
+            for (int q = 0; q < NT; q++)  // the values' first operands over the last slices
+                if (g == S - AHEAD + q * AHEAD / NT) v[q] = vb[2 * q * 64];
+            next = mfma(t, qf[g], next);
+#pragma unroll
+            for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
+                sc[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), sc[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
+                pf[i >> 3][i & 7] = (_Float16)sc[i], pf[i >> 3][(i & 7) + 1] = (_Float16)sc[i + 1];
+            }
+            if (g)
+#pragma unroll
+                for (int i = 8 * (g - 1) / S * 2; i < 8 * g / S * 2; i++) sum += sc[i];
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                if (g == x * S / 4) other(x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int y = u / NT, q = u % NT;
+            const h8 t = v[q];
+            if (y == 0) v[q] = vb[(2 * q + 1) * 64];
+            if (NEXT && y == 1)
+#pragma unroll
+                for (int g = 0; g < AHEAD; g++)
+                    if (g * NT / AHEAD == q) k[g] = kc[g * 64];
+            o[q] = mfma(t, pf[y], o[q]);
+            if (u == 0)
+#pragma unroll
+                for (int i = 8 * (S - 1) / S * 2; i < 16; i++) sum += sc[i];
+            if (u)
+#pragma unroll
+                for (int i = 8 * (u - 1) / (U - 1); i < 8 * u / (U - 1); i++)
+                    mx = i ? max3(mx, next[2 * i], next[2 * i + 1]) : fmaxf(next[0], next[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l = __builtin_fmaf(sum, fa.inv, l);
+        return halves_max(fmaxf(__builtin_fmaf(mx, fb.ks, fb.lcv), LOWEST));
+    };
+    auto look = [&](int j, f16v& sc, float top, const Factors& fa) {
+        const int pos0 = (c0 + j) * KV_BLOCK;
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) {
+            hide(sc, pos0, hh, rlo, rhi);
+            top = top_of(sc, fa);
+        }
+        peak(top, m, l, rescale);
+    };
+
+    // ---- the open block, fp16 from the ring, before the others
+    if (closed >= c0 && closed < c1) {
+        const int d = p.d, pos0 = closed * KV_BLOCK;
+        const unsigned short *const krows = kv_ring_row(p, s.slot, head, 0, pos0), *const vrows = kv_ring_row(p, s.slot, head, 1, pos0);
+        int big = 0;
+        for (int t = tid; t < (s.len - pos0) * d; t += THREADS) {
+            const int y = vrows[t] & 0x7fff;
+            big = y > big ? y : big;
+        }
+#pragma unroll
+        for (int x = 32; x; x >>= 1) {
+            const int y = __shfl_xor(big, x);
+            big = y > big ? y : big;
+        }
+        if (lane == 0) s_big[w] = big;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
+        const float unit = open_unit(big);
+        for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
+            const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
+            h8 y = {}, z = {};
+            if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
+                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / unit));
+            }
+            *((h8*)lds + t) = y;
+            *((h8*)(lds + 4 * DP * 32) + t) = z;
+        }
+        __syncthreads();
+        if (pos0 < some_hi) {
+            f16v sc;
+            scores(0, sc);
+            const Factors fa = factors(true, 1.0f, 127.0f * unit, a.scale);
+            hide(sc, pos0, hh, rlo, full_hi);
+            peak(top_of(sc, fa), m, l, rescale);
+            h8 pf[2];
+            expo(sc, fa, m, l, pf);
+            const h8* const vb = values(0);
+#pragma unroll
+            for (int y = 0; y < 2; y++)
+#pragma unroll
+                for (int q = 0; q < NT; q++) o[q] = mfma(vb[(2 * q + y) * 64], pf[y], o[q]);
+        }
+        __syncthreads();
+    }
+
     // ---- Stage st: blocks 2 st and 2 st + 1 (from c0 on): their weights and sums, and each time the scores of the block behind.  So keys
     // go to LDS one block earlier than values: meanwhile those of 2 st + 3 and 2 st + 4, and the values of 2 st + 2 and 2 st + 3.
-    if (most > 0) {
-        u4 pk[PER], pv[PER];
-        use = look_up(0), ahead = look_up(PERIOD);
-        {
-            u4 k0[PER], k1[PER], v0[PER];
-            request(0, 0, k0), request(1, 0, k1), request(0, 1, v0), request(3, 0, pk), request(2, 1, pv);
-            deposit(0, 0, k0);
-            __syncthreads();  // (block 1's keys come twice)
-            deposit(1, 0, k1), deposit(0, 1, v0);
-        }
+    if (stages) {
+        ahead = use;  // (its addresses may be read from once more after the last block)
+        if (k1 - c0 > PERIOD) ahead = look_up(PERIOD);
+        deposit(0, 0, k0);
+        __syncthreads();  // (block 1's keys come twice)
+        deposit(1, 0, k1_), deposit(0, 1, v0);
         __syncthreads();
         auto more = [&](int st) {  // the end of a stage
             if (2 * st + 2 == j0 + PERIOD) {
                 use = ahead, j0 += PERIOD;
-                ahead = look_up(j0 + PERIOD);
+                if (k1 - c0 > j0 + PERIOD) ahead = look_up(j0 + PERIOD);
             }
             request(2 * st + 5, 0, pk), request(2 * st + 4, 1, pv);
             __syncthreads();
@@ -678,7 +681,7 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
         auto enter = [&]() {
             scores(2 * sa, s0);
             f0 = factors_of(2 * sa);
-            look((c0 + 2 * sa) * KV_BLOCK, s0, largest(s0), f0);
+            look(2 * sa, s0, top_of(s0, f0), f0);
         };
         if (sa == 0) enter();
         __syncthreads();
@@ -689,63 +692,33 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
             more(st);
         }
         for (; st < sb; st++) {
-            const int pos0 = (c0 + 2 * st) * KV_BLOCK;
             h8 k[AHEAD];
             first_keys(2 * st + 1, k);
-            float mx = step(2 * st, s0, f0, s1, k, [](int) {});
-            first_keys(2 * st + 2, k);
             const Factors f1 = factors_of(2 * st + 1);
-            look(pos0 + KV_BLOCK, s1, mx, f1);
-            mx = step(2 * st + 1, s1, f1, s0, k, [&](int x) {
+            float top = step(std::true_type(), 2 * st, s0, f0, s1, f1, k, [](int) {});
+            f0 = factors_of(2 * st + 2);
+            look(2 * st + 1, s1, top, f1);
+            top = step(std::false_type(), 2 * st + 1, s1, f1, s0, f0, k, [&](int x) {
                 deposit_half(2 * st + (x < 2 ? 3 : 2), x >> 1, x < 2 ? pk : pv, x & 1);
             });
-            f0 = factors_of(2 * st + 2);
-            // Four of the eight waves (two to a SIMD) do this behind the barrier: the two are then not at the same place.
-            if (wave < 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
+            look(2 * st + 2, s0, top, f0);
             more(st);
-            if (wave >= 4) look(pos0 + 2 * KV_BLOCK, s0, mx, f0);
         }
         for (; st < stages; st++) {
             deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
             more(st);
         }
-        if (GROUPS > 1)
-            for (; st < most; st++) __syncthreads();
     }
 
-    float den = l + __shfl_xor(l, 32);
-    if (GROUPS > 1) {  // the second group's sums to the first, through LDS, 32 features at a time a wave
-        float* const mine_m = (float*)all_lds + w * 64 + lane;
-        f4* const mine_o = (f4*)((float*)all_lds + 2 * THREADS) + w * 64 + lane;
-        __syncthreads();
-        if (group) mine_m[0] = m, mine_m[THREADS] = den;
-        if (group)
-#pragma unroll
-            for (int q = 0; q < NT; q++)
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    mine_o[(4 * q + j) * THREADS] = f4{o[q][4 * j], o[q][4 * j + 1], o[q][4 * j + 2], o[q][4 * j + 3]};
-        __syncthreads();
-        if (group) return;
-        const float m2 = mine_m[0], n = fmaxf(m, m2), f = exp2_(m - n), f2 = exp2_(m2 - n);
-        den = den * f + mine_m[THREADS] * f2;
-        m = n;
-#pragma unroll
-        for (int q = 0; q < NT; q++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const f4 y = mine_o[(4 * q + j) * THREADS];
-#pragma unroll
-                for (int e = 0; e < 4; e++) o[q][4 * j + e] = o[q][4 * j + e] * f + y[e] * f2;
-            }
-    }
+    const float den = l + __shfl_xor(l, 32);
     const int r = w0 + qr;
     if (r >= r1) return;
-    const long long row = s.row0 + r / a.group;
-    const int g = head * a.group + r % a.group;
-    if (a.splits > 1) {
-        if (hh == 0) a.stat[split * total + row * a.heads_q + g] = make_float2(m, den);
-        float* dst = a.part + (split * total + row * a.heads_q + g) * p.d;
+    const long long row = s.row0 + a.group.quot(r);
+    const int g = head * G + a.group.rem(r);
+    if (splits > 1) {
+        const long long at = split * total + row * a.heads_q + g;
+        if (hh == 0) a.stat[at] = make_float2(m, den);
+        float* dst = a.part + at * p.d;
 #pragma unroll
         for (int q = 0; q < NT; q++)
 #pragma unroll
@@ -788,13 +761,14 @@ __global__ void __launch_bounds__(64 * WAVES * GROUPS, WAVES * GROUPS == 4 && DP
 // were not written.
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 {
+    const int splits = (int)a.splits.d;
     constexpr int NQ = KV_MAX_D / 64;
     __shared__ f4 s_sum[4][NQ][16];
     __shared__ float s_den[4];
     const int tid = threadIdx.x, lane = tid & 63, d = a.kv.d, w = tid >> 6;
     const long long total = (long long)a.kv.n_rows * a.heads_q, x = blockIdx.x;
     float top = LOWEST;
-    for (int s = lane; s < a.splits; s += 64) {
+    for (int s = lane; s < splits; s += 64) {
         const float2 t = a.stat[s * total + x];
         if (t.y != 0.0f) top = fmaxf(top, t.x);
     }
@@ -803,13 +777,13 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
     const int part = lane >> 4, f0 = 4 * (lane & 15);
     f4 sum[NQ] = {};
     float den = 0.0f;
-    for (int s0 = 4 * w + part; s0 < a.splits; s0 += 64) {
+    for (int s0 = 4 * w + part; s0 < splits; s0 += 64) {
         f4 v[4][NQ];
         float f[4];
 #pragma unroll
         for (int u = 0; u < 4; u++) {
             const int s = s0 + 16 * u;
-            const bool there = s < a.splits;
+            const bool there = s < splits;
             const float2 t = there ? a.stat[s * total + x] : make_float2(0.0f, 0.0f);
             const float* src = a.part + (s * total + x) * d + f0;
             f[u] = t.y != 0.0f ? exp2_(t.x - top) : 0.0f;
@@ -865,6 +839,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 constexpr int FEW = 8;
 __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
 {
+    const int splits = (int)a.splits.d;
     const int d = a.kv.d, quads = (d + 3) / 4;
     const long long total = (long long)a.kv.n_rows * a.heads_q, t = (long long)blockIdx.x * 256 + threadIdx.x, x = t / quads;
     if (x >= total) return;
@@ -873,9 +848,9 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
     f4 v[FEW];
 #pragma unroll
     for (int s = 0; s < FEW; s++) {
-        st[s] = s < a.splits ? a.stat[s * total + x] : make_float2(LOWEST, 0.0f);
+        st[s] = s < splits ? a.stat[s * total + x] : make_float2(LOWEST, 0.0f);
         v[s] = f4{};
-        if (s < a.splits) {
+        if (s < splits) {
             const float* src = a.part + (s * total + x) * d + f0;
             if (d % 4 == 0) {
                 v[s] = *(const f4*)src;
@@ -913,20 +888,20 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
 template <int DP>
 hipError_t launch_step(const AttendArgs& a, hipStream_t st)
 {
-    const long long units = (long long)a.kv.heads * a.kv.n_seqs * a.splits;
-    kv_step_kernel<DP><<<(unsigned)((units + 7) / 8 * 8 * a.tiles), 256, 0, st>>>(a);
+    const long long units = (long long)a.kv.heads * a.kv.n_seqs * a.splits.d;
+    kv_step_kernel<DP><<<(unsigned)((units + 7) / 8 * 8 * a.tiles.d), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-template <int DP, int WAVES, int GROUPS>
+template <int DP, int WAVES>
 hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 {
-    constexpr int bytes = GROUPS * 8 * DP * 32 * 2;
+    constexpr int bytes = 8 * DP * 32 * 2;
     if (bytes + 256 > 65536) {  // with the static part
-        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES, GROUPS>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    kv_prompt_kernel<DP, WAVES, GROUPS><<<dim3(tiles * a.kv.heads, a.splits), 64 * WAVES * GROUPS, bytes, st>>>(a);
+    kv_prompt_kernel<DP, WAVES><<<dim3(tiles * a.kv.heads, a.splits.d), 64 * WAVES, bytes, st>>>(a);
     return hipGetLastError();
 }
 
@@ -946,13 +921,13 @@ KvPlan kv_plan(const Kv& p, int heads_q)
     };
     long long units;
     if (rows <= KV_STEP_ROWS) {
-        r.tile = KV_STEP_ROWS, r.groups = 1, r.tiles = 1;
+        r.tile = KV_STEP_ROWS, r.tiles = 1;
         units = (long long)p.n_seqs * p.heads;
     } else {
-        r.tile = rows > 128 && !wide ? 256 : 128, r.groups = 1;
+        r.tile = rows > 128 && !wide ? 256 : 128;
         units = (r.tiles = (int)tiles(r.tile)) * p.heads;
     }
-    const long long want = (r.tile == KV_STEP_ROWS || r.tile * r.groups == 128 ? 512 : 256) / units, most = (blocks + 7) / 8;
+    const long long want = (r.tile == 256 ? 256 : 512) / units, most = (blocks + 7) / 8;
     r.splits = (int)(want < most ? want : most);
     if (r.splits < 1) r.splits = 1;
     return r;
@@ -967,7 +942,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
 {
     AttendArgs a;
     a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
-    a.group = c.heads_q / p.heads, a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = plan.splits, a.tiles = plan.tiles;
+    a.group = Div(c.heads_q / p.heads), a.heads = Div(p.heads), a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = Div(plan.splits), a.tiles = Div(plan.tiles < 1 ? 1 : plan.tiles);
     const size_t total = (size_t)p.n_rows * c.heads_q;
     a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));
     a.vec = p.d % 8 == 0 && ((((uintptr_t)c.q | (uintptr_t)c.out) & 15) | (c.ld_q & 7) | (c.ld_out & 7)) == 0;
@@ -975,11 +950,9 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     hipError_t e;
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
-        constexpr int NARROW = DP > 128 ? 128 : DP;  // what kv_plan gives the two others
         return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st)
-               : plan.tile == 256        ? launch_prompt<NARROW, 8, 1>(a, plan.tiles, st)
-               : plan.groups == 2        ? launch_prompt<NARROW, 4, 2>(a, plan.tiles, st)
-                                         : launch_prompt<DP, 4, 1>(a, plan.tiles, st);
+               : plan.tile == 256        ? launch_prompt<(DP > 128 ? 128 : DP), 8>(a, plan.tiles, st)  // (never that for more)
+                                         : launch_prompt<DP, 4>(a, plan.tiles, st);
     };
     switch (dp) {
         case 32: e = pick(std::integral_constant<int, 32>()); break;

@@ -30,6 +30,20 @@ constexpr int KV_MAX_D = LLMINT8_KV_MAX_D;
 constexpr int KV_MAX_LEN = 1 << 30;
 __host__ __device__ inline int kv_dpad(int d) { return (d + 31) & ~31; }
 
+// Division by a number that the host knows: m = (2^32 - 1) / d is not above 2^32 / d and less than 1 + 1 / d below it, so the product's high
+// half is the quotient of n < 2^31 or one less.
+struct Div {
+    unsigned d, m;
+    __host__ Div() = default;
+    __host__ explicit Div(int x) : d((unsigned)x), m(0xffffffffu / (unsigned)x) {}
+    __device__ __forceinline__ int quot(int n) const
+    {
+        const unsigned q = __umulhi((unsigned)n, m);
+        return (int)(q + ((unsigned)n - q * d >= d));
+    }
+    __device__ __forceinline__ int rem(int n) const { return n - quot(n) * (int)d; }
+};
+
 // Cache and batch as the kernels take them.
 struct Kv {
     int8_t* codes;           // [page][head][block][2][32 dpad]
@@ -40,7 +54,8 @@ struct Kv {
     const int* pages;        // [n_seqs][page_stride]
     const int* slots;        // [n_seqs], or NULL: the sequence's number
     int* status;             // or NULL
-    int n_pages, bpp /* blocks to a page */, n_slots, heads, d;
+    int n_pages, n_slots, heads, d;
+    Div bpp;  // blocks to a page
     int n_seqs, n_rows, page_stride, max_rows, max_len;
 };
 
@@ -64,33 +79,40 @@ __device__ __forceinline__ bool kv_seq(const Kv& p, int b, KvSeq& s)
     s.slot = p.slots ? p.slots[b] : b;
     s.n = row1 - s.row0;
     const bool rows = s.row0 >= 0 && row1 >= s.row0 && row1 <= p.n_rows && s.n <= p.max_rows;
-    const bool ok = rows && s.len >= 0 && s.len <= p.max_len && (long long)s.len <= (long long)p.page_stride * p.bpp * KV_BLOCK &&
+    const bool ok = rows && s.len >= 0 && s.len <= p.max_len && (long long)s.len <= (long long)p.page_stride * p.bpp.d * KV_BLOCK &&
                     (unsigned)s.slot < (unsigned)p.n_slots;
     if (!rows) s.row0 = 0, s.n = 0;
     if (!ok) s.len = 0, s.slot = 0;
     return ok;
 }
 
-// Unit x of those that the sequences have one after the other, count(b) each: its sequence and its number there.  The whole
-// wave takes part; 64 sequences at a time.  false: there is no such unit.
+// Unit x of those that the sequences have one after the other, count(s) each: its sequence and its number there.  The whole wave takes
+// part, 64 sequences at a time.  false: there is no such unit.  wrong: a sequence looked at cannot be.
 template <class F>
-__device__ __forceinline__ bool kv_find(int n_seqs, int x, F count, int& b, int& i)
+__device__ __forceinline__ bool kv_find(const Kv& p, int x, F count, int& b, KvSeq& s, int& i, bool& wrong)
 {
     const int lane = threadIdx.x & 63;
     int base = 0;
-    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
-        const int c = b0 + lane < n_seqs ? count(b0 + lane) : 0;
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
+        KvSeq t = {};
+        int c = 0;
+        if (b0 + lane < p.n_seqs) {
+            if (!kv_seq(p, b0 + lane, t)) wrong = true;
+            c = count(t);
+        }
         int incl = c;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int t = __shfl_up(incl, d);
-            if (lane >= d) incl += t;
+            const int y = __shfl_up(incl, d);
+            if (lane >= d) incl += y;
         }
         const unsigned long long past = __ballot(base + incl > x);
-        if (past) {
+        if (past) {  // (the same for all lanes, and the compiler is to know it: what hangs on it stays scalar)
             const int l = __builtin_amdgcn_readfirstlane(__ffsll(past) - 1);
-            b = b0 + l;  // (the same for all lanes, and the compiler is to know it: what hangs on it stays scalar)
+            b = b0 + l;
             i = __builtin_amdgcn_readfirstlane(x - base - __builtin_amdgcn_readlane(incl - c, l));
+            s.row0 = __builtin_amdgcn_readlane(t.row0, l), s.n = __builtin_amdgcn_readlane(t.n, l);
+            s.len = __builtin_amdgcn_readlane(t.len, l), s.slot = __builtin_amdgcn_readlane(t.slot, l);
             return true;
         }
         base += __builtin_amdgcn_readlane(incl, 63);
@@ -101,9 +123,9 @@ __device__ __forceinline__ bool kv_find(int n_seqs, int x, F count, int& b, int&
 // number of a block in codes and consts; -1: the table names no page
 __device__ __forceinline__ long long kv_block(const Kv& p, int b, int head, int blk)
 {
-    const int page = p.pages[(long long)b * p.page_stride + blk / p.bpp];
+    const int at = p.bpp.quot(blk), page = p.pages[(long long)b * p.page_stride + at];
     if ((unsigned)page >= (unsigned)p.n_pages) return -1;
-    return ((long long)page * p.heads + head) * p.bpp + blk % p.bpp;
+    return ((long long)page * p.heads + head) * p.bpp.d + (blk - at * (int)p.bpp.d);
 }
 
 __device__ __forceinline__ unsigned short* kv_ring_row(const Kv& p, int slot, int head, int kv, int pos)
@@ -138,7 +160,6 @@ struct KvAttend {  // the rest of llmint8_kv_attention's arguments
 struct KvPlan {
     int tile;    // rows (of all query heads that share keys) to a workgroup
     int tiles;   // tiles that a sequence has at most (tile = KV_STEP_ROWS), or that all have together
-    int groups;  // of four waves in a workgroup of 128 rows, that share its positions
     int splits;  // parts of the positions, joined by a kernel of their own if more than one
 };
 KvPlan kv_plan(const Kv& p, int heads_q);

@@ -148,31 +148,25 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a)
 
     int b, i;
     bool wrong = false;
-    auto usable = [&](int q, KvSeq& s) {
-        const bool ok = kv_seq(p, q, s);
-        if (!ok) wrong = true;
-        if (!ok || s.n == 0 || s.len == 0) return false;
-        if (s.len < s.n || (a.rot.half && s.len > a.rot.n_pos)) {
+    KvSeq s;
+    auto blocks = [&](const KvSeq& t) {
+        if (t.n == 0 || t.len == 0) return 0;
+        if (t.len < t.n || (a.rot.half && t.len > a.rot.n_pos)) {
             wrong = true;
-            return false;
+            return 0;
         }
-        return true;
-    };
-    auto blocks = [&](int q) {
-        KvSeq s;
-        return usable(q, s) ? (s.len - 1) / KV_BLOCK - (s.len - s.n) / KV_BLOCK + 1 : 0;
+        return (t.len - 1) / KV_BLOCK - (t.len - t.n) / KV_BLOCK + 1;
     };
     bool found;
     if (p.max_rows == 1) {  // one block a sequence: no need to count
         b = blockIdx.x, i = 0;
-        found = blocks(b) > 0;
+        if (!kv_seq(p, b, s)) wrong = true;
+        found = blocks(s) > 0;
     } else {
-        found = kv_find(p.n_seqs, blockIdx.x, blocks, b, i);
+        found = kv_find(p, blockIdx.x, blocks, b, s, i, wrong);
     }
     if (wrong) kv_flag(p, LLMINT8_KV_BAD_BATCH);
     if (!found) return;
-    KvSeq s;
-    if (!usable(b, s)) return;
 
     const int old = s.len - s.n, f = old / KV_BLOCK, e = s.len / KV_BLOCK, blk = f + i;
     const int lo = blk * KV_BLOCK, hi = lo + KV_BLOCK < s.len ? lo + KV_BLOCK : s.len;  // its positions that there are
@@ -314,19 +308,16 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const Kv p, unsigned short
     const int d = p.d, dpad = kv_dpad(d), LD = dpad + 8, tid = threadIdx.x, head = blockIdx.y;
     bool wrong = false;
     // Blocks of a sequence's rows, counted back from its last: the rows at positions before 0 are one more "block" each 32.
-    auto blocks = [&](int q) {
-        KvSeq s;
-        if (!kv_seq(p, q, s)) wrong = true;
-        if (s.n == 0) return 0;
-        const int first = s.len - s.n + (KV_MAX_LEN >> 1);  // above 0, the blocks' borders where they were
-        return (first + s.n - 1) / KV_BLOCK - first / KV_BLOCK + 1;
+    auto blocks = [&](const KvSeq& t) {
+        if (t.n == 0) return 0;
+        const int first = t.len - t.n + (KV_MAX_LEN >> 1);  // above 0, the blocks' borders where they were
+        return (first + t.n - 1) / KV_BLOCK - first / KV_BLOCK + 1;
     };
     int b, i;
-    const bool found = kv_find(p.n_seqs, blockIdx.x, blocks, b, i);
+    KvSeq s;
+    const bool found = kv_find(p, blockIdx.x, blocks, b, s, i, wrong);
     if (wrong) kv_flag(p, LLMINT8_KV_BAD_BATCH);
     if (!found) return;
-    KvSeq s;
-    kv_seq(p, b, s);
     const int old = s.len - s.n, f = (old + (KV_MAX_LEN >> 1)) / KV_BLOCK - (KV_MAX_LEN >> 1) / KV_BLOCK, blk = f + i;
     const int lo = blk * KV_BLOCK, hi = lo + KV_BLOCK < s.len ? lo + KV_BLOCK : s.len, from = lo > old ? lo : old;
     const long long row = s.row0 + (long long)(from - old);
@@ -401,7 +392,7 @@ Kv kv_args(const llmint8_kv_cache_t* c, const llmint8_kv_batch_t* b)
     Kv p;
     p.codes = c->codes, p.consts = (unsigned*)c->consts, p.ring = (unsigned short*)c->ring;
     p.row_start = b->row_start, p.kv_len = b->kv_len, p.pages = b->pages, p.slots = b->slots, p.status = b->status;
-    p.n_pages = c->n_pages, p.bpp = c->page_tokens / KV_BLOCK, p.n_slots = c->n_slots, p.heads = c->heads, p.d = c->d;
+    p.n_pages = c->n_pages, p.bpp = Div(c->page_tokens / KV_BLOCK), p.n_slots = c->n_slots, p.heads = c->heads, p.d = c->d;
     p.n_seqs = b->n_seqs, p.n_rows = b->n_rows, p.page_stride = b->page_stride;
     p.max_rows = b->max_rows < b->n_rows ? b->max_rows : b->n_rows, p.max_len = b->max_len;
     return p;

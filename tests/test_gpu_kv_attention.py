@@ -45,6 +45,17 @@ def test_many_rows(d):
     dev.check_attention((0, 17, 0, 150, 0), rng, group=1, window=64)
 
 
+@pytest.mark.parametrize("blocks", [1, 2, 3, 54, 55, 56, 57, 58, 62, 63, 64, 65, 110, 111, 112, 113, 114, 128, 168])
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_numbers_of_blocks(blocks, rows):
+    """Around the numbers that the kernels look up or keep at once, with and without an open block."""
+    rng = np.random.default_rng(blocks)
+    for length in (32 * blocks, 32 * blocks + 5):
+        dev = filled((length,), 1, 32, page=32, seed=blocks)
+        dev.check_attention((min(rows, length),), rng)
+        assert int(dev.status) == 0
+
+
 @pytest.mark.parametrize("group, new", [(1, 1), (2, 40)])
 def test_rows_that_see_everything(group, new):
     rng = np.random.default_rng(3)
