@@ -104,9 +104,9 @@ __device__ __forceinline__ void peak(float top, float& M, float& l, G grown)
     }
 }
 
-// Weights of a block as the operands of the second product, and their share of l: by their fp32 values, since those of a block whose
+// Weights of a block as the operands of the second product; returns their sum, of the fp32 values, since those of a block whose
 // values are small may be nothing in fp16.
-__device__ __forceinline__ void expo(const f16v& sc, const Factors& fa, float M, float& l, h8 (&pf)[2])
+__device__ __forceinline__ float expo(const f16v& sc, const Factors& fa, float M, h8 (&pf)[2])
 {
     const float off = fa.lcv - M;
     float p[16], sum = 0.0f;
@@ -116,7 +116,7 @@ __device__ __forceinline__ void expo(const f16v& sc, const Factors& fa, float M,
         sum += p[i];
     }
     pf[0] = pack8(p), pf[1] = pack8(p + 8);
-    l = __builtin_fmaf(sum, fa.inv, l);
+    return sum;
 }
 
 struct AttendArgs {
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         h8 pf[2];
         if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
         peak(top_of(sc, fa), m, l, rescale);
-        expo(sc, fa, m, l, pf);
+        l = __builtin_fmaf(expo(sc, fa, m, pf), fa.inv, l);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             o[t] = mfma(codes8(x.v[t][0], x.v[t][1]), pf[0], o[t]);
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         h8 pf[2];
         hide(sc, base, hh, rlo, rhi);
         peak(top_of(sc, fa), m, l, rescale);
-        expo(sc, fa, m, l, pf);
+        l = __builtin_fmaf(expo(sc, fa, m, pf), fa.inv, l);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             float y[16];
@@ -449,7 +449,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     const int chunk = chunk_of(end - first, splits, 2);
     const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
     const int closed = s.len / KV_BLOCK, k1 = c1 < closed ? c1 : closed;
-    const int stages = k1 > c0 ? (k1 - c0 + 1) / 2 : 0;
+    // (an even number of stages, so that a stage's registers are known to the compiler; one that is not there has no weights)
+    const int stages = k1 > c0 ? (k1 - c0 + 3) / 4 * 2 : 0;
     const long long total = (long long)p.n_rows * a.heads_q;
     if (split && c0 >= c1) {  // nothing left for this part
         for (int r = r0 + tid; r < r1; r += THREADS)
@@ -463,13 +464,13 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         seen(a, s.len, old + a.group.quot(w1 - 1), all_lo, some_hi);
     }
     auto clip = [&](int x) { return x < 0 ? 0 : x > stages ? stages : x; };
-    const int sa = clip((some_lo / KV_BLOCK - c0) >> 1), sb = clip(((some_hi + KV_BLOCK - 1) / KV_BLOCK - c0 + 1) >> 1);
+    const int sa = clip((some_lo / KV_BLOCK - c0) >> 2 << 1), sb = clip(((some_hi + KV_BLOCK - 1) / KV_BLOCK - c0 + 3) >> 2 << 1);
 
     // ---- Lane i of every wave looks up the i-th of 64 blocks, so that a stage waits neither for the page table nor for constants.
     // `ahead` are 64 blocks from PERIOD behind the first of those in use on.
     constexpr int PERIOD = 56;
     struct Looked {
-        int at[2];  // number in codes
+        int at[2];  // where a block's codes begin
         Factors f;
     };
     auto look_up = [&](int j) {
@@ -480,6 +481,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         const bool there = at >= 0 && k < k1;
         at = at < 0 ? 0 : at;  // (weights of 0 for what is not there)
         r.f = factors(there, p.consts[at], a.scale);
+        at *= 2 * KV_BLOCK * DP;
         r.at[0] = (int)at, r.at[1] = (int)(at >> 32);
         return r;
     };
@@ -487,9 +489,10 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     int j0 = 0;  // the first block of `use`
     auto float_at = [&](float x, int j) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), j - j0)); };
     auto factors_of = [&](int j) { return Factors{float_at(use.f.ks, j), float_at(use.f.lcv, j), float_at(use.f.inv, j)}; };
-    // where a block's keys and values lie in LDS
-    auto keys = [&](int j) { return (h8*)(lds + (j & 3) * (DP * 32)) + lane; };
-    auto values = [&](int j) { return (h8*)(lds + (4 + (j & 3)) * (DP * 32)) + lane; };
+    // where the keys and values of block j lie in LDS, by j % 4 (a constant wherever it matters)
+    h8* const my_lds = (h8*)lds + lane;
+    auto keys = [&](int j) { return my_lds + (j & 3) * (DP * 4); };
+    auto values = [&](int j) { return my_lds + (4 + (j & 3)) * (DP * 4); };
     // this thread's 16-byte pieces of the keys (value 0) or values of blocks j and j + 1
     auto request = [&](int j, int value, u4 (&piece)[PER]) {
 #pragma unroll
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             if (PIECES % THREADS && t >= PIECES) break;
             const long long at = (long long)__builtin_amdgcn_readlane(use.at[1], j + x - j0) << 32 |
                                  (unsigned)__builtin_amdgcn_readlane(use.at[0], j + x - j0);
-            piece[i] = *((const u4*)(p.codes + at * (2 * KV_BLOCK * DP)) + value * DP * 2 + u + lane);
+            piece[i] = *((const u4*)(p.codes + at) + value * DP * 2 + u + lane);
         }
     };
     auto deposit_half = [&](int j, int value, const u4 (&piece)[PER], int half) {
@@ -512,10 +515,15 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     auto deposit = [&](int j, int value, const u4 (&piece)[PER]) { deposit_half(j, value, piece, 0), deposit_half(j, value, piece, 1); };
 
     // what the first stages need is requested before the rows of queries are
-    u4 pk[PER], pv[PER], k0[PER], k1_[PER], v0[PER];
+    struct Pieces {
+        u4 k[PER], v[PER];
+    };
+    Pieces first_, even, odd;  // what is on its way for stages of even and odd numbers: two stages ahead, the latency of a load
+    u4 k1_[PER];
     if (stages) {
         use = look_up(0);
-        request(0, 0, k0), request(1, 0, k1_), request(0, 1, v0), request(3, 0, pk), request(2, 1, pv);
+        request(0, 0, first_.k), request(1, 0, k1_), request(0, 1, first_.v);
+        request(3, 0, even.k), request(2, 1, even.v), request(5, 0, odd.k), request(4, 1, odd.v);
     }
     h8 qf[DP / 16];
     load_q<DP>(a, s, head, w0 + qr, hh, qf);
@@ -539,22 +547,29 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
     };
 
-    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums, and between those
-    // products the next scores' maximum, which is returned (for both halves of a row; without what may have to be hidden).  other(x),
-    // x = 0 .. 3: a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS some slices
-    // ahead (its latency) and no further, or registers run out.  k: the next block's first keys; on return, if NEXT, those of
-    // the one behind.
+    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums.  other(x), x = 0 .. 3:
+    // a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS some slices ahead (its
+    // latency) and no further, or registers run out.  k: the next block's first keys; on return, if NEXT, those of the one behind.
+    //
+    // A wave issues an instruction every eight cycles at best, whatever its kind, and registers allow two waves to a SIMD: what
+    // counts is the number of instructions.  So no maximum is taken: M stays as it is unless a weight sum says that it is too low
+    // (above LIMIT, which fp16 weights up to that stand; infinite where a row has seen nothing yet), and then the block's
+    // weights are made anew.
     constexpr int S = DP / 16, AHEAD = S < 4 ? S : 4, U = 2 * NT;
+    constexpr float LIMIT = 4096.0f;
     auto first_keys = [&](int j, h8 (&k)[AHEAD]) {
         const h8* const kb = keys(j);
 #pragma unroll
         for (int g = 0; g < AHEAD; g++) k[g] = kb[g * 64];
     };
-    auto step = [&](auto with_next, int j, f16v& sc, const Factors& fa, f16v& next, const Factors& fb, h8 (&k)[AHEAD], auto other) {
+    auto step = [&](auto slot, auto with_next, int j, f16v& sc, const Factors& fa, f16v& next, h8 (&k)[AHEAD], auto other) {
+        constexpr int J = decltype(slot)::value;  // j % 4
         constexpr bool NEXT = decltype(with_next)::value;
-        const h8 *const kb = keys(j + 1), *const kc = keys(j + 2), *const vb = values(j);
+        const h8 *const kb = keys(J + 1), *const kc = keys(J + 2), *const vb = values(J);
+        const int pos0 = (c0 + j) * KV_BLOCK;
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
         const float off = fa.lcv - m;
-        float sum = 0.0f, mx = 0.0f;
+        float sum = 0.0f, p[16];
         h8 pf[2], v[NT];
         next = f16v{};
 #pragma unroll
@@ -567,17 +582,27 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             next = mfma(t, qf[g], next);
 #pragma unroll
             for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
-                sc[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), sc[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
-                pf[i >> 3][i & 7] = (_Float16)sc[i], pf[i >> 3][(i & 7) + 1] = (_Float16)sc[i + 1];
+                p[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), p[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
+                pf[i >> 3][i & 7] = (_Float16)p[i], pf[i >> 3][(i & 7) + 1] = (_Float16)p[i + 1];
             }
             if (g)
 #pragma unroll
-                for (int i = 8 * (g - 1) / S * 2; i < 8 * g / S * 2; i++) sum += sc[i];
+                for (int i = 8 * (g - 1) / S * 2; i < 8 * g / S * 2; i++) sum += p[i];
 #pragma unroll
             for (int x = 0; x < 4; x++)
                 if (g == x * S / 4) other(x);
             __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = 8 * (S - 1) / S * 2; i < 16; i++) sum += p[i];
+        if (__any(sum > LIMIT)) {
+            const float n = fmaxf(m, top_of(sc, fa)), f = exp2_(m - n);
+            l *= f;
+            m = n;
+            rescale(f);
+            sum = expo(sc, fa, m, pf);
+        }
+        l = __builtin_fmaf(sum, fa.inv, l);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int y = u / NT, q = u % NT;
@@ -588,25 +613,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
                 for (int g = 0; g < AHEAD; g++)
                     if (g * NT / AHEAD == q) k[g] = kc[g * 64];
             o[q] = mfma(t, pf[y], o[q]);
-            if (u == 0)
-#pragma unroll
-                for (int i = 8 * (S - 1) / S * 2; i < 16; i++) sum += sc[i];
-            if (u)
-#pragma unroll
-                for (int i = 8 * (u - 1) / (U - 1); i < 8 * u / (U - 1); i++)
-                    mx = i ? max3(mx, next[2 * i], next[2 * i + 1]) : fmaxf(next[0], next[1]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        l = __builtin_fmaf(sum, fa.inv, l);
-        return halves_max(fmaxf(__builtin_fmaf(mx, fb.ks, fb.lcv), LOWEST));
-    };
-    auto look = [&](int j, f16v& sc, float top, const Factors& fa) {
-        const int pos0 = (c0 + j) * KV_BLOCK;
-        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) {
-            hide(sc, pos0, hh, rlo, rhi);
-            top = top_of(sc, fa);
-        }
-        peak(top, m, l, rescale);
     };
 
     // ---- the open block, fp16 from the ring, before the others
@@ -648,7 +656,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             hide(sc, pos0, hh, rlo, full_hi);
             peak(top_of(sc, fa), m, l, rescale);
             h8 pf[2];
-            expo(sc, fa, m, l, pf);
+            l = __builtin_fmaf(expo(sc, fa, m, pf), fa.inv, l);
             const h8* const vb = values(0);
 #pragma unroll
             for (int y = 0; y < 2; y++)
@@ -663,16 +671,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     if (stages) {
         ahead = use;  // (its addresses may be read from once more after the last block)
         if (k1 - c0 > PERIOD) ahead = look_up(PERIOD);
-        deposit(0, 0, k0);
+        deposit(0, 0, first_.k);
         __syncthreads();  // (block 1's keys come twice)
-        deposit(1, 0, k1_), deposit(0, 1, v0);
+        deposit(1, 0, k1_), deposit(0, 1, first_.v);
         __syncthreads();
-        auto more = [&](int st) {  // the end of a stage
+        auto more = [&](int st, Pieces& x) {  // the end of a stage
             if (2 * st + 2 == j0 + PERIOD) {
                 use = ahead, j0 += PERIOD;
                 if (k1 - c0 > j0 + PERIOD) ahead = look_up(j0 + PERIOD);
             }
-            request(2 * st + 5, 0, pk), request(2 * st + 4, 1, pv);
+            request(2 * st + 7, 0, x.k), request(2 * st + 6, 1, x.v);
             __syncthreads();
         };
         // The wave's first scores are computed in the stage before (its keys are overwritten in its own)
@@ -681,33 +689,35 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         auto enter = [&]() {
             scores(2 * sa, s0);
             f0 = factors_of(2 * sa);
-            look(2 * sa, s0, top_of(s0, f0), f0);
+        };
+        auto idle = [&](int st, Pieces& x) {  // a stage in which the wave's rows see nothing
+            deposit(2 * st + 3, 0, x.k), deposit(2 * st + 2, 1, x.v);
+            more(st, x);
+        };
+        auto busy = [&](auto slot, int st, Pieces& x) {
+            constexpr int J = decltype(slot)::value;
+            typedef std::integral_constant<int, J> first;
+            typedef std::integral_constant<int, J + 1> second;
+            h8 k[AHEAD];
+            first_keys(J + 1, k);
+            const Factors f1 = factors_of(2 * st + 1);
+            step(first(), std::true_type(), 2 * st, s0, f0, s1, k, [](int) {});
+            f0 = factors_of(2 * st + 2);
+            step(second(), std::false_type(), 2 * st + 1, s1, f1, s0, k, [&](int y) {
+                deposit_half(y < 2 ? J + 3 : J + 2, y >> 1, y < 2 ? x.k : x.v, y & 1);
+            });
+            more(st, x);
         };
         if (sa == 0) enter();
         __syncthreads();
         int st = 0;
-        for (; st < sa; st++) {
-            if (st + 1 == sa) enter();
-            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
-            more(st);
+        for (; st < sa; st += 2) {
+            idle(st, even);
+            if (st + 2 == sa) enter();
+            idle(st + 1, odd);
         }
-        for (; st < sb; st++) {
-            h8 k[AHEAD];
-            first_keys(2 * st + 1, k);
-            const Factors f1 = factors_of(2 * st + 1);
-            float top = step(std::true_type(), 2 * st, s0, f0, s1, f1, k, [](int) {});
-            f0 = factors_of(2 * st + 2);
-            look(2 * st + 1, s1, top, f1);
-            top = step(std::false_type(), 2 * st + 1, s1, f1, s0, f0, k, [&](int x) {
-                deposit_half(2 * st + (x < 2 ? 3 : 2), x >> 1, x < 2 ? pk : pv, x & 1);
-            });
-            look(2 * st + 2, s0, top, f0);
-            more(st);
-        }
-        for (; st < stages; st++) {
-            deposit(2 * st + 3, 0, pk), deposit(2 * st + 2, 1, pv);
-            more(st);
-        }
+        for (; st < sb; st += 2) busy(std::integral_constant<int, 0>(), st, even), busy(std::integral_constant<int, 2>(), st + 1, odd);
+        for (; st < stages; st += 2) idle(st, even), idle(st + 1, odd);
     }
 
     const float den = l + __shfl_xor(l, 32);
