@@ -228,7 +228,6 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     const int k1 = c1 < closed ? c1 : closed;
 
     h8 qf[DP / 16];
-    load_q<DP>(a, s, head, r0 + qr, hh, qf);
     int rlo, rhi;  // what this lane's row sees
     seen(a, s.len, s.len - s.n + a.group.quot(r0 + qr), rlo, rhi);
 
@@ -265,12 +264,14 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         x.at = (long long)__builtin_amdgcn_readlane((int)(at_ >> 32), i & 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)at_, i & 63);
         x.f = {uniform(f_.ks, i & 63), uniform(f_.lcv, i & 63), uniform(f_.inv, i & 63)};
     };
-    auto request = [&](const Block& x, u4 (&y)[NT], int value) {
-        const u4* src = (const u4*)(p.codes + x.at * (2 * KV_BLOCK * DP)) + lane + 64 * NT * value;
+    // (where: the lane; or 0, when the block is not wanted but the number of requests on their way has to be the same)
+    auto request = [&](const Block& x, u4 (&y)[NT], int value, int where) {
+        const u4* src = (const u4*)(p.codes + x.at * (2 * KV_BLOCK * DP)) + where + 64 * NT * value;
 #pragma unroll
         for (int t = 0; t < NT; t++) y[t] = __builtin_nontemporal_load(src + 64 * t);
     };
-    auto take = [&](int i, Block& x) {
+    auto take = [&](auto refill, int i, Block& x) {
+        constexpr bool REFILL = decltype(refill)::value;
         f16v sc = {};
 #pragma unroll
         for (int t = 0; t < NT; t++) {
@@ -278,10 +279,10 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
             sc = mfma(codes8(x.k[t][2], x.k[t][3]), qf[2 * t + 1], sc);
         }
         const Factors fa = x.f;
-        const bool more = i + 2 < nb;
-        if (more) {
-            name(i + 2, x);
-            request(x, x.k, 0);
+        const int where = i + 2 < nb ? lane : 0;
+        if (REFILL) {
+            if (i + 2 < nb) name(i + 2, x);
+            request(x, x.k, 0, where);
         }
         const int pos0 = (c0 + w + 4 * i) * KV_BLOCK;
         h8 pf[2];
@@ -293,21 +294,23 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
             o[t] = mfma(codes8(x.v[t][0], x.v[t][1]), pf[0], o[t]);
             o[t] = mfma(codes8(x.v[t][2], x.v[t][3]), pf[1], o[t]);
         }
-        if (more) request(x, x.v, 1);
+        if (REFILL) request(x, x.v, 1, where);
     };
+    Block x, y;
     if (nb > 0) {
-        Block x, y;
         look_up(0);
-        name(0, x);
-        request(x, x.k, 0), request(x, x.v, 1);
-        if (nb > 1) {
-            name(1, y);
-            request(y, y.k, 0), request(y, y.v, 1);
-        }
-        for (int i = 0; i < nb; i += 2) {
-            take(i, x);
-            if (i + 1 < nb) take(i + 1, y);
-        }
+        name(0, x), name(nb > 1, y);
+        request(x, x.k, 0, lane), request(x, x.v, 1, lane);
+        request(y, y.k, 0, nb > 1 ? lane : 0), request(y, y.v, 1, nb > 1 ? lane : 0);
+    }
+    load_q<DP>(a, s, head, r0 + qr, hh, qf);
+    // (a wait for the rows of queries inside the loop would be one for what was requested since, too)
+#pragma unroll
+    for (int t = 0; t < DP / 16; t++) asm volatile("" : "+v"(qf[t]));
+    if (nb > 0) {
+        int i = 0;
+        for (; i + 1 < nb; i += 2) take(std::true_type(), i, x), take(std::true_type(), i + 1, y);
+        if (i < nb) take(std::false_type(), i, x);
     }
     // The open block, fp16: by the wave whose turn it is.  Its values are scaled by a power of two to what codes are, at most 128.
     if (closed >= c0 && closed < c1 && ((closed - c0) & 3) == w) {
@@ -708,6 +711,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             });
             more(st, x);
         };
+        // The rows of queries have to be there before the loop: a wait for them inside would be one for what was requested since, too
+#pragma unroll
+        for (int t = 0; t < DP / 16; t++) asm volatile("" : "+v"(qf[t]));
         if (sa == 0) enter();
         __syncthreads();
         int st = 0;
