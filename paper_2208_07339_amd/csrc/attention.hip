@@ -507,15 +507,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             piece[i] = *((const u4*)(p.codes + at) + value * DP * 2 + u + lane);
         }
     };
-    auto deposit_half = [&](int j, int value, const u4 (&piece)[PER], int half) {
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;
-            if (PIECES % THREADS && t >= PIECES) break;
-            ((value ? values(j + x) : keys(j + x)) + 2 * u)[64 * half] = codes8(piece[i][2 * half], piece[i][2 * half + 1]);
-        }
+    // the i-th of them into LDS, converted: its first or second eight codes
+    auto deposit_half = [&](int j, int value, const u4& piece, int i, int half) {
+        const int t = w * 64 + THREADS * i, x = t >= DP * 2, u = t - x * DP * 2;
+        if (PIECES % THREADS && t >= PIECES) return;
+        ((value ? values(j + x) : keys(j + x)) + 2 * u)[64 * half] = codes8(piece[2 * half], piece[2 * half + 1]);
     };
-    auto deposit = [&](int j, int value, const u4 (&piece)[PER]) { deposit_half(j, value, piece, 0), deposit_half(j, value, piece, 1); };
+    auto deposit = [&](int j, int value, const u4 (&piece)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; i++) deposit_half(j, value, piece[i], i, 0), deposit_half(j, value, piece[i], i, 1);
+    };
 
     // what the first stages need is requested before the rows of queries are
     struct Pieces {
@@ -550,30 +551,36 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         for (int g = 0; g < DP / 16; g++) sc = mfma(kb[g * 64], qf[g], sc);
     };
 
-    // Weights of block j from its scores in slices between the products of the next block's scores, then its sums.  other(x), x = 0 .. 3:
-    // a quarter of what else there is to do.  The order is fixed slice by slice: operands are read from LDS some slices ahead (its
-    // latency) and no further, or registers run out.  k: the next block's first keys; on return, if NEXT, those of the one behind.
+    // Block j, whose scores are sc and whose first eight weights a lane are there (pfa, their sum suma): the next block's scores,
+    // product by product, and between these products the other eight weights; then the block's sums, and between these products the next
+    // block's first eight weights.  So the matrix unit and the vector unit have the same share of each slice, which is what keeps
+    // both busy with the two waves to a SIMD that registers allow.  other(x), x = 0 .. 7: an eighth of what else there is to do.
+    // The order is fixed slice by slice: operands are read from LDS some slices ahead (its latency) and no further, or registers run
+    // out.  k: the next block's first keys; on return, if NEXT, those of the one behind.
     //
-    // A wave issues an instruction every eight cycles at best, whatever its kind, and registers allow two waves to a SIMD: what
-    // counts is the number of instructions.  So no maximum is taken: M stays as it is unless a weight sum says that it is too low
-    // (above LIMIT, which fp16 weights up to that stand; infinite where a row has seen nothing yet), and then the block's
-    // weights are made anew.
+    // No maximum is taken: M stays as it is unless a weight sum says that it is too low (above LIMIT, which fp16 weights up to that
+    // stand; infinite where a row has seen nothing yet), and then the block's weights are made anew.
     constexpr int S = DP / 16, AHEAD = S < 4 ? S : 4, U = 2 * NT;
     constexpr float LIMIT = 4096.0f;
+    h8 pfa;
+    float suma;
     auto first_keys = [&](int j, h8 (&k)[AHEAD]) {
         const h8* const kb = keys(j);
 #pragma unroll
         for (int g = 0; g < AHEAD; g++) k[g] = kb[g * 64];
     };
-    auto step = [&](auto slot, auto with_next, int j, f16v& sc, const Factors& fa, f16v& next, h8 (&k)[AHEAD], auto other) {
+    auto masked = [&](int j, f16v& sc) {
+        const int pos0 = (c0 + j) * KV_BLOCK;
+        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
+    };
+    auto step = [&](auto slot, auto with_next, int j, const f16v& sc, const Factors& fa, f16v& next, const Factors& fb, h8 (&k)[AHEAD],
+                    auto other) {
         constexpr int J = decltype(slot)::value;  // j % 4
         constexpr bool NEXT = decltype(with_next)::value;
         const h8 *const kb = keys(J + 1), *const kc = keys(J + 2), *const vb = values(J);
-        const int pos0 = (c0 + j) * KV_BLOCK;
-        if (pos0 < all_lo || pos0 + KV_BLOCK > all_hi) hide(sc, pos0, hh, rlo, rhi);
-        const float off = fa.lcv - m;
-        float sum = 0.0f, p[16];
+        float off = fa.lcv - m, sum = suma, p[8];
         h8 pf[2], v[NT];
+        pf[0] = pfa;
         next = f16v{};
 #pragma unroll
         for (int g = 0; g < S; g++) {
@@ -584,20 +591,17 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
                 if (g == S - AHEAD + q * AHEAD / NT) v[q] = vb[2 * q * 64];
             next = mfma(t, qf[g], next);
 #pragma unroll
-            for (int i = 8 * g / S * 2; i < 8 * (g + 1) / S * 2; i += 2) {
-                p[i] = exp2_(__builtin_fmaf(sc[i], fa.ks, off)), p[i + 1] = exp2_(__builtin_fmaf(sc[i + 1], fa.ks, off));
-                pf[i >> 3][i & 7] = (_Float16)p[i], pf[i >> 3][(i & 7) + 1] = (_Float16)p[i + 1];
+            for (int i = 8 * g / S; i < 8 * (g + 1) / S; i++) {
+                p[i] = exp2_(__builtin_fmaf(sc[8 + i], fa.ks, off));
+                if (i & 1) pf[1][i - 1] = (_Float16)p[i - 1], pf[1][i] = (_Float16)p[i];
+                if (i) sum += p[i - 1];
             }
-            if (g)
-#pragma unroll
-                for (int i = 8 * (g - 1) / S * 2; i < 8 * g / S * 2; i++) sum += p[i];
 #pragma unroll
             for (int x = 0; x < 4; x++)
                 if (g == x * S / 4) other(x);
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int i = 8 * (S - 1) / S * 2; i < 16; i++) sum += p[i];
+        sum += p[7];
         if (__any(sum > LIMIT)) {
             const float n = fmaxf(m, top_of(sc, fa)), f = exp2_(m - n);
             l *= f;
@@ -606,6 +610,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             sum = expo(sc, fa, m, pf);
         }
         l = __builtin_fmaf(sum, fa.inv, l);
+        masked(j + 1, next);
+        off = fb.lcv - m;
+        suma = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int y = u / NT, q = u % NT;
@@ -616,8 +623,19 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
                 for (int g = 0; g < AHEAD; g++)
                     if (g * NT / AHEAD == q) k[g] = kc[g * 64];
             o[q] = mfma(t, pf[y], o[q]);
+            if (u)  // (the last product of the scores takes a while)
+#pragma unroll
+                for (int i = 8 * (u - 1) / (U - 1); i < 8 * u / (U - 1); i++) {
+                    p[i] = exp2_(__builtin_fmaf(next[i], fb.ks, off));
+                    if (i & 1) pfa[i - 1] = (_Float16)p[i - 1], pfa[i] = (_Float16)p[i];
+                    if (i) suma += p[i - 1];
+                }
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                if (u == x * U / 4) other(4 + x);
             __builtin_amdgcn_sched_barrier(0);
         }
+        suma += p[7];
     };
 
     // ---- the open block, fp16 from the ring, before the others
@@ -692,6 +710,11 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         auto enter = [&]() {
             scores(2 * sa, s0);
             f0 = factors_of(2 * sa);
+            masked(2 * sa, s0);
+            h8 pf[2];
+            expo(s0, f0, m, pf);
+            pfa = pf[0];
+            suma = __builtin_inff();  // (the weights are made anew by M's first value if a row has none, and by any other)
         };
         auto idle = [&](int st, Pieces& x) {  // a stage in which the wave's rows see nothing
             deposit(2 * st + 3, 0, x.k), deposit(2 * st + 2, 1, x.v);
@@ -704,11 +727,15 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
             h8 k[AHEAD];
             first_keys(J + 1, k);
             const Factors f1 = factors_of(2 * st + 1);
-            step(first(), std::true_type(), 2 * st, s0, f0, s1, k, [](int) {});
+            // the conversions: keys in the first half of the stage, values in the second, and not before what they come from is there
+            auto part = [&](int value, const u4 (&y)[PER], int n) {
+#pragma unroll
+                for (int i = 0; i < 2 * PER; i++)
+                    if (n == (8 * i + 4) / (2 * PER)) deposit_half(value ? J + 2 : J + 3, value, y[i >> 1], i >> 1, i & 1);
+            };
+            step(first(), std::true_type(), 2 * st, s0, f0, s1, f1, k, [&](int n) { part(0, x.k, n); });
             f0 = factors_of(2 * st + 2);
-            step(second(), std::false_type(), 2 * st + 1, s1, f1, s0, k, [&](int y) {
-                deposit_half(y < 2 ? J + 3 : J + 2, y >> 1, y < 2 ? x.k : x.v, y & 1);
-            });
+            step(second(), std::false_type(), 2 * st + 1, s1, f1, s0, f0, k, [&](int n) { part(1, x.v, n); });
             more(st, x);
         };
         // The rows of queries have to be there before the loop: a wait for them inside would be one for what was requested since, too
