@@ -249,20 +249,26 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
         Factors f;
     };
     long long at_ = 0;
+    unsigned c_ = 0;
+    bool there_ = false;
     Factors f_ = {};
-    auto look_up = [&](int i0) {
+    auto look_at = [&](int i0) {
         const int i = i0 + lane < nb ? i0 + lane : nb - 1;
         at_ = kv_block(p, b, head, c0 + w + 4 * i);
-        const bool there = at_ >= 0;
-        if (!there) kv_flag(p, LLMINT8_KV_BAD_PAGE);
-        at_ = there ? at_ : 0;  // (weights of 0 for what is not there)
-        f_ = factors(there, p.consts[at_], a.scale);
+        there_ = at_ >= 0;
+        if (!there_) kv_flag(p, LLMINT8_KV_BAD_PAGE);
+        at_ = there_ ? at_ : 0;  // (weights of 0 for what is not there)
+        c_ = p.consts[at_];
     };
+    auto weigh = [&]() { f_ = factors(there_, c_, a.scale); };
     auto uniform = [](float x, int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i)); };
-    auto name = [&](int i, Block& x) {  // the i-th block: where it is
-        if (i && (i & 63) == 0) look_up(i);
+    auto place = [&](int i, Block& x) {  // the i-th block: where it is, and its factors
         x.at = (long long)__builtin_amdgcn_readlane((int)(at_ >> 32), i & 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)at_, i & 63);
-        x.f = {uniform(f_.ks, i & 63), uniform(f_.lcv, i & 63), uniform(f_.inv, i & 63)};
+    };
+    auto factor = [&](int i, Block& x) { x.f = {uniform(f_.ks, i & 63), uniform(f_.lcv, i & 63), uniform(f_.inv, i & 63)}; };
+    auto name = [&](int i, Block& x) {
+        if ((i & 63) == 0) look_at(i), weigh();
+        place(i, x), factor(i, x);
     };
     // (where: the lane; or 0, when the block is not wanted but the number of requests on their way has to be the same)
     auto request = [&](const Block& x, u4 (&y)[NT], int value, int where) {
@@ -298,8 +304,8 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     };
     Block x, y;
     if (nb > 0) {
-        look_up(0);
-        name(0, x), name(nb > 1, y);
+        look_at(0);
+        place(0, x), place(nb > 1, y);
         request(x, x.k, 0, lane), request(x, x.v, 1, lane);
         request(y, y.k, 0, nb > 1 ? lane : 0), request(y, y.v, 1, nb > 1 ? lane : 0);
     }
@@ -308,6 +314,8 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 #pragma unroll
     for (int t = 0; t < DP / 16; t++) asm volatile("" : "+v"(qf[t]));
     if (nb > 0) {
+        weigh();
+        factor(0, x), factor(nb > 1, y);
         int i = 0;
         for (; i + 1 < nb; i += 2) take(std::true_type(), i, x), take(std::true_type(), i + 1, y);
         if (i < nb) take(std::false_type(), i, x);
@@ -474,18 +482,25 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     constexpr int PERIOD = 56;
     struct Looked {
         int at[2];  // where a block's codes begin
+        unsigned c;
+        bool there;
         Factors f;
     };
-    auto look_up = [&](int j) {
+    auto look_at = [&](int j) {
         Looked r;
         const int k = c0 + j + lane;
         long long at = kv_block(p, b, head, k < k1 ? k : k1 - 1);
         if (at < 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
-        const bool there = at >= 0 && k < k1;
+        r.there = at >= 0 && k < k1;
         at = at < 0 ? 0 : at;  // (weights of 0 for what is not there)
-        r.f = factors(there, p.consts[at], a.scale);
+        r.c = p.consts[at];
         at *= 2 * KV_BLOCK * DP;
         r.at[0] = (int)at, r.at[1] = (int)(at >> 32);
+        return r;
+    };
+    auto look_up = [&](int j) {
+        Looked r = look_at(j);
+        r.f = factors(r.there, r.c, a.scale);
         return r;
     };
     Looked use, ahead;
@@ -525,7 +540,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     Pieces first_, even, odd;  // what is on its way for stages of even and odd numbers: two stages ahead, the latency of a load
     u4 k1_[PER];
     if (stages) {
-        use = look_up(0);
+        use = look_at(0);  // (what is requested next does not wait for the constants)
         request(0, 0, first_.k), request(1, 0, k1_), request(0, 1, first_.v);
         request(3, 0, even.k), request(2, 1, even.v), request(5, 0, odd.k), request(4, 1, odd.v);
     }
@@ -690,6 +705,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     // ---- Stage st: blocks 2 st and 2 st + 1 (from c0 on): their weights and sums, and each time the scores of the block behind.  So keys
     // go to LDS one block earlier than values: meanwhile those of 2 st + 3 and 2 st + 4, and the values of 2 st + 2 and 2 st + 3.
     if (stages) {
+        use.f = factors(use.there, use.c, a.scale);
         ahead = use;  // (its addresses may be read from once more after the last block)
         if (k1 - c0 > PERIOD) ahead = look_up(PERIOD);
         deposit(0, 0, first_.k);
@@ -962,14 +978,21 @@ KvPlan kv_plan(const Kv& p, int heads_q)
         const long long x = (all + p.n_seqs * (t - 1)) / t, y = p.n_seqs * ((rows + t - 1) / t);
         return x < y ? x : y;
     };
+    // The step kernel takes what it has registers for, and more rows where the cache's blocks and the row tiles are few: it reads and
+    // converts a block once for every 32 rows, but starts and ends in a third of the time (five tokens of 48 heads that share keys,
+    // eight sequences of 1 000 to 9 000 positions: 30 us against 42; 2 048 rows of 32 heads: 95 against 61).
+    const long long few = tiles(KV_STEP_ROWS) * p.heads;
     long long units;
-    if (rows <= KV_STEP_ROWS) {
-        r.tile = KV_STEP_ROWS, r.tiles = 1;
-        units = (long long)p.n_seqs * p.heads;
+    if (rows <= KV_STEP_ROWS || few * blocks <= 24576) {
+        r.tile = KV_STEP_ROWS, r.tiles = (int)((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS);
+        units = few;
     } else {
-        r.tile = rows > 128 && !wide ? 256 : 128;
+        // 256 rows convert a block half as often as two times 128, but are one workgroup to a compute unit, whose start and end nothing
+        // covers (2 048 positions: 70 us against 61; 8 192: 787 against 820)
+        r.tile = blocks >= 128 && rows > 128 && !wide ? 256 : 128;
         units = (r.tiles = (int)tiles(r.tile)) * p.heads;
     }
+    // one round of the chip, two workgroups to a compute unit if they have at most four waves
     const long long want = (r.tile == 256 ? 256 : 512) / units, most = (blocks + 7) / 8;
     r.splits = (int)(want < most ? want : most);
     if (r.splits < 1) r.splits = 1;
