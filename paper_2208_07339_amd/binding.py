@@ -23,6 +23,7 @@ SYMBOLS = [
 ]
 
 _lib = None
+_f16 = None  # torch.float16, once torch is there
 
 
 class _KvCache(C.Structure):  # llmint8_kv_cache_t
@@ -50,7 +51,9 @@ def lib():
                            "(hipcc, gfx950). There is no fallback path.")
     # torch first: it ships its own HIP runtime, and the library must bind to the one the tensors and
     # streams it is handed come from (a second runtime loaded earlier sees no device)
-    import torch  # noqa: F401
+    import torch
+    global _f16
+    _f16 = torch.float16
     L = C.CDLL(LIB_PATH)
     vp, i32, sz, f32 = C.c_void_p, C.c_int, C.c_size_t, C.c_float
     L.llmint8_status_string.restype = C.c_char_p
@@ -491,10 +494,8 @@ class KvCache:
         c = _KvCache(_ptr(self.codes), _ptr(self.consts), _ptr(self.ring), n_pages, self.page_tokens, self.ring.shape[0],
                      heads, self.d)
         object.__setattr__(self, "_c", c)
-
-    @property
-    def heads(self):
-        return self.codes.shape[1]
+        object.__setattr__(self, "heads", heads)
+        lib()  # (fails here if it is missing, and sets torch up)
 
     @staticmethod
     def allocate(n_pages, page_tokens, n_slots, heads, d, device="cuda"):
@@ -532,35 +533,33 @@ class KvBatch:
         object.__setattr__(self, "_c", c)
 
 
-def _head_rows(t, n_rows, d):
+def _head_rows(t, n_rows, heads, d):
     """Row stride of fp16 rows [n_rows, heads, d] whose heads lie one after the other."""
-    assert t.is_cuda and t.dtype == _torch().float16 and t.dim() == 3 and t.shape[0] == n_rows and t.shape[2] == d
-    rows, heads, one = t.stride()
-    assert (one == 1 or d == 1) and (heads == d or t.shape[1] == 1)
-    return rows if n_rows > 1 else max(rows, t.shape[1] * d)
+    assert t.dtype == _f16 and t.shape == (n_rows, heads, d) and t.is_cuda
+    row, head, one = t.stride()
+    assert (one == 1 or d == 1) and (head == d or heads == 1)
+    return row if n_rows > 1 else max(row, heads * d)
 
 
 def kv_append(cache, batch, k, v, q=None, q_out=None, cos=None, sin=None, pairs=False):
     """llmint8_kv_append: k, v [n_rows, heads, d] fp16 (rows may be slices of wider ones) into the cache; q [n_rows, heads_q, d],
     if given, rotated like the keys into q_out, which is returned (made if not given; may be q).  cos, sin: fp32
     [positions, rotated features / 2], or None: no rotation."""
-    torch = _torch()
-    n, d = batch.n_rows, cache.d
-    assert k.shape[1] == v.shape[1] == cache.heads
+    n, d, heads = batch.n_rows, cache.d, cache.heads
     rot = n_pos = ld_q = ld_out = heads_q = 0
     if cos is not None:
-        assert cos.is_cuda and sin.is_cuda and cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape
-        assert cos.dim() == 2 and cos.is_contiguous() and sin.is_contiguous()
-        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+        n_pos, half = cos.shape
+        rot = 2 * half
+        assert cos.shape == sin.shape and cos.dtype == sin.dtype == _torch().float32 and cos.is_cuda and sin.is_cuda
+        assert cos.is_contiguous() and sin.is_contiguous()
     if q is not None:
         heads_q = q.shape[1]
         if q_out is None:
-            q_out = torch.empty((n, heads_q, d), dtype=torch.float16, device=q.device)
-        assert q_out.shape == q.shape
-        ld_q, ld_out = _head_rows(q, n, d), _head_rows(q_out, n, d)
-    _check(lib().llmint8_kv_append(C.byref(cache._c), C.byref(batch._c), _ptr(k), _head_rows(k, n, d), _ptr(v),
-                                   _head_rows(v, n, d), _ptr(q), ld_q, _ptr(q_out) if q is not None else None, ld_out, heads_q, _ptr(cos),
-                                   _ptr(sin), n_pos, rot, int(pairs), _stream()))
+            q_out = _torch().empty((n, heads_q, d), dtype=_f16, device=q.device)
+        ld_q, ld_out = _head_rows(q, n, heads_q, d), _head_rows(q_out, n, heads_q, d)
+    _check(lib().llmint8_kv_append(cache._c, batch._c, _ptr(k), _head_rows(k, n, heads, d), _ptr(v), _head_rows(v, n, heads, d),
+                                   _ptr(q), ld_q, _ptr(q_out) if q is not None else None, ld_out, heads_q, _ptr(cos), _ptr(sin),
+                                   n_pos, rot, int(pairs), _stream()))
     return q_out
 
 
@@ -574,25 +573,23 @@ def kv_attention(cache, batch, q, scale=None, causal=True, window=0, ws=None, ou
     """llmint8_kv_attention: q [n_rows, heads_q, d] fp16 over the cache -> out, the same shape.  scale: 1 / sqrt(d) if None."""
     n, d, heads_q = batch.n_rows, cache.d, q.shape[1]
     if out is None:
-        out = _torch().empty((n, heads_q, d), dtype=_torch().float16, device=q.device)
-    assert out.shape == q.shape
+        out = _torch().empty((n, heads_q, d), dtype=_f16, device=q.device)
     if ws is None:
         ws = kv_attention_workspace(cache, batch, heads_q)
-    _check(lib().llmint8_kv_attention(C.byref(cache._c), C.byref(batch._c), _ptr(q), _head_rows(q, n, d), heads_q,
+    _check(lib().llmint8_kv_attention(cache._c, batch._c, _ptr(q), _head_rows(q, n, heads_q, d), heads_q,
                                       d ** -0.5 if scale is None else scale, int(causal), window, _ptr(out),
-                                      _head_rows(out, n, d), _ptr(ws.buf), ws.nbytes, _stream()))
+                                      _head_rows(out, n, heads_q, d), _ptr(ws.buf), ws.nbytes, _stream()))
     return out
 
 
 def kv_read(cache, batch, k=None, v=None):
     """llmint8_kv_read: keys and values at the batch's rows' positions, fp16 [n_rows, heads, d] each."""
-    torch = _torch()
     shape = (batch.n_rows, cache.heads, cache.d)
     if k is None and v is None:
-        k, v = (torch.empty(shape, dtype=torch.float16, device=cache.codes.device) for _ in range(2))
+        k, v = (_torch().empty(shape, dtype=_f16, device=cache.codes.device) for _ in range(2))
     for t in (k, v):
-        assert t is None or (t.is_cuda and t.dtype == torch.float16 and tuple(t.shape) == shape and t.is_contiguous())
-    _check(lib().llmint8_kv_read(C.byref(cache._c), C.byref(batch._c), _ptr(k), _ptr(v), _stream()))
+        assert t is None or (t.dtype == _f16 and t.shape == shape and t.is_contiguous() and t.is_cuda)
+    _check(lib().llmint8_kv_read(cache._c, batch._c, _ptr(k), _ptr(v), _stream()))
     return k, v
 
 

@@ -57,31 +57,25 @@ struct AppendArgs {
     Rows k, v, q;
     unsigned short* q_out;
     long long ld_q_out;
-    int heads_q, q_group, open_group;
+    int heads_q, q_group, head_groups;  // query heads to a workgroup; workgroups of key/value heads
     Rotation rot;
 };
 
-// Elements j and partner of a pair
-__device__ __forceinline__ void pair_of(const Rotation& r, int i, int& a, int& b)
-{
-    a = r.pairs ? 2 * i : i;
-    b = r.pairs ? 2 * i + 1 : i + r.half;
-}
-
-// Rows row .. row + n - 1 (positions pos ...) of heads h0 .. h1 - 1, from `in` to out(row number, head) -> pointer, rotated if turned,
-// made finite if FINITE.  VEC: d, rot and everything's alignment allow 8 features at a time (and halves of a pair
-// to lie in whole groups of 8); a thread has both halves of what it turns, so input and output may be the same.
+// Rows row .. row + n - 1 (positions pos ...) of heads h0 .. h1 - 1, rotated if turned, made finite if FINITE, to out(row number, head,
+// feature, value): eight features at a time if VEC, which d, rot and everything's alignment then allow (halves of pairs lie in
+// whole groups of 8), else one.  The work is that of threads 0 .. threads - 1; one has both halves of what it turns, so input and
+// output may be the same.
 template <bool VEC, bool FINITE, class Out>
-__device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, bool turned, int d, int row, int pos, int n, int h0,
-                                          int h1, Out out, bool& bad)
+__device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, bool turned, int d, int row, int pos, int n, int h0, int h1,
+                                          int thread, int threads, Out out, bool& bad)
 {
     const int nh = h1 - h0, half = turned ? rot.half : 0;
     const int per = VEC ? (rot.pairs || !half ? d / 8 : half / 8 + (d - 2 * half) / 8) : half + (d - 2 * half);
     const int total = n * nh * per;
-    for (int t = threadIdx.x; t < total; t += blockDim.x) {
-        const int u = t % per, gh = t / per % nh, i = t / per / nh;
+#pragma unroll 4
+    for (int t = thread; t < total; t += threads) {
+        const int rest = t / per, u = t - rest * per, i = nh == 1 ? rest : rest / nh, gh = rest - i * nh;
         const unsigned short* src = in.p + (row + i) * in.ld + (long long)(h0 + gh) * d;
-        unsigned short* dst = out(i, h0 + gh);
         const float* c = rot.cos + (long long)(pos + i) * half;
         const float* s = rot.sin + (long long)(pos + i) * half;
         if constexpr (VEC) {
@@ -96,8 +90,8 @@ __device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, b
                     a[e] = x, b[e] = y;
                 }
                 if (FINITE) a = finite8(a, bad), b = finite8(b, bad);
-                *(us8*)(dst + 8 * u) = a;
-                *(us8*)(dst + half + 8 * u) = b;
+                out(i, h0 + gh, 8 * u, a);
+                out(i, h0 + gh, half + 8 * u, b);
             } else {
                 const int f = 8 * (half && !rot.pairs ? u + half / 8 : u);
                 us8 a = *(const us8*)(src + f);
@@ -111,40 +105,50 @@ __device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, b
                     }
                 }
                 if (FINITE) a = finite8(a, bad);
-                *(us8*)(dst + f) = a;
+                out(i, h0 + gh, f, a);
             }
         } else {
             if (u < half) {
-                int ja, jb;
-                pair_of(rot, u, ja, jb);
+                const int ja = rot.pairs ? 2 * u : u, jb = rot.pairs ? 2 * u + 1 : u + half;
                 unsigned short x = src[ja], y = src[jb];
                 turn(x, y, c[u], s[u]);
                 if (FINITE) x = finite(x, bad), y = finite(y, bad);
-                dst[ja] = x, dst[jb] = y;
+                out(i, h0 + gh, ja, x);
+                out(i, h0 + gh, jb, y);
             } else {
-                const int f = half + u;
-                const unsigned short x = src[f];
-                dst[f] = FINITE ? finite(x, bad) : x;
+                unsigned short x = src[half + u];
+                if (FINITE) x = finite(x, bad);
+                out(i, h0 + gh, half + u, x);
             }
         }
     }
 }
 
-// One workgroup to a block that gets new tokens and a key/value head (y < heads), or to such a block's tokens and q_group query heads
-// (the y behind).  A block that gets full: its 32 rows go through LDS, where they are turned, their maximum is taken
-// and the codes are collected into tiles.  A block that stays open: its new rows go straight to the ring, open_group heads to
-// a workgroup, the other heads' workgroups have nothing to do.  The fp16 rows of the last two blocks go to the ring.
+__device__ __forceinline__ void put(unsigned short* p, us8 v) { *(us8*)p = v; }
+__device__ __forceinline__ void put(unsigned short* p, unsigned short v) { *p = v; }
+__device__ __forceinline__ unsigned larger(unsigned m, us8 v)
+{
+    const u4 y = __builtin_bit_cast(u4, v) & 0x7fff7fffu;
+    return pk_max_u16(pk_max_u16(m, pk_max_u16(y[0], y[1])), pk_max_u16(y[2], y[3]));
+}
+__device__ __forceinline__ unsigned larger(unsigned m, unsigned short v) { return pk_max_u16(m, v & 0x7fffu); }
+
+// One wave to a block that gets new tokens and a key/value head, HEADS waves to a workgroup (y < the heads' groups); the workgroups
+// behind take such a block's tokens and q_group query heads each.  A block that gets full: keys, then values, go through LDS, where
+// the codes are collected into tiles; their maximum is taken on the way.  The fp16 rows of the last two blocks go to the ring.  (A
+// workgroup to a block and head instead, its four waves meeting at barriers, took 134 us for 8 192 tokens of 40 heads and 18 us for a
+// token each of 96 sequences.)
 // A call that begins inside block f and ends more than a block later writes, for a later block c, the half of the ring that
-// holds f's old rows: then the workgroup of f writes c's rows there, when it has read the old ones.
+// holds f's old rows: then the wave of f writes c's rows there, when it has read the old ones.
 // LDS rows are 16 bytes longer than their data, so that the 16-byte reads of 32 rows at one feature spread over the banks.
+constexpr int HEADS = 2;
 template <bool VEC>
-__global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(64 * HEADS) kv_append_kernel(const AppendArgs a)
 {
     extern __shared__ __align__(16) unsigned short lds[];
-    __shared__ unsigned s_max[2][4];
     const Kv& p = a.kv;
     const int d = p.d, dpad = kv_dpad(d), LD = dpad + 8;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     int b, i;
     bool wrong = false;
@@ -173,122 +177,95 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a)
     const int from = lo > old ? lo : old;                                               // the new ones: from .. hi - 1
     bool bad = false;
 
-    if ((int)blockIdx.y >= p.heads) {
-        const int h0 = ((int)blockIdx.y - p.heads) * a.q_group, h1 = h0 + a.q_group < a.heads_q ? h0 + a.q_group : a.heads_q;
+    if ((int)blockIdx.y >= a.head_groups) {
+        const int h0 = ((int)blockIdx.y - a.head_groups) * a.q_group, h1 = h0 + a.q_group < a.heads_q ? h0 + a.q_group : a.heads_q;
         const int r0 = s.row0 + from - old;
-        move_rows<VEC, false>(a.q, a.rot, a.rot.half > 0, d, r0, from, hi - from, h0, h1,
-                              [&](int r, int g) { return a.q_out + (r0 + r) * a.ld_q_out + (long long)g * d; }, bad);
+        move_rows<VEC, false>(a.q, a.rot, a.rot.half > 0, d, r0, from, hi - from, h0, h1, threadIdx.x, 64 * HEADS,
+                              [&](int r, int g, int j, auto v) { put(a.q_out + (r0 + r) * a.ld_q_out + (long long)g * d + j, v); }, bad);
         return;
     }
-    const int head = blockIdx.y;
+    const int head = blockIdx.y * HEADS + w;
+    if (head >= p.heads) return;
     const bool full = hi - lo == KV_BLOCK;
     // the later block whose rows overwrite what this call reads of f
     const int clash = old % KV_BLOCK && f < e - 1 ? ((e - 1 - f) % 2 == 0 ? e - 1 : e) : -1;
-    auto to_ring = [&](int block, int h0, int h1) {
+    auto to_ring = [&](int block, int kv) {
         const int l = block * KV_BLOCK > old ? block * KV_BLOCK : old;
         const int n = (block + 1) * KV_BLOCK < s.len ? (block + 1) * KV_BLOCK - l : s.len - l;
-        move_rows<VEC, true>(a.k, a.rot, a.rot.half > 0, d, s.row0 + l - old, l, n, h0, h1,
-                             [&](int r, int g) { return kv_ring_row(p, s.slot, g, 0, l + r); }, bad);
-        move_rows<VEC, true>(a.v, a.rot, false, d, s.row0 + l - old, l, n, h0, h1,
-                             [&](int r, int g) { return kv_ring_row(p, s.slot, g, 1, l + r); }, bad);
+        move_rows<VEC, true>(kv ? a.v : a.k, a.rot, kv == 0 && a.rot.half > 0, d, s.row0 + l - old, l, n, head, head + 1, lane, 64,
+                             [&](int r, int, int j, auto v) { put(kv_ring_row(p, s.slot, head, kv, l + r) + j, v); }, bad);
     };
     if (!full) {
-        if (head % a.open_group) return;
-        const int h1 = head + a.open_group < p.heads ? head + a.open_group : p.heads;
-        if (blk != clash) to_ring(blk, head, h1);
+        if (blk != clash) to_ring(blk, 0), to_ring(blk, 1);
         if (bad) kv_flag(p, LLMINT8_KV_NOT_FINITE);
         return;
     }
 
     const long long at = kv_block(p, b, head, blk);
-    // ---- the block's rows into LDS
-    unsigned short* const L[2] = {lds, lds + KV_BLOCK * LD};
+    const bool keep = blk >= e - 1 && blk != clash;  // to the ring, too
+    unsigned short* const T = lds + w * KV_BLOCK * LD;
+    if (dpad > d)
+        for (int t = lane; t < KV_BLOCK * (dpad - d); t += 64) T[t / (dpad - d) * LD + d + t % (dpad - d)] = 0;
+#pragma unroll
     for (int kv = 0; kv < 2; kv++) {
-        unsigned short* const T = L[kv];
-        for (int t = tid; t < (from - lo) * (VEC ? d / 8 : d); t += 256) {  // those that were there
-            const int r = t / (VEC ? d / 8 : d), u = t % (VEC ? d / 8 : d);
+        unsigned m = 0;
+        const int per = VEC ? d / 8 : d;
+#pragma unroll 4
+        for (int t = lane; t < (from - lo) * per; t += 64) {  // the rows that were there
+            const int r = t / per, u = t - r * per;
             const unsigned short* src = kv_ring_row(p, s.slot, head, kv, lo + r);
-            if (VEC)
-                *(us8*)(T + r * LD + 8 * u) = *(const us8*)(src + 8 * u);
-            else
+            if constexpr (VEC) {
+                const us8 v = *(const us8*)(src + 8 * u);
+                m = larger(m, v);
+                put(T + r * LD + 8 * u, v);
+            } else {
+                m = larger(m, src[u]);
                 T[r * LD + u] = src[u];
+            }
         }
-        if (dpad > d)
-            for (int t = tid; t < KV_BLOCK * (dpad - d); t += 256) T[t / (dpad - d) * LD + d + t % (dpad - d)] = 0;
-        move_rows<VEC, true>(kv ? a.v : a.k, a.rot, kv == 0 && a.rot.half > 0, d, s.row0 + from - old, from, hi - from, head, head + 1,
-                             [&](int r, int) { return T + (from - lo + r) * LD; }, bad);
-    }
-    __syncthreads();
-    if (blk == f && clash >= 0) to_ring(clash, head, head + 1);
-    if (bad) kv_flag(p, LLMINT8_KV_NOT_FINITE);
-    if (at < 0) {
-        if (tid == 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
-    }
-    // ---- to the ring, if one of the last two blocks, and the maxima
-    const bool keep = blk >= e - 1 && blk != clash;
-    unsigned m[2] = {0, 0};
-    const int c8 = dpad / 8;
+        move_rows<VEC, true>(kv ? a.v : a.k, a.rot, kv == 0 && a.rot.half > 0, d, s.row0 + from - old, from, hi - from, head, head + 1, lane,
+                             64, [&](int r, int, int j, auto v) {
+                                 m = larger(m, v);
+                                 put(T + (from - lo + r) * LD + j, v);
+                                 if (keep) put(kv_ring_row(p, s.slot, head, kv, from + r) + j, v);
+                             }, bad);
+        if (blk == f && clash >= 0) to_ring(clash, kv);
+        __builtin_amdgcn_wave_barrier();  // (a wave's accesses to LDS are in order)
 #pragma unroll
-    for (int kv = 0; kv < 2; kv++)
-        for (int t = tid; t < KV_BLOCK * c8; t += 256) {
-            const int r = t / c8, u = t % c8;
-            const us8 x = *(const us8*)(L[kv] + r * LD + 8 * u);
-            const u4 y = __builtin_bit_cast(u4, x) & 0x7fff7fffu;
+        for (int x = 32; x; x >>= 1) m = pk_max_u16(m, (unsigned)__shfl_xor((int)m, x));
+        const unsigned c = (m & 0xffffu) > (m >> 16) ? m & 0xffffu : m >> 16;
+        if (at >= 0) {
+            if (lane == 0) ((unsigned short*)(p.consts + at))[kv] = (unsigned short)c;
+            // codes: 16 bytes of a tile to a lane at a time
+            const float fac = code_factor(f16_bits_to_float((unsigned short)c));
+            int8_t* const dst = p.codes + at * (2ll * KV_BLOCK * dpad) + (long long)kv * KV_BLOCK * dpad;
+            const int hh = lane >> 5, r = lane & 31;
+            for (int g = 0; g < dpad / 32; g++) {
+                unsigned o[4];
+                if (kv == 0) {
+                    const us8* src = (const us8*)(T + r * LD + 32 * g + 16 * hh);
+                    const us8 x = src[0], y = src[1];
 #pragma unroll
-            for (int q = 0; q < 4; q++) m[kv] = pk_max_u16(m[kv], y[q]);
-            if (keep && lo + r >= from) {
-                unsigned short* dst = kv_ring_row(p, s.slot, head, kv, lo + r);
-                if (VEC) {
-                    if (8 * u < d) *(us8*)(dst + 8 * u) = x;
+                    for (int j = 0; j < 4; j++) {
+                        const us8& z = j < 2 ? x : y;
+                        const int k = 4 * (j & 1);
+                        o[j] = pack_low_bytes(code_bits(z[k], fac), code_bits(z[k + 1], fac), code_bits(z[k + 2], fac), code_bits(z[k + 3], fac));
+                    }
                 } else {
+                    const unsigned short* src = T + 32 * g + r;
 #pragma unroll
-                    for (int q = 0; q < 8; q++)
-                        if (8 * u + q < d) dst[8 * u + q] = x[q];
+                    for (int j = 0; j < 4; j++) {
+                        const unsigned short* z = src + (8 * j + 4 * hh) * LD;
+                        o[j] = pack_low_bytes(code_bits(z[0], fac), code_bits(z[LD], fac), code_bits(z[2 * LD], fac), code_bits(z[3 * LD], fac));
+                    }
                 }
+                *(u4*)(dst + (g * 64 + lane) * 16) = u4{o[0], o[1], o[2], o[3]};
             }
         }
-#pragma unroll
-    for (int kv = 0; kv < 2; kv++) {
-#pragma unroll
-        for (int x = 32; x; x >>= 1) m[kv] = pk_max_u16(m[kv], (unsigned)__shfl_xor((int)m[kv], x));
-        if (lane == 0) s_max[kv][w] = m[kv];
+        __builtin_amdgcn_wave_barrier();
     }
-    __syncthreads();
-    if (at < 0) return;
-    unsigned c[2];
-#pragma unroll
-    for (int kv = 0; kv < 2; kv++) {
-        unsigned x = s_max[kv][0];
-        for (int q = 1; q < 4; q++) x = pk_max_u16(x, s_max[kv][q]);
-        c[kv] = (x & 0xffffu) > (x >> 16) ? x & 0xffffu : x >> 16;
-    }
-    if (tid == 0) p.consts[at] = c[0] | (c[1] << 16);
-    // ---- codes: 16 bytes of a tile to a thread
-    int8_t* const dst = p.codes + at * (2ll * KV_BLOCK * dpad);
-    const int pieces = dpad * 2;  // of 16 bytes, keys or values
-    for (int t = tid; t < 2 * pieces; t += 256) {
-        const int kv = t >= pieces, q = t - kv * pieces, g = q >> 6, l = q & 63, hh = l >> 5, r = l & 31;
-        const float fac = code_factor(f16_bits_to_float((unsigned short)c[kv]));
-        unsigned o[4];
-        if (kv == 0) {
-            const us8* src = (const us8*)(L[0] + r * LD + 32 * g + 16 * hh);
-            const us8 x = src[0], y = src[1];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const us8& z = j < 2 ? x : y;
-                const int k = 4 * (j & 1);
-                o[j] = pack_low_bytes(code_bits(z[k], fac), code_bits(z[k + 1], fac), code_bits(z[k + 2], fac), code_bits(z[k + 3], fac));
-            }
-        } else {
-            const unsigned short* src = L[1] + 32 * g + r;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const unsigned short* z = src + (8 * j + 4 * hh) * LD;
-                o[j] = pack_low_bytes(code_bits(z[0], fac), code_bits(z[LD], fac), code_bits(z[2 * LD], fac), code_bits(z[3 * LD], fac));
-            }
-        }
-        *(u4*)(dst + (long long)kv * KV_BLOCK * dpad + q * 16) = u4{o[0], o[1], o[2], o[3]};
-    }
+    if (bad) kv_flag(p, LLMINT8_KV_NOT_FINITE);
+    if (at < 0 && lane == 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
 }
 
 // c code / 127 for an integer n = c code that fp32 holds exactly: the correctly rounded fp32 quotient (reciprocal, and one
@@ -405,7 +382,7 @@ inline long long most_blocks(const Kv& p)
     return a < b ? a : b;
 }
 
-inline size_t block_lds(int d) { return 2ull * KV_BLOCK * (kv_dpad(d) + 8) * 2; }
+inline size_t block_lds(int d) { return (size_t)KV_BLOCK * (kv_dpad(d) + 8) * 2; }
 
 hipError_t launch_kv_append(const Kv& p, const KvAppend& c, hipStream_t st)
 {
@@ -416,22 +393,20 @@ hipError_t launch_kv_append(const Kv& p, const KvAppend& c, hipStream_t st)
     a.rot = {c.cos, c.sin, c.n_pos, c.rot / 2, c.pairs};
     const bool has_q = c.q && !(c.q == c.q_out && c.rot == 0);
     const int rows = p.max_rows < KV_BLOCK ? p.max_rows : KV_BLOCK;
-    // heads to a workgroup where a block's new rows are only moved: about four groups of 8 features to a thread
-    auto group = [&](int heads) {
-        const int g = 1024 / (rows * ((p.d + 7) / 8));
-        return g < 1 ? 1 : g > heads ? heads : g;
-    };
-    a.q_group = has_q ? group(c.heads_q) : 1, a.open_group = group(p.heads);
+    // query heads to a workgroup: about four groups of 8 features to a thread
+    const int g = 512 / (rows * ((p.d + 7) / 8));
+    a.q_group = g < 1 ? 1 : has_q && g > c.heads_q ? c.heads_q : g;
+    a.head_groups = (p.heads + HEADS - 1) / HEADS;
     const int qy = has_q ? (c.heads_q + a.q_group - 1) / a.q_group : 0;
     auto aligned = [](const void* q, long long ld) { return ((uintptr_t)q & 15) == 0 && ld % 8 == 0; };
     bool vec = p.d % 8 == 0 && aligned(c.k, c.ld_k) && aligned(c.v, c.ld_v);
     if (has_q) vec = vec && aligned(c.q, c.ld_q) && aligned(c.q_out, c.ld_q_out);
     if (c.rot) vec = vec && aligned(c.cos, 0) && aligned(c.sin, 0) && c.rot % (c.pairs ? 8 : 16) == 0;
-    const dim3 grid((unsigned)most_blocks(p), p.heads + qy);
+    const dim3 grid((unsigned)most_blocks(p), a.head_groups + qy);
     if (vec)
-        kv_append_kernel<true><<<grid, 256, block_lds(p.d), st>>>(a);
+        kv_append_kernel<true><<<grid, 64 * HEADS, HEADS * block_lds(p.d), st>>>(a);
     else
-        kv_append_kernel<false><<<grid, 256, block_lds(p.d), st>>>(a);
+        kv_append_kernel<false><<<grid, 64 * HEADS, HEADS * block_lds(p.d), st>>>(a);
     return hipGetLastError();
 }
 
@@ -440,9 +415,9 @@ hipError_t launch_kv_read(const Kv& p, void* k_out, void* v_out, hipStream_t st)
     const dim3 grid((unsigned)most_blocks(p), p.heads);
     const bool vec = p.d % 8 == 0 && (((uintptr_t)k_out | (uintptr_t)v_out) & 15) == 0;
     if (vec)
-        kv_read_kernel<true><<<grid, 256, block_lds(p.d) / 2, st>>>(p, (unsigned short*)k_out, (unsigned short*)v_out);
+        kv_read_kernel<true><<<grid, 256, block_lds(p.d), st>>>(p, (unsigned short*)k_out, (unsigned short*)v_out);
     else
-        kv_read_kernel<false><<<grid, 256, block_lds(p.d) / 2, st>>>(p, (unsigned short*)k_out, (unsigned short*)v_out);
+        kv_read_kernel<false><<<grid, 256, block_lds(p.d), st>>>(p, (unsigned short*)k_out, (unsigned short*)v_out);
     return hipGetLastError();
 }
 
