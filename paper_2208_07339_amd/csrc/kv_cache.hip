@@ -142,6 +142,15 @@ __device__ __forceinline__ unsigned larger(unsigned m, unsigned short v) { retur
 // holds f's old rows: then the wave of f writes c's rows there, when it has read the old ones.
 // LDS rows are 16 bytes longer than their data, so that the 16-byte reads of 32 rows at one feature spread over the banks.
 constexpr int HEADS = 2;
+
+// Between a wave's accesses to memory that its lanes share: they are done in order, and so they are to be compiled.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 template <bool VEC>
 __global__ void __launch_bounds__(64 * HEADS) kv_append_kernel(const AppendArgs a)
 {
@@ -229,8 +238,8 @@ __global__ void __launch_bounds__(64 * HEADS) kv_append_kernel(const AppendArgs 
                                  put(T + (from - lo + r) * LD + j, v);
                                  if (keep) put(kv_ring_row(p, s.slot, head, kv, from + r) + j, v);
                              }, bad);
+        wave_order();
         if (blk == f && clash >= 0) to_ring(clash, kv);
-        __builtin_amdgcn_wave_barrier();  // (a wave's accesses to LDS are in order)
 #pragma unroll
         for (int x = 32; x; x >>= 1) m = pk_max_u16(m, (unsigned)__shfl_xor((int)m, x));
         const unsigned c = (m & 0xffffu) > (m >> 16) ? m & 0xffffu : m >> 16;
@@ -262,7 +271,7 @@ __global__ void __launch_bounds__(64 * HEADS) kv_append_kernel(const AppendArgs 
                 *(u4*)(dst + (g * 64 + lane) * 16) = u4{o[0], o[1], o[2], o[3]};
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
     }
     if (bad) kv_flag(p, LLMINT8_KV_NOT_FINITE);
     if (at < 0 && lane == 0) kv_flag(p, LLMINT8_KV_BAD_PAGE);
