@@ -253,14 +253,16 @@ int llmint8_zp_linear(const void *X_f16, int s, int h, float alpha, const int8_t
  * blocks that both have.
  *
  * A batch says which rows of a call belong to which sequence, and where these are in the cache:
- *   row_start [n_seqs + 1]  sequence b has rows row_start[b] .. row_start[b+1] - 1 (none is allowed)
+ *   row_start [n_seqs + 1]  sequence b has rows row_start[b] .. row_start[b+1] - 1 (none is allowed).  Outputs of rows that are
+ *                           no sequence's are not specified
  *   kv_len    [n_seqs]      its positions, those of the call's own tokens included: row i of its n is at position
  *                           kv_len[b] - n + i.  0: the sequence is idle (append: its rows are left out)
  *   pages     [n_seqs][page_stride]  its pages in order; entries past its length are not read
  *   slots     [n_seqs]      its slot of the ring, one of its own; NULL: b
  *   status    one word, or NULL: bits are set (never cleared) where the arrays hold what cannot be, which only the
  *             device sees: LLMINT8_KV_BAD_BATCH for row_start, kv_len or slots out of range (or beyond max_rows, max_len, the
- *             table's width, the rotation's table; append: fewer positions than rows): the sequence is left out, outputs zero;
+ *             table's width, the rotation's table; append: fewer positions than rows): the sequence is left out.  Attention and
+ *             read give zeros for its rows, if row_start and max_rows allow that it has such; append leaves its q_out alone;
  *             LLMINT8_KV_BAD_PAGE for a page that does not exist: its positions are left out;
  *             LLMINT8_KV_NOT_FINITE: a key or value was infinite or NaN, or became so by its rotation.  The cache holds
  *             +-65504, or 0 for NaN, in its place, so that no other row's result is touched.
@@ -302,9 +304,9 @@ int llmint8_kv_append(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t 
 
 /* out row of query head g = sum_j w_j v_j, w = softmax over j of scale * q . k_j, with the keys and values of head
  * g / (heads_q / heads) at the positions j that the row sees: causal != 0: j up to its own position, else all kv_len; window > 0
- * (causal only): no j further back than window - 1 before its own.  A row that sees nothing (kv_len smaller than its
- * sequence's rows, an idle sequence) is zero.  scale >= 0.  Sums, maxima and weights are fp32; weights are rounded to fp16 for the
- * matrix units, the result once to fp16.
+ * (causal only): no j further back than window - 1 before its own.  A row that sees nothing (an idle sequence's, or a causal
+ * one at a position before 0, where kv_len is smaller than its sequence's rows) is zero.  scale >= 0, finite.  Sums, maxima and
+ * weights are fp32; weights are rounded to fp16 for the matrix units, the result once to fp16.
  *   q    in   fp16, row r and head g at r * ld_q + g * d;  heads_q a multiple of the cache's heads
  *   out  out  fp16, the same with ld_out
  *   ws        llmint8_kv_attention_workspace_bytes(batch, heads_q, heads, d) bytes; may be NULL where that is 0              */

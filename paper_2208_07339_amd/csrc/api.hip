@@ -619,7 +619,7 @@ int llmint8_kv_append(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t*
 size_t llmint8_kv_attention_workspace_bytes(const llmint8_kv_batch_t* batch, int heads_q, int heads, int d)
 {
     if (!batch || batch->n_seqs < 1 || batch->n_rows < 1 || batch->max_rows < 1 || batch->max_len < 0 || heads < 1 || heads_q < heads ||
-        heads_q % heads || d < 1 || d > KV_MAX_D)
+        heads_q % heads || d < 1 || d > KV_MAX_D || batch->max_len > KV_MAX_LEN / 4)
         return 0;
     Kv p = {};
     p.heads = heads, p.d = d, p.n_seqs = batch->n_seqs, p.n_rows = batch->n_rows, p.max_len = batch->max_len;

@@ -4,13 +4,16 @@
 // a row sees, l = sum exp(x_j - m):  out = sum_j w_j c_v / 127 v_j.  One pass over the positions.  The values' constants go into the
 // exponents: with y_j = x_j + log c_v the weight that is multiplied by a code is p_j = exp(y_j - M), M the running maximum of y, so
 // that fp16 weights have their full precision where they count whatever the values' size, and a block's share of l is
-// (sum p_j) / c_v.  What has been summed is scaled by exp(M_old - M_new) when M has to grow, which it does only by more than
-// 2^GROW: until then weights up to 2^GROW are as good.  Exponentials are to base 2, log2(e) being in the scale.
+// (sum p_j) / c_v.  What has been summed is scaled by exp(M_old - M_new) when M has to grow, which it need not do until weights
+// get larger than some power of two (GROW, LIMIT): up to it they are as good.  Exponentials are to base 2, log2(e) being in the scale.
 //
 // Both products are fp16 MFMAs (32 x 32 x 16) with fp32 sums.  Codes are exact in fp16: 0x6400 + u is the fp16 number 1024 + u, so a
 // byte permutation and a packed subtraction make two values of two codes.  Rows of queries are the N side of both products, S^T = K
-// Q^T and O^T = V^T P^T: a lane has one row of queries, so maximum, sum and scaling need one exchange between the lane's two halves,
+// Q^T and O^T = V^T P^T: a lane has one row of queries, so maximum, sum and scaling need one exchange between the wave's two halves,
 // and the scores a lane has computed are the operand of the second product as they are (kv.h).
+//
+// Roundings: a weight to fp16 (relative 2^-11, or 2^-25 of the largest), which is the operand's type and as fine as the result; l is
+// summed from the fp32 weights; the fp16 values of the open block to fp16 once more, scaled by a power of two.  All sums are fp32.
 #include "kv.h"
 
 namespace llmint8 {
@@ -185,7 +188,12 @@ __device__ __forceinline__ float open_unit(unsigned largest)
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
-// every wave blocks of its own; sums meet in LDS.  Bound by HBM.
+// every wave blocks of its own; sums meet in LDS.  Bound by HBM: 1 byte a cached number, about 4 operations to it for each row,
+// which the matrix units have to spare even where only one of a tile's 32 rows is there.  Each wave has two blocks on their way (of
+// d = 128: 8 KiB each, 32 MiB on the chip).  Two sequences of 100 003 and 131 071 positions, 64 heads over 8 of 128, one row each:
+// 473 MB in 82 us, 5.8 TB/s (a kernel that only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us,
+// 5.0 TB/s; the longest sequences end last.  Short ones are latency, from the page table to the codes to the sum of the four waves:
+// 6.5 us for 75 positions of 12 heads of 64.
 // ---------------------------------------------------------------------------------------------------------------------------
 constexpr int JOIN_FLOATS = 32 * 36;  // for a wave's sums in LDS: 32 rows of 32 features, or fewer of more
 
@@ -428,8 +436,12 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 // ---------------------------------------------------------------------------------------------------------------------------
 // Many rows: a workgroup takes a tile of 32 rows a wave (tokens, and for each the query heads that share its keys), its waves the
 // same blocks of the cache two at a time (a stage) from LDS, where the codes lie as fp16 in operand order: they are converted once
-// for all rows.  Bound by the matrix units and by what makes scores weights, which are kept busy at the same time: the scores of the
-// next block are computed while the weights of this one are.  So LDS holds keys one block ahead of values.
+// for all rows.  Bound by the matrix units, by what makes scores weights and by the reads of LDS, each about half of the time and
+// kept busy at the same time: the scores of the next block are computed while the weights of this one are.  So LDS holds keys one
+// block ahead of values.  (Operands of 64 rows a wave halve the reads, but leave one wave to a SIMD, which then issues vector
+// instructions half as often: no faster.)  8 192 tokens of 40 heads of 128, each seeing those before it: 680 us, 1.01 PFLOP/s of
+// what they see; a matrix product of 16 384 x 16 384 x 16 384 by the library reaches 1.32.  1 024 tokens behind 20 011, 32 heads over
+// 8: 336 us with the join, 1.02 PFLOP/s.  2 048 tokens of 32 heads: 57 us, 0.60; the last tile's 64 blocks are its time.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <int DP, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
@@ -815,7 +827,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     }
 }
 
-// Joins the splits, many of them: four waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the
+// Joins the splits, many of them (latency, 4.3 us for 40 rows of 12 parts): four waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the
 // splits dealt out over the waves and their quarters, four in flight each.  A part that had nothing to do has l = 0, and its sums
 // were not written.
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
@@ -894,7 +906,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
         }
 }
 
-// The same for up to eight: a thread to four features of a row and head.
+// The same for up to eight: a thread to four features of a row and head (HBM: 1 024 rows of 32 heads in two parts, 9 us).
 constexpr int FEW = 8;
 __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
 {
@@ -1008,7 +1020,8 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
 {
     AttendArgs a;
     a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
-    a.group = Div(c.heads_q / p.heads), a.heads = Div(p.heads), a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window, a.splits = Div(plan.splits), a.tiles = Div(plan.tiles < 1 ? 1 : plan.tiles);
+    a.group = Div(c.heads_q / p.heads), a.heads = Div(p.heads), a.splits = Div(plan.splits), a.tiles = Div(plan.tiles < 1 ? 1 : plan.tiles);
+    a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window;
     const size_t total = (size_t)p.n_rows * c.heads_q;
     a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));
     a.vec = p.d % 8 == 0 && ((((uintptr_t)c.q | (uintptr_t)c.out) & 15) | (c.ld_q & 7) | (c.ld_out & 7)) == 0;
