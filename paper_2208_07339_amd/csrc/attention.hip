@@ -827,9 +827,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     }
 }
 
-// Joins the splits, many of them (latency, 4.3 us for 40 rows of 12 parts): four waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the
+// Joins the splits, many of them: four waves to a row and head, 16 lanes x 4 features (as many times as d has them) to a split, the
 // splits dealt out over the waves and their quarters, four in flight each.  A part that had nothing to do has l = 0, and its sums
-// were not written.
+// were not written.  Latency: 4.8 us for 128 rows and heads in 32 parts.
 __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
 {
     const int splits = (int)a.splits.d;
@@ -906,8 +906,10 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const AttendArgs a)
         }
 }
 
-// The same for up to eight: a thread to four features of a row and head (HBM: 1 024 rows of 32 heads in two parts, 9 us).
-constexpr int FEW = 8;
+// The same for at most N: a thread to four features of a row and head, everything requested at once (40 rows and heads in 12 parts:
+// 3.9 us against 4.2, 1 920 in 10: 4.7 against 10).  HBM where rows are many: 1 024 rows of 32 heads in two parts, 9.3 us (12.7 where N is
+// 16).
+template <int N>
 __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
 {
     const int splits = (int)a.splits.d;
@@ -915,10 +917,10 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
     const long long total = (long long)a.kv.n_rows * a.heads_q, t = (long long)blockIdx.x * 256 + threadIdx.x, x = t / quads;
     if (x >= total) return;
     const int f0 = 4 * (int)(t - x * quads);
-    float2 st[FEW];
-    f4 v[FEW];
+    float2 st[N];
+    f4 v[N];
 #pragma unroll
-    for (int s = 0; s < FEW; s++) {
+    for (int s = 0; s < N; s++) {
         st[s] = s < splits ? a.stat[s * total + x] : make_float2(LOWEST, 0.0f);
         v[s] = f4{};
         if (s < splits) {
@@ -934,11 +936,11 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
     }
     float top = LOWEST, den = 0.0f;
 #pragma unroll
-    for (int s = 0; s < FEW; s++)
+    for (int s = 0; s < N; s++)
         if (st[s].y != 0.0f) top = fmaxf(top, st[s].x);
     f4 sum = {};
 #pragma unroll
-    for (int s = 0; s < FEW; s++)
+    for (int s = 0; s < N; s++)
         if (st[s].y != 0.0f) {
             const float f = exp2_(st[s].x - top);
             den += f * st[s].y;
@@ -1044,10 +1046,13 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
         default: e = pick(std::integral_constant<int, 256>()); break;
     }
     if (e != hipSuccess || plan.splits == 1) return e;
-    if (plan.splits > FEW)
+    const unsigned quads = (unsigned)((total * ((p.d + 3) / 4) + 255) / 256);
+    if (plan.splits > 16)
         kv_join_kernel<<<(unsigned)total, 256, 0, st>>>(a);
+    else if (plan.splits > 4)
+        kv_join_few_kernel<16><<<quads, 256, 0, st>>>(a);
     else
-        kv_join_few_kernel<<<(unsigned)((total * ((p.d + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
+        kv_join_few_kernel<4><<<quads, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
