@@ -190,8 +190,8 @@ __device__ __forceinline__ float open_unit(unsigned largest)
 // Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
 // every wave blocks of its own; sums meet in LDS.  Bound by HBM: 1 byte a cached number, about 4 operations to it for each row,
 // which the matrix units have to spare even where only one of a tile's 32 rows is there.  Each wave has two blocks on their way (of
-// d = 128: 8 KiB each, 32 MiB on the chip).  Two sequences of 100 003 and 131 071 positions, 64 heads over 8 of 128, one row each:
-// 473 MB in 82 us, 5.8 TB/s (a kernel that only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us,
+// d = 128: 8 KiB each, 32 MiB on the chip).  Two sequences of 257 000 positions together, 64 heads over 8 of 128, one row each: 527 MB
+// in 82 us, 6.4 TB/s (a kernel that only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us,
 // 5.0 TB/s; the longest sequences end last.  Short ones are latency, from the page table to the codes to the sum of the four waves:
 // 6.5 us for 75 positions of 12 heads of 64.
 // ---------------------------------------------------------------------------------------------------------------------------
