@@ -624,7 +624,7 @@ size_t llmint8_kv_attention_workspace_bytes(const llmint8_kv_batch_t* batch, int
     Kv p = {};
     p.heads = heads, p.d = d, p.n_seqs = batch->n_seqs, p.n_rows = batch->n_rows, p.max_len = batch->max_len;
     p.max_rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
-    return kv_attention_ws(kv_plan(p, heads_q), p.n_rows, heads_q, d);
+    return kv_attention_ws(kv_plan(p, heads_q, 0), p.n_rows, heads_q, d);
 }
 
 int llmint8_kv_attention(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* batch, const void* q_f16, int64_t ld_q,
@@ -639,7 +639,12 @@ int llmint8_kv_attention(const llmint8_kv_cache_t* cache, const llmint8_kv_batch
     if (ld_q < (int64_t)heads_q * cache->d || ld_out < (int64_t)heads_q * cache->d) return LLMINT8_INVALID_ARG;
     if ((int64_t)heads_q * batch->n_rows > KV_MAX_LEN || (int64_t)cache->heads * batch->n_seqs > KV_MAX_LEN) return LLMINT8_SHAPE;
     const Kv p = kv_args(cache, batch);
-    const KvPlan plan = kv_plan(p, heads_q);
+    KvPlan plan = kv_plan(p, heads_q, 0);
+    if (window) {  // the workspace's size is that without one
+        const int most = plan.splits;
+        plan = kv_plan(p, heads_q, window);
+        if (plan.splits > most) plan.splits = most;
+    }
     const size_t need = kv_attention_ws(plan, p.n_rows, heads_q, p.d);
     if (need && (!ws || ws_bytes < need)) return LLMINT8_WORKSPACE;
     KvAttend a = {q_f16, out_f16, ld_q, ld_out, heads_q, scale, causal != 0, window};

@@ -982,33 +982,49 @@ hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 
 constexpr int KV_STEP_ROWS = 32;
 
-KvPlan kv_plan(const Kv& p, int heads_q)
+KvPlan kv_plan(const Kv& p, int heads_q, int window)
 {
     KvPlan r;
     const long long group = heads_q / p.heads, rows = p.max_rows * group, all = p.n_rows * group;
-    const int blocks = (p.max_len + KV_BLOCK - 1) / KV_BLOCK;
     const bool wide = kv_dpad(p.d) > 128;
     auto tiles = [&](long long t) {  // of t rows, that all sequences have together, at most
         const long long x = (all + p.n_seqs * (t - 1)) / t, y = p.n_seqs * ((rows + t - 1) / t);
         return x < y ? x : y;
     };
+    auto seen = [&](long long t) {  // blocks that a tile of t rows sees, at most
+        const long long in = (p.max_len + KV_BLOCK - 1) / KV_BLOCK, w = (window + (t + group - 1) / group + 2 * (KV_BLOCK - 1)) / KV_BLOCK;
+        return (int)(window && w < in ? w : in);
+    };
     // The step kernel takes what it has registers for, and more rows where the cache's blocks and the row tiles are few: it reads and
     // converts a block once for every 32 rows, but starts and ends in a third of the time (five tokens of 48 heads that share keys,
     // eight sequences of 1 000 to 9 000 positions: 30 us against 42; 2 048 rows of 32 heads: 95 against 61).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
-    long long units;
+    int blocks = seen(KV_STEP_ROWS);
     if (rows <= KV_STEP_ROWS || few * blocks <= 24576) {
+        // One workgroup to a compute unit: two to each read no faster and have more to join (one row over 4 000 positions of 32 heads
+        // in 8 parts 11.8 us, in 16 13.4; 40 over 16 000 of 8 in 16 parts 19.3, in 32 22.8).  Sequences may differ in length, so
+        // that parts of some end early: there, twice as many (the eight above in 3 parts 33 us, in 7 25).
         r.tile = KV_STEP_ROWS, r.tiles = (int)((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS);
-        units = few;
+        const long long want = (p.n_seqs > 1 ? 512 : 256) / few, most = (blocks + 7) / 8;
+        r.splits = (int)(want < most ? want : most);
     } else {
         // 256 rows convert a block half as often as two times 128, but are one workgroup to a compute unit, whose start and end nothing
         // covers (2 048 positions: 70 us against 61; 8 192: 787 against 820)
-        r.tile = blocks >= 128 && rows > 128 && !wide ? 256 : 128;
-        units = (r.tiles = (int)tiles(r.tile)) * p.heads;
+        r.tile = seen(128) >= 128 && rows > 128 && !wide ? 256 : 128;
+        blocks = seen(r.tile);
+        r.tiles = (int)tiles(r.tile);
+        // Parts, one round of the chip at most: a workgroup's blocks one after the other (0.75 us each, 1.05 with two waves to a SIMD)
+        // against what the join reads and writes (1 024 rows of 32 heads over themselves in one part 29 us, in two 41; behind 20 011
+        // others 690 in one by that, 337 in two).
+        const int units = r.tiles * p.heads, want = (r.tile == 256 ? 256 : 512) / units, most = (blocks + 7) / 8;
+        const float join = (float)p.n_rows * heads_q * p.d * (8 / 4.5e6f);
+        float least = 0;
+        r.splits = 1;
+        for (int x = 1; x <= want && x <= most; x++) {
+            const float t = (r.tile == 256 || units * x > 256 ? 1.05f : 0.75f) * blocks / x + (x > 1 ? 5 + x * join : 0);
+            if (x == 1 || t < least) least = t, r.splits = x;
+        }
     }
-    // one round of the chip, two workgroups to a compute unit if they have at most four waves
-    const long long want = (r.tile == 256 ? 256 : 512) / units, most = (blocks + 7) / 8;
-    r.splits = (int)(want < most ? want : most);
     if (r.splits < 1) r.splits = 1;
     return r;
 }

@@ -162,7 +162,7 @@ struct KvPlan {
     int tiles;   // tiles that a sequence has at most (tile = KV_STEP_ROWS), or that all have together
     int splits;  // parts of the positions, joined by a kernel of their own if more than one
 };
-KvPlan kv_plan(const Kv& p, int heads_q);
+KvPlan kv_plan(const Kv& p, int heads_q, int window);  // window 0: none
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d);
 hipError_t launch_kv_attention(const Kv& p, const KvAttend& a, const KvPlan& plan, void* ws, hipStream_t st);
 
