@@ -443,15 +443,20 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 // what they see; a matrix product of 16 384 x 16 384 x 16 384 by the library reaches 1.32.  1 024 tokens behind 20 011, 32 heads over
 // 8: 336 us with the join, 1.02 PFLOP/s.  2 048 tokens of 32 heads: 57 us, 0.60; the last tile's 64 blocks are its time.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
+//
+// PARTS 2: two such groups of waves to a workgroup and tile, each with half of its blocks and an LDS of its own; the second's sums go to
+// the first through LDS.  They meet at the same barriers, so both go through the first's number of stages (which has not fewer).
+template <int DP, int WAVES, int PARTS>
+__global__ void __launch_bounds__(64 * WAVES * PARTS, WAVES * PARTS == 4 && DP <= 128 ? 2 : 1) kv_prompt_kernel(const AttendArgs a)
 {
     constexpr int NT = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int PIECES = DP * 4, PER = (PIECES + THREADS - 1) / THREADS;  // 16-byte pieces of two blocks' keys, or values; to a thread
-    extern __shared__ __align__(16) _Float16 lds[];                         // [keys, values][4 blocks][DP * 32]
+    extern __shared__ __align__(16) _Float16 all_lds[];                     // [PARTS][keys, values][4 blocks][DP * 32]
     __shared__ int s_big[WAVES];
     const Kv& p = a.kv;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
+    const int part = PARTS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+    const int tid = threadIdx.x - part * THREADS, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
+    _Float16* const lds = all_lds + part * 8 * DP * 32;
     // the heads of a tile one after the other: with a multiple of 8 heads, a head's tiles all run on one XCD and share its L2
     const int head = a.heads.rem(blockIdx.x), split = blockIdx.y, splits = (int)a.splits.d, G = (int)a.group.d;
     bool wrong = false;
@@ -469,14 +474,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     seen(a, s.len, old + a.group.quot(r0), lo, x1);
     seen(a, s.len, old + a.group.quot(r1 - 1), x0, hi);
     const int first = lo / KV_BLOCK, end = (hi + KV_BLOCK - 1) / KV_BLOCK;
-    const int chunk = chunk_of(end - first, splits, 2);
-    const int c0 = first + split * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;
+    const int chunk = chunk_of(end - first, splits * PARTS, 2);
+    const int g0 = first + split * PARTS * chunk, g1 = g0 + PARTS * chunk < end ? g0 + PARTS * chunk : end;  // the workgroup's blocks
+    const int c0 = g0 + part * chunk, c1 = c0 + chunk < end ? c0 + chunk : end;                              // this part's
     const int closed = s.len / KV_BLOCK, k1 = c1 < closed ? c1 : closed;
     // (an even number of stages, so that a stage's registers are known to the compiler; one that is not there has no weights)
-    const int stages = k1 > c0 ? (k1 - c0 + 3) / 4 * 2 : 0;
+    const int last = g0 + chunk < closed && g0 + chunk < end ? g0 + chunk : closed < end ? closed : end;  // of the first part
+    const int stages = last > g0 ? (last - g0 + 3) / 4 * 2 : 0;
     const long long total = (long long)p.n_rows * a.heads_q;
-    if (split && c0 >= c1) {  // nothing left for this part
-        for (int r = r0 + tid; r < r1; r += THREADS)
+    if (split && g0 >= g1) {  // nothing left
+        for (int r = r0 + (int)threadIdx.x; r < r1; r += THREADS * PARTS)
             a.stat[split * total + (s.row0 + a.group.quot(r)) * (long long)a.heads_q + head * G + a.group.rem(r)] = make_float2(LOWEST, 0.0f);
         return;
     }
@@ -666,38 +673,42 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
     };
 
     // ---- the open block, fp16 from the ring, before the others
-    if (closed >= c0 && closed < c1) {
+    if (closed >= g0 && closed < g1) {
+        const bool mine = closed >= c0 && closed < c1;
         const int d = p.d, pos0 = closed * KV_BLOCK;
         const unsigned short *const krows = kv_ring_row(p, s.slot, head, 0, pos0), *const vrows = kv_ring_row(p, s.slot, head, 1, pos0);
         int big = 0;
-        for (int t = tid; t < (s.len - pos0) * d; t += THREADS) {
-            const int y = vrows[t] & 0x7fff;
-            big = y > big ? y : big;
-        }
+        if (mine) {
+            for (int t = tid; t < (s.len - pos0) * d; t += THREADS) {
+                const int y = vrows[t] & 0x7fff;
+                big = y > big ? y : big;
+            }
 #pragma unroll
-        for (int x = 32; x; x >>= 1) {
-            const int y = __shfl_xor(big, x);
-            big = y > big ? y : big;
+            for (int x = 32; x; x >>= 1) {
+                const int y = __shfl_xor(big, x);
+                big = y > big ? y : big;
+            }
+            if (lane == 0) s_big[w] = big;
         }
-        if (lane == 0) s_big[w] = big;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < WAVES; x++) big = s_big[x] > big ? s_big[x] : big;
         const float unit = open_unit(big);
-        for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
-            const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
-            h8 y = {}, z = {};
-            if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
+        if (mine)
+            for (int t = tid; t < KV_BLOCK * DP / 8; t += THREADS) {  // eight of a lane's keys and values each
+                const int at = t >> 6, r = t & 31, h = (t >> 5) & 1, f = 32 * (at >> 1) + r;
+                h8 y = {}, z = {};
+                if (pos0 + r < s.len) y = q8((const _Float16*)krows + r * d, 32 * (at >> 1) + 16 * h + 8 * (at & 1), d, d % 8 == 0);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
-                if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / unit));
+                for (int i = 0; i < 8; i++) {
+                    const int q = 16 * (at & 1) + 8 * (i >> 2) + 4 * h + (i & 3);
+                    if (pos0 + q < s.len && f < d) z[i] = (_Float16)(f16_bits_to_float(vrows[q * d + f]) * (1.0f / unit));
+                }
+                *((h8*)lds + t) = y;
+                *((h8*)(lds + 4 * DP * 32) + t) = z;
             }
-            *((h8*)lds + t) = y;
-            *((h8*)(lds + 4 * DP * 32) + t) = z;
-        }
         __syncthreads();
-        if (pos0 < some_hi) {
+        if (mine && pos0 < some_hi) {
             f16v sc;
             scores(0, sc);
             const Factors fa = factors(true, 1.0f, 127.0f * unit, a.scale);
@@ -781,6 +792,31 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 4 && DP <= 128 ? 2 : 1) k
         for (; st < stages; st += 2) idle(st, even), idle(st + 1, odd);
     }
 
+    if constexpr (PARTS == 2) {
+        f4* const sums = (f4*)all_lds + w * NT * 4 * 64 + lane;
+        float2* const stat = (float2*)((f4*)all_lds + WAVES * NT * 4 * 64) + w * 64 + lane;
+        __syncthreads();  // (the last stage's operands have been read)
+        if (part) {
+            *stat = make_float2(m, l);
+#pragma unroll
+            for (int q = 0; q < NT; q++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) sums[(q * 4 + j) * 64] = f4{o[q][4 * j], o[q][4 * j + 1], o[q][4 * j + 2], o[q][4 * j + 3]};
+        }
+        __syncthreads();
+        if (part) return;
+        const float2 t = *stat;
+        const float top = fmaxf(m, t.x), f = exp2_(m - top), g = exp2_(t.x - top);
+        m = top, l = l * f + t.y * g;
+#pragma unroll
+        for (int q = 0; q < NT; q++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const f4 y = sums[(q * 4 + j) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[q][4 * j + e] = o[q][4 * j + e] * f + y[e] * g;
+            }
+    }
     const float den = l + __shfl_xor(l, 32);
     const int r = w0 + qr;
     if (r >= r1) return;
@@ -966,15 +1002,15 @@ hipError_t launch_step(const AttendArgs& a, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DP, int WAVES>
+template <int DP, int WAVES, int PARTS>
 hipError_t launch_prompt(const AttendArgs& a, int tiles, hipStream_t st)
 {
-    constexpr int bytes = 8 * DP * 32 * 2;
+    constexpr int bytes = PARTS * 8 * DP * 32 * 2;
     if (bytes + 256 > 65536) {  // with the static part
-        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)kv_prompt_kernel<DP, WAVES, PARTS>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    kv_prompt_kernel<DP, WAVES><<<dim3(tiles * a.kv.heads, a.splits.d), 64 * WAVES, bytes, st>>>(a);
+    kv_prompt_kernel<DP, WAVES, PARTS><<<dim3(tiles * a.kv.heads, a.splits.d), 64 * WAVES * PARTS, bytes, st>>>(a);
     return hipGetLastError();
 }
 
@@ -984,7 +1020,7 @@ constexpr int KV_STEP_ROWS = 32;
 
 KvPlan kv_plan(const Kv& p, int heads_q, int window)
 {
-    KvPlan r;
+    KvPlan r = {};
     const long long group = heads_q / p.heads, rows = p.max_rows * group, all = p.n_rows * group;
     const bool wide = kv_dpad(p.d) > 128;
     auto tiles = [&](long long t) {  // of t rows, that all sequences have together, at most
@@ -1024,6 +1060,16 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
             const float t = (r.tile == 256 || units * x > 256 ? 1.05f : 0.75f) * blocks / x + (x > 1 ? 5 + x * join : 0);
             if (x == 1 || t < least) least = t, r.splits = x;
         }
+        // Two halves of a workgroup to a tile, each with half of its blocks: where tiles are few, the last ones, which see most, are the
+        // time.  One such workgroup to a compute unit, so at most two rounds, of which the second starts when the first's short
+        // ones end (rows over themselves, in halves and not: 4 096 of 8 heads 72 us and 77, of 16 97 and 116, 8 192 of 8 170 and 216, but
+        // 2 048 of 32 65 and 60).  mean: blocks that a tile sees on average.
+        const int pairs = (int)tiles(128) * p.heads, longest = seen(128);
+        if (!wide && pairs <= 512) {
+            const int mean = (p.max_len + KV_BLOCK - 1) / KV_BLOCK - p.max_rows / (2 * KV_BLOCK);
+            const float t = 0.58f * fmaxf((float)longest, pairs * (float)(mean < longest ? mean : longest) / 256);
+            if (t + (pairs > 256 ? 35 : 5) < least) r = {128, (int)tiles(128), 1, true};
+        }
     }
     if (r.splits < 1) r.splits = 1;
     return r;
@@ -1048,8 +1094,9 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
         return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st)
-               : plan.tile == 256        ? launch_prompt<(DP > 128 ? 128 : DP), 8>(a, plan.tiles, st)  // (never that for more)
-                                         : launch_prompt<DP, 4>(a, plan.tiles, st);
+               : plan.tile == 256        ? launch_prompt<(DP > 128 ? 128 : DP), 8, 1>(a, plan.tiles, st)  // (never that for more)
+               : plan.halves             ? launch_prompt<(DP > 128 ? 128 : DP), 4, 2>(a, plan.tiles, st)
+                                         : launch_prompt<DP, 4, 1>(a, plan.tiles, st);
     };
     switch (dp) {
         case 32: e = pick(std::integral_constant<int, 32>()); break;

@@ -161,6 +161,7 @@ struct KvPlan {
     int tile;    // rows (of all query heads that share keys) to a workgroup
     int tiles;   // tiles that a sequence has at most (tile = KV_STEP_ROWS), or that all have together
     int splits;  // parts of the positions, joined by a kernel of their own if more than one
+    bool halves;  // (tile = 128) a tile's blocks on two halves of a workgroup
 };
 KvPlan kv_plan(const Kv& p, int heads_q, int window);  // window 0: none
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d);

@@ -48,3 +48,27 @@ def test_captured_prompt_of_wide_heads():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
+
+
+@pytest.mark.parametrize("d", [32, 40, 64, 96, 128])
+@pytest.mark.parametrize("new, past, heads", [(1500, 0, 16), (1535, 0, 16), (1536, 0, 16), (900, 700, 24)])
+def test_tiles_of_two_halves(d, new, past, heads):
+    """Rows whose tiles' blocks two halves of a workgroup share: numbers of blocks of all remainders, windows, everything seen."""
+    rng = np.random.default_rng(d)
+    dev = Device(1, heads, d, page=128, most=new + past, seed=d)
+    if past:
+        dev.append([past], rng)
+    dev.append([new], rng)
+    dev.check_attention([new], rng)
+    if d == 64:
+        dev.check_attention([new], rng, window=700)
+        dev.check_attention([new], rng, causal=False)
+        dev.check_attention([new], rng, lengths=[new + past - 32])
+
+
+def test_two_halves_and_ragged_sequences():
+    rng = np.random.default_rng(8)
+    dev = Device(4, 16, 64, page=64, most=1600, seed=8)
+    dev.append([1500, 90, 33, 7], rng)
+    dev.check_attention([1400, 90, 20, 7], rng)
+    dev.check_attention([1400, 90, 20, 7], rng, idle=(1,))
