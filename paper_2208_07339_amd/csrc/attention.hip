@@ -1039,7 +1039,7 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     if (rows <= KV_STEP_ROWS || few * blocks <= 24576) {
         // One workgroup to a compute unit: two to each read no faster and have more to join (one row over 4 000 positions of 32 heads
         // in 8 parts 11.8 us, in 16 13.4; 40 over 16 000 of 8 in 16 parts 19.3, in 32 22.8).  Sequences may differ in length, so
-        // that parts of some end early: there, twice as many (the eight above in 3 parts 33 us, in 7 25).
+        // that parts of some end early: there, twice as many (the eight above in 4 parts 33 us, in 7 25).
         r.tile = KV_STEP_ROWS, r.tiles = (int)((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS);
         const long long want = (p.n_seqs > 1 ? 512 : 256) / few, most = (blocks + 7) / 8;
         r.splits = (int)(want < most ? want : most);
