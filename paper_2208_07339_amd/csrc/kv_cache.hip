@@ -70,19 +70,21 @@ __device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, b
                                           int thread, int threads, Out out, bool& bad)
 {
     const int nh = h1 - h0, half = turned ? rot.half : 0;
-    const int per = VEC ? (rot.pairs || !half ? d / 8 : half / 8 + (d - 2 * half) / 8) : half + (d - 2 * half);
-    const int total = n * nh * per;
+    // what is turned, and the rest: loops of their own, without branches, so that the requests of several turns go out together
+    auto all = [&](int per, auto body) {
+        const int total = n * nh * per;
 #pragma unroll 4
-    for (int t = thread; t < total; t += threads) {
-        const int rest = t / per, u = t - rest * per, i = nh == 1 ? rest : rest / nh, gh = rest - i * nh;
-        const unsigned short* src = in.p + (row + i) * in.ld + (long long)(h0 + gh) * d;
-        const float* c = rot.cos + (long long)(pos + i) * half;
-        const float* s = rot.sin + (long long)(pos + i) * half;
-        if constexpr (VEC) {
-            if (half && !rot.pairs && u < half / 8) {
+        for (int t = thread; t < total; t += threads) {
+            const int rest = t / per, u = t - rest * per, i = nh == 1 ? rest : rest / nh, gh = rest - i * nh;
+            body(i, h0 + gh, u, in.p + (row + i) * in.ld + (long long)(h0 + gh) * d, (long long)(pos + i) * half);
+        }
+    };
+    if constexpr (VEC) {
+        if (half && !rot.pairs)
+            all(half / 8, [&](int i, int g, int u, const unsigned short* src, long long at) {
                 us8 a = *(const us8*)(src + 8 * u), b = *(const us8*)(src + half + 8 * u);
-                const f4 cc[2] = {*(const f4*)(c + 8 * u), *(const f4*)(c + 8 * u + 4)};
-                const f4 ss[2] = {*(const f4*)(s + 8 * u), *(const f4*)(s + 8 * u + 4)};
+                const float *c = rot.cos + at + 8 * u, *s = rot.sin + at + 8 * u;
+                const f4 cc[2] = {*(const f4*)c, *(const f4*)(c + 4)}, ss[2] = {*(const f4*)s, *(const f4*)(s + 4)};
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     unsigned short x = a[e], y = b[e];
@@ -90,37 +92,44 @@ __device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, b
                     a[e] = x, b[e] = y;
                 }
                 if (FINITE) a = finite8(a, bad), b = finite8(b, bad);
-                out(i, h0 + gh, 8 * u, a);
-                out(i, h0 + gh, half + 8 * u, b);
-            } else {
-                const int f = 8 * (half && !rot.pairs ? u + half / 8 : u);
-                us8 a = *(const us8*)(src + f);
-                if (half && rot.pairs && f < 2 * half) {
-                    const f4 cc = *(const f4*)(c + f / 2), ss = *(const f4*)(s + f / 2);
+                out(i, g, 8 * u, a);
+                out(i, g, half + 8 * u, b);
+            });
+        if (half && rot.pairs)
+            all(half / 4, [&](int i, int g, int u, const unsigned short* src, long long at) {
+                us8 a = *(const us8*)(src + 8 * u);
+                const f4 cc = *(const f4*)(rot.cos + at + 4 * u), ss = *(const f4*)(rot.sin + at + 4 * u);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        unsigned short x = a[2 * e], y = a[2 * e + 1];
-                        turn(x, y, cc[e], ss[e]);
-                        a[2 * e] = x, a[2 * e + 1] = y;
-                    }
+                for (int e = 0; e < 4; e++) {
+                    unsigned short x = a[2 * e], y = a[2 * e + 1];
+                    turn(x, y, cc[e], ss[e]);
+                    a[2 * e] = x, a[2 * e + 1] = y;
                 }
                 if (FINITE) a = finite8(a, bad);
-                out(i, h0 + gh, f, a);
-            }
-        } else {
-            if (u < half) {
+                out(i, g, 8 * u, a);
+            });
+        if (d > 2 * half)
+            all((d - 2 * half) / 8, [&](int i, int g, int u, const unsigned short* src, long long) {
+                us8 a = *(const us8*)(src + 2 * half + 8 * u);
+                if (FINITE) a = finite8(a, bad);
+                out(i, g, 2 * half + 8 * u, a);
+            });
+    } else {
+        if (half)
+            all(half, [&](int i, int g, int u, const unsigned short* src, long long at) {
                 const int ja = rot.pairs ? 2 * u : u, jb = rot.pairs ? 2 * u + 1 : u + half;
                 unsigned short x = src[ja], y = src[jb];
-                turn(x, y, c[u], s[u]);
+                turn(x, y, rot.cos[at + u], rot.sin[at + u]);
                 if (FINITE) x = finite(x, bad), y = finite(y, bad);
-                out(i, h0 + gh, ja, x);
-                out(i, h0 + gh, jb, y);
-            } else {
-                unsigned short x = src[half + u];
+                out(i, g, ja, x);
+                out(i, g, jb, y);
+            });
+        if (d > 2 * half)
+            all(d - 2 * half, [&](int i, int g, int u, const unsigned short* src, long long) {
+                unsigned short x = src[2 * half + u];
                 if (FINITE) x = finite(x, bad);
-                out(i, h0 + gh, half + u, x);
-            }
-        }
+                out(i, g, 2 * half + u, x);
+            });
     }
 }
 
@@ -136,10 +145,10 @@ __device__ __forceinline__ unsigned larger(unsigned m, unsigned short v) { retur
 // One wave to a block that gets new tokens and a key/value head, HEADS waves to a workgroup (y < the heads' groups); the workgroups
 // behind take such a block's tokens and q_group query heads each.  A block that gets full: keys, then values, go through LDS, where
 // the codes are collected into tiles; their maximum is taken on the way.  The fp16 rows of the last two blocks go to the ring.
-// Bound by HBM: 8 192 tokens of 40 heads of 128 with their queries read 252 MB and write 168 in 111 us, 3.8 TB/s (a copy: 4.76).
+// Bound by HBM: 8 192 tokens of 40 heads of 128 with their queries read 252 MB and write 168 in 102 us, 4.1 TB/s (a copy: 4.76).
 // Single tokens are latency: 96 sequences of 40 heads 15 us, of which blocks that get full are the longest.  (A workgroup to a block
-// and head instead, its four waves meeting at barriers, took 134 and 18 us; a wave to the keys and one to the values of a block and
-// head 124 and 14.)
+// and head instead, its four waves meeting at barriers, took 134 and 18 us where this took 111 and 15, a wave to the keys and one to
+// the values of a block and head 124 and 14.)
 // A call that begins inside block f and ends more than a block later writes, for a later block c, the half of the ring that
 // holds f's old rows: then the wave of f writes c's rows there, when it has read the old ones.
 // LDS rows are 16 bytes longer than their data, so that the 16-byte reads of 32 rows at one feature spread over the banks.
@@ -405,8 +414,10 @@ hipError_t launch_kv_append(const Kv& p, const KvAppend& c, hipStream_t st)
     a.rot = {c.cos, c.sin, c.n_pos, c.rot / 2, c.pairs};
     const bool has_q = c.q && !(c.q == c.q_out && c.rot == 0);
     const int rows = p.max_rows < KV_BLOCK ? p.max_rows : KV_BLOCK;
-    // query heads to a workgroup: about four groups of 8 features to a thread
-    const int g = 512 / (rows * ((p.d + 7) / 8));
+    // query heads to a workgroup: about four groups of 8 features to a thread, or 16 where there are more than enough workgroups
+    // (17 550 tokens of 48 heads 155 and 138 us; eight times five tokens of 48 heads 4.1 and 8)
+    const int of4 = 512 / (rows * ((p.d + 7) / 8)), g4 = of4 < 1 ? 1 : of4;
+    const int g = has_q && most_blocks(p) * ((c.heads_q + g4 - 1) / g4) > 4096 ? 2048 / (rows * ((p.d + 7) / 8)) : g4;
     a.q_group = g < 1 ? 1 : has_q && g > c.heads_q ? c.heads_q : g;
     a.head_groups = (p.heads + HEADS - 1) / HEADS;
     const int qy = has_q ? (c.heads_q + a.q_group - 1) / a.q_group : 0;
