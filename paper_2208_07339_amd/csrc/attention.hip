@@ -45,7 +45,8 @@ __device__ __forceinline__ h8 pack8(const float* p)
     return r;
 }
 
-// What a block's scores and weights are taken by.  A block that is not there: weights of 0.
+// What a block's scores and weights are taken by.  A block that is not there: weights of 0, by finite factors and lcv alone, since
+// the constants that are read in its place may be anything, infinite ones too.
 struct Factors {
     float ks;   // of the scores; above 0, so that a masked -inf stays one
     float lcv;  // log2 of the values' constant.  A block of zeros counts as 2^-24, the smallest constant: its weights count in l
@@ -54,7 +55,7 @@ struct Factors {
 __device__ __forceinline__ Factors factors(bool there, float ck, float cv, float scale)
 {
     cv = fmaxf(cv, 0x1p-24f);
-    return {fmaxf(ck * scale, 1e-30f), there ? __builtin_amdgcn_logf(cv) : -__builtin_inff(), there ? 1.0f / cv : 0.0f};
+    return {there ? fmaxf(ck * scale, 1e-30f) : 1e-30f, there ? __builtin_amdgcn_logf(cv) : -__builtin_inff(), there ? 1.0f / cv : 0.0f};
 }
 __device__ __forceinline__ Factors factors(bool there, unsigned c, float scale)
 {
