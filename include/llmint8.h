@@ -374,6 +374,17 @@ int llmint8_debug_mfma_for(int s, int h, int o, int zeropoint);
  * coarser constants of llmint8_quantize_weight_granular always read it twice.  Without a GPU, the answer for 256 compute units. */
 int llmint8_debug_weight_reads_for(int h, int o, int zeropoint);
 
+/* Test/support: how llmint8_kv_attention cuts up a call of this batch's sizes: the rows (of all query heads that share keys) to a
+ * tile, 32 for the kernel for few rows or 128 or 256 of that for many; in how many parts the positions are, which are joined
+ * afterwards if there are more than one; whether a tile's blocks are on two halves of a workgroup; the workgroups that are
+ * launched.  LLMINT8_INVALID_ARG for sizes that llmint8_kv_attention_workspace_bytes refuses, or a window < 0.  Host arithmetic
+ * only: needs no GPU.                                                                          */
+typedef struct {
+    int tile, parts, halves;
+    int64_t workgroups;
+} llmint8_kv_plan_t;
+int llmint8_debug_kv_plan_for(const llmint8_kv_batch_t *batch, int heads_q, int heads, int d, int window, llmint8_kv_plan_t *plan);
+
 /* Test/support: private layouts -> plain row-major int8 ([h x o], [s x h]). */
 int llmint8_export_weight(const int8_t *Wq, int h, int o, int8_t *W_i8_rowmajor, llmint8_stream_t stream);
 int llmint8_export_rows(const int8_t *Xq, int s, int h, int8_t *X_i8_rowmajor, llmint8_stream_t stream);

@@ -12,6 +12,6 @@ from .binding import (  # noqa: F401
     debug_kernel_for, debug_mfma_for, debug_weight_reads_for, dequantize_rows,
     init, linear_static, STATIC_SCRATCH_BYTES, probe_mfma, probe_read,
     GRANULARITY, ZpWeight, ZpRows, zp_quantize_weight, zp_quantize_rows, zp_matmul, zp_linear,
-    KvCache, KvBatch, kv_append, kv_attention, kv_attention_workspace, kv_read,
+    KvCache, KvBatch, kv_append, kv_attention, kv_attention_workspace, kv_read, debug_kv_plan_for,
     KV_BLOCK, KV_RING, KV_MAX_D, KV_BAD_BATCH, KV_BAD_PAGE, KV_NOT_FINITE,
 )

@@ -19,7 +19,7 @@ SYMBOLS = [
     "llmint8_debug_decode_shape", "llmint8_debug_kernel_for", "llmint8_debug_mfma_for",
     "llmint8_debug_weight_reads_for",
     "llmint8_kv_codes_bytes", "llmint8_kv_consts_bytes", "llmint8_kv_ring_bytes", "llmint8_kv_append",
-    "llmint8_kv_attention_workspace_bytes", "llmint8_kv_attention", "llmint8_kv_read",
+    "llmint8_kv_attention_workspace_bytes", "llmint8_kv_attention", "llmint8_kv_read", "llmint8_debug_kv_plan_for",
 ]
 
 _lib = None
@@ -35,6 +35,10 @@ class _KvBatch(C.Structure):  # llmint8_kv_batch_t
     _fields_ = [("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("slots", C.c_void_p),
                 ("status", C.c_void_p), ("n_seqs", C.c_int), ("n_rows", C.c_int), ("page_stride", C.c_int),
                 ("max_rows", C.c_int), ("max_len", C.c_int)]
+
+
+class KvPlan(C.Structure):  # llmint8_kv_plan_t
+    _fields_ = [("tile", C.c_int), ("parts", C.c_int), ("halves", C.c_int), ("workgroups", C.c_int64)]
 
 
 class Llmint8Error(RuntimeError):
@@ -134,6 +138,8 @@ def lib():
     L.llmint8_kv_attention_workspace_bytes.argtypes = [batch, i32, i32, i32]
     L.llmint8_kv_attention.restype = i32
     L.llmint8_kv_attention.argtypes = [cache, batch, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp]
+    L.llmint8_debug_kv_plan_for.restype = i32
+    L.llmint8_debug_kv_plan_for.argtypes = [batch, i32, i32, i32, i32, C.POINTER(KvPlan)]
     L.llmint8_kv_read.restype = i32
     L.llmint8_kv_read.argtypes = [cache, batch, vp, vp, vp]
     _lib = L
@@ -580,6 +586,13 @@ def kv_attention(cache, batch, q, scale=None, causal=True, window=0, ws=None, ou
                                       d ** -0.5 if scale is None else scale, int(causal), window, _ptr(out),
                                       _head_rows(out, n, heads_q, d), _ptr(ws.buf), ws.nbytes, _stream()))
     return out
+
+
+def debug_kv_plan_for(cache, batch, heads_q, window=0):
+    """llmint8_debug_kv_plan_for: rows of a tile, parts, halves and workgroups of a call of kv_attention (no GPU needed)."""
+    p = KvPlan()
+    _check(lib().llmint8_debug_kv_plan_for(batch._c, heads_q, cache.heads, cache.d, window, p))
+    return p
 
 
 def kv_read(cache, batch, k=None, v=None):

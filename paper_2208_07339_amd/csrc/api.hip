@@ -577,6 +577,28 @@ int llmint8_export_rows(const int8_t* Xq, int s, int h, int8_t* X_i8_rowmajor, l
 
 // ---- 8-bit key/value cache ----
 
+// What a plan is made from; false: sizes that attention refuses
+static bool kv_sizes(const llmint8_kv_batch_t* b, int heads_q, int heads, int d, Kv& p)
+{
+    if (!b || b->n_seqs < 1 || b->n_rows < 1 || b->max_rows < 1 || b->max_len < 0 || heads < 1 || heads_q < heads || heads_q % heads || d < 1 ||
+        d > KV_MAX_D || b->max_len > KV_MAX_LEN / 4)
+        return false;
+    p = {};
+    p.heads = heads, p.d = d, p.n_seqs = b->n_seqs, p.n_rows = b->n_rows, p.max_len = b->max_len;
+    p.max_rows = b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
+    return true;
+}
+
+// The plan of a call: the workspace's size is that without a window
+static KvPlan kv_plan_within_ws(const Kv& p, int heads_q, int window)
+{
+    const KvPlan whole = kv_plan(p, heads_q, 0);
+    if (!window) return whole;
+    KvPlan r = kv_plan(p, heads_q, window);
+    if (r.splits > whole.splits) r.splits = whole.splits;
+    return r;
+}
+
 size_t llmint8_kv_codes_bytes(int n_pages, int page_tokens, int heads, int d)
 {
     if (n_pages < 1 || page_tokens < 1 || page_tokens % KV_BLOCK || heads < 1 || d < 1 || d > KV_MAX_D) return 0;
@@ -618,13 +640,18 @@ int llmint8_kv_append(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t*
 
 size_t llmint8_kv_attention_workspace_bytes(const llmint8_kv_batch_t* batch, int heads_q, int heads, int d)
 {
-    if (!batch || batch->n_seqs < 1 || batch->n_rows < 1 || batch->max_rows < 1 || batch->max_len < 0 || heads < 1 || heads_q < heads ||
-        heads_q % heads || d < 1 || d > KV_MAX_D || batch->max_len > KV_MAX_LEN / 4)
-        return 0;
-    Kv p = {};
-    p.heads = heads, p.d = d, p.n_seqs = batch->n_seqs, p.n_rows = batch->n_rows, p.max_len = batch->max_len;
-    p.max_rows = batch->max_rows < batch->n_rows ? batch->max_rows : batch->n_rows;
+    Kv p;
+    if (!kv_sizes(batch, heads_q, heads, d, p)) return 0;
     return kv_attention_ws(kv_plan(p, heads_q, 0), p.n_rows, heads_q, d);
+}
+
+int llmint8_debug_kv_plan_for(const llmint8_kv_batch_t* batch, int heads_q, int heads, int d, int window, llmint8_kv_plan_t* plan)
+{
+    Kv p;
+    if (!plan || window < 0 || !kv_sizes(batch, heads_q, heads, d, p)) return LLMINT8_INVALID_ARG;
+    const KvPlan r = kv_plan_within_ws(p, heads_q, window);
+    *plan = {r.tile, r.splits, r.halves, kv_attention_workgroups(p, r)};
+    return LLMINT8_OK;
 }
 
 int llmint8_kv_attention(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* batch, const void* q_f16, int64_t ld_q,
@@ -639,12 +666,7 @@ int llmint8_kv_attention(const llmint8_kv_cache_t* cache, const llmint8_kv_batch
     if (ld_q < (int64_t)heads_q * cache->d || ld_out < (int64_t)heads_q * cache->d) return LLMINT8_INVALID_ARG;
     if ((int64_t)heads_q * batch->n_rows > KV_MAX_LEN || (int64_t)cache->heads * batch->n_seqs > KV_MAX_LEN) return LLMINT8_SHAPE;
     const Kv p = kv_args(cache, batch);
-    KvPlan plan = kv_plan(p, heads_q, 0);
-    if (window) {  // the workspace's size is that without one
-        const int most = plan.splits;
-        plan = kv_plan(p, heads_q, window);
-        if (plan.splits > most) plan.splits = most;
-    }
+    const KvPlan plan = kv_plan_within_ws(p, heads_q, window);
     const size_t need = kv_attention_ws(plan, p.n_rows, heads_q, p.d);
     if (need && (!ws || ws_bytes < need)) return LLMINT8_WORKSPACE;
     KvAttend a = {q_f16, out_f16, ld_q, ld_out, heads_q, scale, causal != 0, window};

@@ -996,10 +996,9 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
 }
 
 template <int DP>
-hipError_t launch_step(const AttendArgs& a, hipStream_t st)
+hipError_t launch_step(const AttendArgs& a, const KvPlan& plan, hipStream_t st)
 {
-    const long long units = (long long)a.kv.heads * a.kv.n_seqs * a.splits.d;
-    kv_step_kernel<DP><<<(unsigned)((units + 7) / 8 * 8 * a.tiles.d), 256, 0, st>>>(a);
+    kv_step_kernel<DP><<<(unsigned)kv_attention_workgroups(a.kv, plan), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -1076,6 +1075,13 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     return r;
 }
 
+long long kv_attention_workgroups(const Kv& p, const KvPlan& plan)
+{
+    // (the step kernel: parts of sequences and heads in eights, for the XCDs, with the tiles that a sequence has at most)
+    if (plan.tile == KV_STEP_ROWS) return ((long long)p.heads * p.n_seqs * plan.splits + 7) / 8 * 8 * plan.tiles;
+    return (long long)plan.tiles * p.heads * plan.splits;
+}
+
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d)
 {
     return plan.splits > 1 ? (size_t)plan.splits * n_rows * heads_q * (4 * (size_t)d + 8) + 512 : 0;
@@ -1094,7 +1100,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     hipError_t e;
     auto pick = [&](auto w) {
         constexpr int DP = decltype(w)::value;
-        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, st)
+        return plan.tile == KV_STEP_ROWS ? launch_step<DP>(a, plan, st)
                : plan.tile == 256        ? launch_prompt<(DP > 128 ? 128 : DP), 8, 1>(a, plan.tiles, st)  // (never that for more)
                : plan.halves             ? launch_prompt<(DP > 128 ? 128 : DP), 4, 2>(a, plan.tiles, st)
                                          : launch_prompt<DP, 4, 1>(a, plan.tiles, st);

@@ -165,6 +165,7 @@ struct KvPlan {
 };
 KvPlan kv_plan(const Kv& p, int heads_q, int window);  // window 0: none
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d);
+long long kv_attention_workgroups(const Kv& p, const KvPlan& plan);  // without those of a join
 hipError_t launch_kv_attention(const Kv& p, const KvAttend& a, const KvPlan& plan, void* ws, hipStream_t st);
 
 }  // namespace llmint8

@@ -1,0 +1,67 @@
+"""How kv_attention cuts calls up (llmint8_debug_kv_plan_for): host arithmetic, no GPU."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def L():
+    import os
+
+    import paper_2208_07339_amd as L
+    if not os.path.exists(L.LIB_PATH):
+        from paper_2208_07339_amd.build import build
+        build()
+    L.lib()
+    return L
+
+
+def plan(L, seqs, n_rows, max_rows, max_len, heads_q, heads, d, window=0):
+    """-> (rows to a tile, parts, halves, workgroups), or a status."""
+    from paper_2208_07339_amd.binding import KvPlan, _KvBatch
+    batch, p = _KvBatch(None, None, None, None, None, seqs, n_rows, 1, max_rows, max_len), KvPlan()
+    status = L.lib().llmint8_debug_kv_plan_for(C.byref(batch), heads_q, heads, d, window, C.byref(p))
+    return status or (p.tile, p.parts, p.halves, p.workgroups)
+
+
+def test_forms(L):
+    # one token: a tile of the kernel for few rows to each head, and parts where the axis is long
+    assert plan(L, 1, 1, 1, 76, 12, 12, 64) == (32, 1, 0, 16)
+    assert plan(L, 1, 1, 1, 4001, 40, 40, 128) == (32, 6, 0, 240)
+    # rows of all query heads that share keys together
+    assert plan(L, 64, 64, 1, 4101, 32, 8, 128) == (32, 1, 0, 512)
+    # prompts: 128 rows, 256 where the axis is long, parts where rows are few, halves where the tiles are
+    assert plan(L, 1, 2048, 2048, 2048, 32, 32, 128) == (128, 1, 0, 512)
+    assert plan(L, 1, 8192, 8192, 8192, 40, 40, 128) == (256, 1, 0, 1280)
+    assert plan(L, 1, 1024, 1024, 21035, 32, 8, 128) == (256, 2, 0, 256)
+    assert plan(L, 1, 1500, 1500, 1500, 16, 16, 128) == (128, 1, 1, 192)
+    assert plan(L, 1, 1500, 1500, 1500, 16, 16, 129)[2] == 0  # halves are for heads of up to 128
+    # a window leaves less to see
+    assert plan(L, 1, 2100, 2100, 4200, 32, 32, 64) == (256, 1, 0, 288)
+    assert plan(L, 1, 2100, 2100, 4200, 32, 32, 64, 1000) == (128, 1, 0, 544)
+    assert plan(L, 1, 2100, 2100, 4200, 32, 32, 64, 4201) == (256, 1, 0, 288)
+    # max_rows beyond the rows that there are changes nothing
+    assert plan(L, 1, 1, 4096, 4001, 40, 40, 128) == plan(L, 1, 1, 1, 4001, 40, 40, 128)
+
+
+@pytest.mark.parametrize("window", [0, 1, 1000, 2 ** 31 - 1])
+def test_parts_are_what_the_workspace_is_for(L, window):
+    from paper_2208_07339_amd.binding import _KvBatch
+    for seqs, rows, length, hq, h, d in [(1, 1, 4001, 40, 40, 128), (2, 1, 131072, 64, 8, 128), (1, 1024, 21035, 32, 8, 128), (3, 50, 9000, 8, 2, 200)]:
+        batch = _KvBatch(None, None, None, None, None, seqs, seqs * rows, 1, rows, length)
+        n = L.lib().llmint8_kv_attention_workspace_bytes(C.byref(batch), hq, h, d)
+        parts = plan(L, seqs, seqs * rows, rows, length, hq, h, d, window)[1]
+        need = parts * seqs * rows * hq * (4 * d + 8)
+        assert parts == 1 or need < n
+        assert window or n == need + 512
+
+
+def test_refusals(L):
+    assert plan(L, 1, 1, 1, 100, 4, 2, 64)[0] == 32
+    for bad in ((0, 1, 1, 100, 4, 2, 64), (1, 0, 1, 100, 4, 2, 64), (1, 1, 0, 100, 4, 2, 64), (1, 1, 1, -1, 4, 2, 64), (1, 1, 1, 2 ** 30, 4, 2, 64),
+                (1, 1, 1, 100, 3, 2, 64), (1, 1, 1, 100, 0, 0, 64), (1, 1, 1, 100, 4, 2, 0), (1, 1, 1, 100, 4, 2, 257), (1, 1, 1, 100, 4, 2, 64, -1)):
+        assert plan(L, *bad) == 1, bad
+    f = L.lib().llmint8_debug_kv_plan_for
+    from paper_2208_07339_amd.binding import KvPlan, _KvBatch
+    assert f(None, 4, 2, 64, 0, C.byref(KvPlan())) == 1
+    assert f(C.byref(_KvBatch(None, None, None, None, None, 1, 1, 1, 1, 100)), 4, 2, 64, 0, None) == 1
