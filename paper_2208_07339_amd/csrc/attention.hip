@@ -138,6 +138,24 @@ struct AttendArgs {
     bool vec;      // d and the rows of q allow 16-byte accesses
 };
 
+// Four numbers of a result: rounded in one place, since a compiler may fuse the product with the conversion (one rounding) or not (two),
+// and the bits are not to hang on which store follows.
+__device__ __forceinline__ h4 rounded(f4 x, float f)
+{
+    return h4{(_Float16)(x[0] * f), (_Float16)(x[1] * f), (_Float16)(x[2] * f), (_Float16)(x[3] * f)};
+}
+// those of them that a row has: the first n
+__device__ __forceinline__ void put4(_Float16* dst, h4 y, int n, bool vec)
+{
+    if (vec) {
+        if (n > 0) *(h4*)dst = y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (e < n) dst[e] = y[e];
+    }
+}
+
 // features f .. f + 7 of a row of d
 __device__ __forceinline__ h8 q8(const _Float16* row, int f, int d, bool vec)
 {
@@ -421,14 +439,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
                         if (at + e < p.d) dst[e] = sum[e];
                 }
             } else {
-                _Float16* dst = a.out + row * a.ld_out + (long long)g * p.d + at;
-                if (a.vec) {
-                    *(h4*)dst = h4{(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv), (_Float16)(sum[3] * inv)};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (at + e < p.d) dst[e] = (_Float16)(sum[e] * inv);
-                }
+                put4(a.out + row * a.ld_out + (long long)g * p.d + at, rounded(sum, inv), p.d - at, a.vec);
             }
         }
     }
@@ -850,16 +861,7 @@ __global__ void __launch_bounds__(64 * WAVES * PARTS, WAVES * PARTS == 4 && DP <
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const int f = 32 * q + 8 * j + 4 * hh;
-                h4 y;
-#pragma unroll
-                for (int e = 0; e < 4; e++) y[e] = (_Float16)(o[q][4 * j + e] * inv);
-                if (a.vec) {
-                    if (f < p.d) *(h4*)(dst + f) = y;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (f + e < p.d) dst[f + e] = y[e];
-                }
+                put4(dst + f, rounded(f4{o[q][4 * j], o[q][4 * j + 1], o[q][4 * j + 2], o[q][4 * j + 3]}, inv), p.d - f, a.vec);
             }
     }
 }
@@ -986,13 +988,7 @@ __global__ void __launch_bounds__(256) kv_join_few_kernel(const AttendArgs a)
         }
     const float inv = den != 0.0f ? 1.0f / den : 0.0f;
     _Float16* dst = a.out + x / a.heads_q * a.ld_out + x % a.heads_q * d + f0;
-    if (a.vec) {
-        *(h4*)dst = h4{(_Float16)(sum[0] * inv), (_Float16)(sum[1] * inv), (_Float16)(sum[2] * inv), (_Float16)(sum[3] * inv)};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-            if (f0 + e < d) dst[e] = (_Float16)(sum[e] * inv);
-    }
+    put4(dst, rounded(sum, inv), d - f0, a.vec);
 }
 
 template <int DP>

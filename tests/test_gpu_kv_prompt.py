@@ -218,6 +218,33 @@ def test_scores_that_grow_along_the_axis():
             dev.check(want, q=q, scale=1.0)
 
 
+FEW = {"rows32 parts": ((32, True, False), 2, 3, [40, 1], [4200, 2000]), "rows32 many parts": ((32, True, False), 2, 4, [1], [9000])}
+
+
+@pytest.mark.parametrize("d", [32, 36])
+@pytest.mark.parametrize("form", [*FORMS, *FEW])
+def test_strides_and_alignment(form, d):
+    """The same bits wherever the rows are, with parts and without."""
+    want, heads, group, new, lengths = {**FORMS, **FEW}[form]
+    dev = Prompt(heads, group, new, lengths, d, seed=7)
+    q = dev.queries()
+    rows, hq, _ = q.shape
+    plain = dev.check(want, q=q)
+    batch = dev.batch(dev.new, dev.lengths())
+    dev.expect(want, batch)
+    for off, extra in [(0, 3), (1, 3), (8, 16)]:
+        wide = dev.torch.full((rows * (hq * d + extra) + 16,), 9.0, dtype=dev.torch.float16, device="cuda")
+
+        def view(t):
+            return t[off:off + rows * (hq * d + extra)].view(rows, hq * d + extra)[:, :hq * d].unflatten(1, (hq, d))
+        qs, out = view(wide.clone()), view(wide)
+        qs.copy_(dev.dev(q))
+        dev.L.kv_attention(dev.cache, batch, qs, out=out)
+        assert dev.torch.equal(out, plain)
+        out.fill_(9.0)
+        assert (wide == 9.0).all()  # nothing was written between the rows
+
+
 @pytest.mark.parametrize("what", ["rows", "length", "table", "slot", "most_len"])
 @pytest.mark.parametrize("form", FORMS)
 def test_batches_that_cannot_be(form, what):
