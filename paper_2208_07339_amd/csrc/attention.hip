@@ -1068,6 +1068,9 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
         }
     }
     if (r.splits < 1) r.splits = 1;
+    // One tile more than there are, where a wave does not look at all sequences together: its workgroups look past the last one, so that
+    // a sequence that cannot be is found also where it has no tile of its own.
+    if (r.tile != KV_STEP_ROWS && p.n_seqs > 64) r.tiles++;
     return r;
 }
 
