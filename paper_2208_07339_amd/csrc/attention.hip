@@ -133,6 +133,8 @@ struct AttendArgs {
     float scale;         // log2(e) included
     int causal, window;
     Div splits, tiles;  // tiles: of 32 rows to a sequence, few rows
+    Div units;          // workgroups to each of these
+    bool ragged;
     float* part;   // [split][row * heads_q + head][d] sums, not divided
     float2* stat;  // [split][row * heads_q + head] (m, l)
     bool vec;      // d and the rows of q allow 16-byte accesses
@@ -225,8 +227,16 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
     // Workgroups go to the eight XCDs in turn: the row tiles of one part of one sequence's positions run on one XCD, one after the
-    // other, and find the codes in its L2.
-    const int turn = blockIdx.x / 8, tile = a.tiles.rem(turn), unit = a.tiles.quot(turn) * 8 + blockIdx.x % 8;
+    // other, and find the codes in its L2.  Where most tiles are not there (`ragged`) the first tiles of all come first instead: else
+    // those that are there would be so many workgroups apart, and might all be dealt to the same few compute units (64 sequences of 300
+    // positions, one of 100 rows, the others of one, 8 heads: 45 us against 21).
+    int tile, unit;
+    if (a.ragged) {
+        tile = a.units.quot(blockIdx.x), unit = a.units.rem(blockIdx.x);
+    } else {
+        const int turn = blockIdx.x / 8;
+        tile = a.tiles.rem(turn), unit = a.tiles.quot(turn) * 8 + blockIdx.x % 8;
+    }
     const int who = a.splits.quot(unit), split = a.splits.rem(unit), head = a.heads.rem(who), b = a.heads.quot(who), splits = (int)a.splits.d;
     const int g_ = (int)a.group.d;
     if (b >= p.n_seqs) return;
@@ -1032,13 +1042,18 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     // eight sequences of 1 000 to 9 000 positions: 30 us against 42; 2 048 rows of 32 heads: 95 against 61).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
     int blocks = seen(KV_STEP_ROWS);
-    if (rows <= KV_STEP_ROWS || few * blocks <= 24576) {
+    // It is launched with the most tiles that a sequence has for every one, and those that are not there cost their start: as much as is
+    // saved at about 8 000 (64 sequences of 300 positions, 8 heads, one of 500 rows and the others of one: 38 us against 40 by the
+    // kernel for many rows; of 700: 47 against 40; 256 sequences, one of 2 048 rows that see 128 positions: 205 against 35).
+    const long long launched = p.n_seqs * ((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS) * p.heads;
+    if (rows <= KV_STEP_ROWS || (few * (blocks > 1 ? blocks : 1) <= 24576 && launched - few <= 8192)) {
         // One workgroup to a compute unit: two to each read no faster and have more to join (one row over 4 000 positions of 32 heads
         // in 8 parts 11.8 us, in 16 13.4; 40 over 16 000 of 8 in 16 parts 19.3, in 32 22.8).  Sequences may differ in length, so
         // that parts of some end early: there, twice as many (the eight above in 4 parts 33 us, in 7 25).
         r.tile = KV_STEP_ROWS, r.tiles = (int)((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS);
         const long long want = (p.n_seqs > 1 ? 512 : 256) / few, most = (blocks + 7) / 8;
         r.splits = (int)(want < most ? want : most);
+        r.ragged = 2 * launched >= 3 * few;
     } else {
         // 256 rows convert a block half as often as two times 128, but are one workgroup to a compute unit, whose start and end nothing
         // covers (2 048 positions: 70 us against 61; 8 192: 787 against 820)
@@ -1064,7 +1079,7 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
         if (!wide && pairs <= 512) {
             const int mean = (p.max_len + KV_BLOCK - 1) / KV_BLOCK - p.max_rows / (2 * KV_BLOCK);
             const float t = 0.58f * fmaxf((float)longest, pairs * (float)(mean < longest ? mean : longest) / 256);
-            if (t + (pairs > 256 ? 35 : 5) < least) r = {128, (int)tiles(128), 1, true};
+            if (t + (pairs > 256 ? 35 : 5) < least) r = {128, (int)tiles(128), 1, true, false};
         }
     }
     if (r.splits < 1) r.splits = 1;
@@ -1091,6 +1106,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     AttendArgs a;
     a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
     a.group = Div(c.heads_q / p.heads), a.heads = Div(p.heads), a.splits = Div(plan.splits), a.tiles = Div(plan.tiles < 1 ? 1 : plan.tiles);
+    a.units = Div((int)(kv_attention_workgroups(p, plan) / a.tiles.d)), a.ragged = plan.ragged;
     a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window;
     const size_t total = (size_t)p.n_rows * c.heads_q;
     a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));

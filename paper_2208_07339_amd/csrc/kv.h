@@ -162,6 +162,7 @@ struct KvPlan {
     int tiles;   // tiles that a sequence has at most (tile = KV_STEP_ROWS), or that all have together
     int splits;  // parts of the positions, joined by a kernel of their own if more than one
     bool halves;  // (tile = 128) a tile's blocks on two halves of a workgroup
+    bool ragged;  // (tile = KV_STEP_ROWS) most sequences have far fewer tiles than the one with the most
 };
 KvPlan kv_plan(const Kv& p, int heads_q, int window);  // window 0: none
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d);

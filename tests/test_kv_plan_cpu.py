@@ -65,3 +65,18 @@ def test_refusals(L):
     from paper_2208_07339_amd.binding import KvPlan, _KvBatch
     assert f(None, 4, 2, 64, 0, C.byref(KvPlan())) == 1
     assert f(C.byref(_KvBatch(None, None, None, None, None, 1, 1, 1, 1, 100)), 4, 2, 64, 0, None) == 1
+
+
+def test_workgroups_without_rows(L):
+    """The kernel for few rows is launched with the longest sequence's tiles for all: not where most of these would not be there."""
+    # 256 sequences, one of 2 048 rows, the others of one: 131 072 workgroups for 2 303 rows
+    assert plan(L, 256, 2303, 2048, 2048, 8, 8, 128, 128)[0] == 128
+    assert plan(L, 4096, 4095 + 131072, 131072, 131072, 1, 1, 64, 1)[3] < 10000
+    assert plan(L, 1, 1 << 28, 1 << 28, 0, 4, 4, 1)[3] * 256 < 1 << 32  # rows that see nothing
+    for seqs in (1, 3, 64, 100, 1000):
+        for rows in (33, 100, 1000, 10000):
+            for length in (1, 100, 1000, 100000):
+                for window in (0, 1, 100):
+                    n = plan(L, seqs, seqs - 1 + rows, rows, length, 8, 8, 64, window)[3]
+                    tiles = 8 * (seqs + rows // 32 + 1)  # of 32 rows, that there are
+                    assert n <= max(512, tiles) + 8192, (seqs, rows, length, window, n)
