@@ -1060,27 +1060,32 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
         r.tile = seen(128) >= 128 && rows > 128 && !wide ? 256 : 128;
         blocks = seen(r.tile);
         r.tiles = (int)tiles(r.tile);
+        // Blocks that a compute unit goes through one after the other where n workgroups share `room` places: those of the longest; on
+        // average; and in so many rounds, of the shortest, since behind a long past a second round is as long as the first.
+        auto in_turn = [&](int n, int room, int longest) {
+            const int end = (p.max_len + KV_BLOCK - 1) / KV_BLOCK, mean = end - p.max_rows / (2 * KV_BLOCK), shortest = end - p.max_rows / KV_BLOCK;
+            auto one = [&](int x) { return (float)(x < longest ? x : longest); };
+            return fmaxf((float)longest, fmaxf(n * one(mean) / room, (n + room - 1) / room * one(shortest)));
+        };
         // Parts, one round of the chip at most: a workgroup's blocks one after the other (0.75 us each, 1.05 with two waves to a SIMD)
         // against what the join reads and writes (1 024 rows of 32 heads over themselves in one part 29 us, in two 41; behind 20 011
         // others 690 in one by that, 337 in two).
-        const int units = r.tiles * p.heads, want = (r.tile == 256 ? 256 : 512) / units, most = (blocks + 7) / 8;
+        const int units = r.tiles * p.heads, room = r.tile == 256 ? 256 : 512, want = room / units, most = (blocks + 7) / 8;
         const float join = (float)p.n_rows * heads_q * p.d * (8 / 4.5e6f);
-        float least = 0;
+        float least = (r.tile == 256 || units > 256 ? 1.05f : 0.75f) * in_turn(units, room, blocks);
         r.splits = 1;
-        for (int x = 1; x <= want && x <= most; x++) {
-            const float t = (r.tile == 256 || units * x > 256 ? 1.05f : 0.75f) * blocks / x + (x > 1 ? 5 + x * join : 0);
-            if (x == 1 || t < least) least = t, r.splits = x;
+        for (int x = 2; x <= want && x <= most; x++) {
+            const float t = (r.tile == 256 || units * x > 256 ? 1.05f : 0.75f) * blocks / x + 5 + x * join;
+            if (t < least) least = t, r.splits = x;
         }
         // Two halves of a workgroup to a tile, each with half of its blocks: where tiles are few, the last ones, which see most, are the
         // time.  One such workgroup to a compute unit, so at most two rounds, of which the second starts when the first's short
         // ones end (rows over themselves, in halves and not: 4 096 of 8 heads 72 us and 77, of 16 97 and 116, 8 192 of 8 170 and 216, but
-        // 2 048 of 32 65 and 60).  mean: blocks that a tile sees on average.
-        const int pairs = (int)tiles(128) * p.heads, longest = seen(128);
-        if (!wide && pairs <= 512) {
-            const int mean = (p.max_len + KV_BLOCK - 1) / KV_BLOCK - p.max_rows / (2 * KV_BLOCK);
-            const float t = 0.58f * fmaxf((float)longest, pairs * (float)(mean < longest ? mean : longest) / 256);
-            if (t + (pairs > 256 ? 35 : 5) < least) r = {128, (int)tiles(128), 1, true, false};
-        }
+        // 2 048 of 32 65 and 60).  Where there are no short ones, behind a long past, two rounds are worth it only against two of the
+        // others (1 024 rows of 40 heads over 6 000: 190 us, 160 in tiles of 256; 20 times 96 rows of 32/8 heads over 6 000: 239 and 330).
+        const int pairs = (int)tiles(128) * p.heads;
+        if (!wide && pairs <= 512 && 0.58f * in_turn(pairs, 256, seen(128)) + (pairs > 256 ? 35 : 5) < least)
+            r = {128, (int)tiles(128), 1, true, false};
     }
     if (r.splits < 1) r.splits = 1;
     // One tile more than there are, where a wave does not look at all sequences together: its workgroups look past the last one, so that

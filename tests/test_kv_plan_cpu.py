@@ -80,3 +80,16 @@ def test_workgroups_without_rows(L):
                     n = plan(L, seqs, seqs - 1 + rows, rows, length, 8, 8, 64, window)[3]
                     tiles = 8 * (seqs + rows // 32 + 1)  # of 32 rows, that there are
                     assert n <= max(512, tiles) + 8192, (seqs, rows, length, window, n)
+
+
+@pytest.mark.parametrize("seqs, rows, length, heads_q, heads, form", [
+    # more tiles of 256 rows than the chip holds at once: two halves where those of 128 rows are no more than two rounds
+    (20, 96, 6000, 32, 8, (128, 1, 1)), (1, 2688, 8688, 24, 24, (128, 1, 1)),
+    # behind a long past a second round of halves is as long as the first: one round of whole tiles
+    (1, 1024, 6000, 40, 40, (256, 1, 0)), (1, 900, 16000, 40, 8, (256, 1, 0)), (4, 300, 4200, 24, 24, (256, 1, 0)), (40, 129, 5000, 4, 4, (256, 1, 0)),
+    (3, 1500, 6000, 10, 10, (256, 1, 0)), (1, 1100, 3000, 40, 40, (128, 1, 0)), (2, 500, 3000, 40, 40, (128, 1, 0)),
+    # one round of halves, or a second that is short
+    (1, 1024, 8000, 32, 8, (128, 1, 1)), (60, 50, 5000, 8, 1, (128, 1, 1)), (1, 4096, 4096, 16, 16, (128, 1, 1)), (1, 8192, 8192, 8, 8, (128, 1, 1)),
+    (1, 3000, 3000, 16, 16, (128, 1, 1))])
+def test_halves_by_rounds(L, seqs, rows, length, heads_q, heads, form):
+    assert plan(L, seqs, seqs * rows, rows, length, heads_q, heads, 128)[:3] == form
