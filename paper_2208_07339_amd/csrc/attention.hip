@@ -134,7 +134,7 @@ struct AttendArgs {
     int causal, window;
     Div splits, tiles;  // tiles: of 32 rows to a sequence, few rows
     Div units;          // workgroups to each of these
-    bool ragged;
+    bool by_tile;       // their order: all first tiles, all second ones, ...
     float* part;   // [split][row * heads_q + head][d] sums, not divided
     float2* stat;  // [split][row * heads_q + head] (m, l)
     bool vec;      // d and the rows of q allow 16-byte accesses
@@ -227,11 +227,9 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
     const Kv& p = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qr = lane & 31, hh = lane >> 5;
     // Workgroups go to the eight XCDs in turn: the row tiles of one part of one sequence's positions run on one XCD, one after the
-    // other, and find the codes in its L2.  Where most tiles are not there (`ragged`) the first tiles of all come first instead: else
-    // those that are there would be so many workgroups apart, and might all be dealt to the same few compute units (64 sequences of 300
-    // positions, one of 100 rows, the others of one, 8 heads: 45 us against 21).
+    // other, and find the codes in its L2.  Or the first tiles of all parts come first (step_by_tile).
     int tile, unit;
-    if (a.ragged) {
+    if (a.by_tile) {
         tile = a.units.quot(blockIdx.x), unit = a.units.rem(blockIdx.x);
     } else {
         const int turn = blockIdx.x / 8;
@@ -1094,11 +1092,24 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     return r;
 }
 
+// Parts of sequences and heads, each with as many tiles as a sequence has at most
+inline long long step_units(const Kv& p, const KvPlan& plan) { return (long long)p.heads * p.n_seqs * plan.splits; }
+
+// Whether the step kernel's workgroups go by tile.  A part's tiles on one XCD leave XCDs without work where parts are few (500 rows of
+// 48 heads that share one: one XCD had all of them, 111 us against 23), and where most tiles are not there, those that are would be so
+// many workgroups apart that they might all be dealt to the same few compute units (64 sequences of 300 positions, one of 100 rows,
+// the others of one, 8 heads: 45 us against 21).
+inline bool step_by_tile(const Kv& p, const KvPlan& plan)
+{
+    const long long units = step_units(p, plan);
+    return plan.ragged || 8 * ((units + 7) / 8 * 8 - units) >= units;
+}
+
 long long kv_attention_workgroups(const Kv& p, const KvPlan& plan)
 {
-    // (the step kernel: parts of sequences and heads in eights, for the XCDs, with the tiles that a sequence has at most)
-    if (plan.tile == KV_STEP_ROWS) return ((long long)p.heads * p.n_seqs * plan.splits + 7) / 8 * 8 * plan.tiles;
-    return (long long)plan.tiles * p.heads * plan.splits;
+    if (plan.tile != KV_STEP_ROWS) return (long long)plan.tiles * p.heads * plan.splits;
+    const long long units = step_units(p, plan);
+    return (step_by_tile(p, plan) ? units : (units + 7) / 8 * 8) * plan.tiles;
 }
 
 size_t kv_attention_ws(const KvPlan& plan, int n_rows, int heads_q, int d)
@@ -1111,7 +1122,7 @@ hipError_t launch_kv_attention(const Kv& p, const KvAttend& c, const KvPlan& pla
     AttendArgs a;
     a.kv = p, a.q = (const _Float16*)c.q, a.out = (_Float16*)c.out, a.ld_q = c.ld_q, a.ld_out = c.ld_out, a.heads_q = c.heads_q;
     a.group = Div(c.heads_q / p.heads), a.heads = Div(p.heads), a.splits = Div(plan.splits), a.tiles = Div(plan.tiles < 1 ? 1 : plan.tiles);
-    a.units = Div((int)(kv_attention_workgroups(p, plan) / a.tiles.d)), a.ragged = plan.ragged;
+    a.units = Div((int)step_units(p, plan)), a.by_tile = step_by_tile(p, plan);
     a.scale = c.scale * LOG2E, a.causal = c.causal, a.window = c.window;
     const size_t total = (size_t)p.n_rows * c.heads_q;
     a.stat = (float2*)ws, a.part = (float*)((char*)ws + ((plan.splits * total * 8 + 255) & ~(size_t)255));

@@ -19,3 +19,18 @@ def test_one_prompt_among_single_rows(heads, group, new, lengths, window, tile):
     dev.check_attention(new, rng, group=group, window=window)
     dev.check_attention(new, rng, group=group, window=window, idle=(0, len(new) - 1))
     assert int(dev.status) == 0
+
+
+@pytest.mark.parametrize("heads, group, new, lengths", [
+    (1, 48, [30], [400]), (1, 48, [7, 3, 5], [1000, 90, 2000]), (2, 8, [100], [3000]), (3, 1, [700], [900]), (9, 1, [200], [200]), (12, 1, [300, 40], [300, 250]),
+    (17, 1, [90], [130])])
+def test_few_parts(heads, group, new, lengths):
+    """Numbers of heads and parts that are no multiple of eight, with many tiles."""
+    rng = np.random.default_rng(heads)
+    dev = Device(len(new), heads, 64, page=64, most=max(lengths), seed=heads)
+    dev.append(lengths, rng)
+    assert dev.L.debug_kv_plan_for(dev.cache, dev.batch(new, lengths), heads * group).tile == 32
+    dev.check_attention(new, rng, group=group)
+    dev.check_attention(new, rng, group=group, causal=False)
+    dev.check_attention(new, rng, group=group, window=60)
+    assert int(dev.status) == 0

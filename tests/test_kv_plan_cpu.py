@@ -26,7 +26,7 @@ def plan(L, seqs, n_rows, max_rows, max_len, heads_q, heads, d, window=0):
 
 def test_forms(L):
     # one token: a tile of the kernel for few rows to each head, and parts where the axis is long
-    assert plan(L, 1, 1, 1, 76, 12, 12, 64) == (32, 1, 0, 16)
+    assert plan(L, 1, 1, 1, 76, 12, 12, 64) == (32, 1, 0, 12)
     assert plan(L, 1, 1, 1, 4001, 40, 40, 128) == (32, 6, 0, 240)
     # rows of all query heads that share keys together
     assert plan(L, 64, 64, 1, 4101, 32, 8, 128) == (32, 1, 0, 512)
@@ -93,3 +93,11 @@ def test_workgroups_without_rows(L):
     (1, 3000, 3000, 16, 16, (128, 1, 1))])
 def test_halves_by_rounds(L, seqs, rows, length, heads_q, heads, form):
     assert plan(L, seqs, seqs * rows, rows, length, heads_q, heads, 128)[:3] == form
+
+
+@pytest.mark.parametrize("seqs, rows, length, heads_q, heads, tiles, parts", [
+    (1, 500, 500, 48, 1, 750, 1), (1, 100, 5000, 48, 1, 150, 1), (1, 1000, 1000, 16, 2, 500, 1), (1, 1000, 1000, 12, 12, 384, 1),
+    (1, 20, 2000, 48, 1, 30, 8), (1, 500, 500, 32, 32, 512, 1), (1, 1, 4001, 40, 40, 40, 6)])
+def test_workgroups_are_the_tiles_that_there_are(L, seqs, rows, length, heads_q, heads, tiles, parts):
+    """Few parts: not rounded up to one for each XCD, which would leave XCDs without work."""
+    assert plan(L, seqs, seqs * rows, rows, length, heads_q, heads, 128)[:4] == (32, parts, 0, tiles * parts)
