@@ -413,18 +413,19 @@ hipError_t launch_kv_append(const Kv& p, const KvAppend& c, hipStream_t st)
     a.q_out = (unsigned short*)c.q_out, a.ld_q_out = c.ld_q_out, a.heads_q = c.heads_q;
     a.rot = {c.cos, c.sin, c.n_pos, c.rot / 2, c.pairs};
     const bool has_q = c.q && !(c.q == c.q_out && c.rot == 0);
-    const int rows = p.max_rows < KV_BLOCK ? p.max_rows : KV_BLOCK;
-    // query heads to a workgroup: about four groups of 8 features to a thread, or 16 where there are more than enough workgroups
-    // (17 550 tokens of 48 heads 155 and 138 us; eight times five tokens of 48 heads 4.1 and 8)
-    const int of4 = 512 / (rows * ((p.d + 7) / 8)), g4 = of4 < 1 ? 1 : of4;
-    const int g = has_q && most_blocks(p) * ((c.heads_q + g4 - 1) / g4) > 4096 ? 2048 / (rows * ((p.d + 7) / 8)) : g4;
-    a.q_group = g < 1 ? 1 : has_q && g > c.heads_q ? c.heads_q : g;
-    a.head_groups = (p.heads + HEADS - 1) / HEADS;
-    const int qy = has_q ? (c.heads_q + a.q_group - 1) / a.q_group : 0;
     auto aligned = [](const void* q, long long ld) { return ((uintptr_t)q & 15) == 0 && ld % 8 == 0; };
     bool vec = p.d % 8 == 0 && aligned(c.k, c.ld_k) && aligned(c.v, c.ld_v);
     if (has_q) vec = vec && aligned(c.q, c.ld_q) && aligned(c.q_out, c.ld_q_out);
     if (c.rot) vec = vec && aligned(c.cos, 0) && aligned(c.sin, 0) && c.rot % (c.pairs ? 8 : 16) == 0;
+    const int rows = p.max_rows < KV_BLOCK ? p.max_rows : KV_BLOCK;
+    // query heads to a workgroup: about four groups of 8 features to a thread, or 16 where there are more than enough workgroups (17 550
+    // tokens of 48 heads 118 and 101 us; eight times five tokens of 48 heads 4.1 and 8).  Not with accesses of two bytes, whose turns
+    // are eight times as many (8 192 tokens of 32 heads of 80, 20 features rotated: 102 us, and 124 with the larger groups).
+    const int of4 = 512 / (rows * ((p.d + 7) / 8)), g4 = of4 < 1 ? 1 : of4;
+    const int g = has_q && vec && most_blocks(p) * ((c.heads_q + g4 - 1) / g4) > 4096 ? 2048 / (rows * ((p.d + 7) / 8)) : g4;
+    a.q_group = g < 1 ? 1 : has_q && g > c.heads_q ? c.heads_q : g;
+    a.head_groups = (p.heads + HEADS - 1) / HEADS;
+    const int qy = has_q ? (c.heads_q + a.q_group - 1) / a.q_group : 0;
     const dim3 grid((unsigned)most_blocks(p), a.head_groups + qy);
     if (vec)
         kv_append_kernel<true><<<grid, 64 * HEADS, HEADS * block_lds(p.d), st>>>(a);
