@@ -305,8 +305,9 @@ int llmint8_kv_append(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t 
 /* out row of query head g = sum_j w_j v_j, w = softmax over j of scale * q . k_j, with the keys and values of head
  * g / (heads_q / heads) at the positions j that the row sees: causal != 0: j up to its own position, else all kv_len; window > 0
  * (causal only): no j further back than window - 1 before its own.  A row that sees nothing (an idle sequence's, or a causal
- * one at a position before 0, where kv_len is smaller than its sequence's rows) is zero.  scale >= 0, finite.  Sums, maxima and
- * weights are fp32; weights are rounded to fp16 for the matrix units, the result once to fp16.
+ * one at a position before 0, where kv_len is smaller than its sequence's rows) is zero.  scale >= 0, finite, and such that 1.45
+ * scale |q . k_j| is in fp32's range (else a row may be NaN).  Sums, maxima and weights are fp32; weights are rounded to fp16 for
+ * the matrix units, the result once to fp16.
  *   q    in   fp16, row r and head g at r * ld_q + g * d;  heads_q a multiple of the cache's heads
  *   out  out  fp16, the same with ld_out
  *   ws        llmint8_kv_attention_workspace_bytes(batch, heads_q, heads, d) bytes; may be NULL where that is 0              */

@@ -208,13 +208,19 @@ __device__ __forceinline__ float open_unit(unsigned largest)
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Few rows (at most 32 with all query heads that share keys): the cache is read once, straight into registers in operand order,
-// every wave blocks of its own; sums meet in LDS.  Bound by HBM: 1 byte a cached number, about 4 operations to it for each row,
-// which the matrix units have to spare even where only one of a tile's 32 rows is there.  Each wave has two blocks on their way (of
-// d = 128: 8 KiB each, 32 MiB on the chip).  Two sequences of 257 000 positions together, 64 heads over 8 of 128, one row each: 527 MB
-// in 82 us, 6.4 TB/s (a kernel that only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us,
-// 5.0 TB/s; the longest sequences end last.  Short ones are latency, from the page table to the codes to the sum of the four waves:
-// 6.5 us for 75 positions of 12 heads of 64.
+// Few rows, or little work (kv_plan): a workgroup to a tile of 32 rows (tokens, and for each the query heads that share its keys) and a
+// part of the positions.  The codes come straight into registers in operand order, every wave blocks of its own; sums meet in LDS.
+// Sequences of more than 32 rows have more tiles, each of which reads and converts the blocks again: from the L2 (eight times 3 to
+// 7 rows of 48 heads that share keys, 4 to 11 tiles: 1.4 times the codes come from behind it), but the conversion is about half of a
+// tile's vector instructions.  Loads are marked as not to be kept, which does not keep them from the L2 for that long (the same bytes
+// come from behind it without the mark), and is worth it where an axis is long (the two sequences below 91 us, 102 without).
+// Single rows are bound by HBM: 1 byte a cached number, about 4 operations to it for each row, which the matrix units have to spare
+// even where only one of a tile's 32 rows is there.  Each wave has two blocks on their way (of d = 128: 8 KiB each, 32 MiB on the
+// chip).  Two sequences of 257 000 positions together, 64 heads over 8 of 128, one row each: 527 MB in 81 us, 6.5 TB/s (a kernel that
+// only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us, 5.0 TB/s; the longest sequences end last.
+// Short ones are latency, from the page table to the codes to the sum of the four waves: 6.6 us for 76 positions of 12 heads of 64.
+// Heads of more than 128 take 353 to 512 registers a lane, 97 to 256 of them accumulation registers: one wave to a SIMD, and 2 (of d =
+// 224) or 11 (of 256) in memory.  One row over 4 000 positions of 16 heads of 256: 17 us; 64 of 200 to 4 100 of 16/2: 63.
 // ---------------------------------------------------------------------------------------------------------------------------
 constexpr int JOIN_FLOATS = 32 * 36;  // for a wave's sums in LDS: 32 rows of 32 features, or fewer of more
 
@@ -459,9 +465,11 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) kv_step_kernel(const At
 // for all rows.  Bound by the matrix units, by what makes scores weights and by the reads of LDS, each about half of the time and
 // kept busy at the same time: the scores of the next block are computed while the weights of this one are.  So LDS holds keys one
 // block ahead of values.  (Operands of 64 rows a wave halve the reads, but leave one wave to a SIMD, which then issues vector
-// instructions half as often: no faster.)  8 192 tokens of 40 heads of 128, each seeing those before it: 680 us, 1.01 PFLOP/s of
-// what they see; a matrix product of 16 384 x 16 384 x 16 384 by the library reaches 1.32.  1 024 tokens behind 20 011, 32 heads over
-// 8: 336 us with the join, 1.02 PFLOP/s.  2 048 tokens of 32 heads: 57 us, 0.60; the last tile's 64 blocks are its time.
+// instructions half as often: no faster.)  8 192 tokens of 40 heads of 128, each seeing those before it: 690 us, 0.99 PFLOP/s of what
+// they see (675 to 730 from card to card, by the clock that power leaves); a matrix product of 16 384 x 16 384 x 16 384 by the library reaches
+// 1.32.  1 024 tokens behind 20 011, 32 heads over 8: 336 us with the join, 1.02 PFLOP/s.  2 048 tokens of 32 heads: 57 us, 0.60; the
+// last tile's 64 blocks are its time.  Heads of more than 128 take 356 to 512 registers: one wave to a SIMD, and 7 (of 256) in memory.
+// 2 048 tokens of 16 heads of 256: 101 us, 0.34 PFLOP/s; 8 192 of 16/2: 751, 0.73.
 // ---------------------------------------------------------------------------------------------------------------------------
 //
 // PARTS 2: two such groups of waves to a workgroup and tile, each with half of its blocks and an LDS of its own; the second's sums go to
@@ -1036,8 +1044,11 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
         return (int)(window && w < in ? w : in);
     };
     // The step kernel takes what it has registers for, and more rows where the cache's blocks and the row tiles are few: it reads and
-    // converts a block once for every 32 rows, but starts and ends in a third of the time (five tokens of 48 heads that share keys,
-    // eight sequences of 1 000 to 9 000 positions: 30 us against 42; 2 048 rows of 32 heads: 95 against 61).
+    // converts a block once for every 32 rows, but starts and ends in a third of the time.  By it and by the kernel for many rows: eight
+    // times 5 tokens of 48 heads that share keys over 1 000 to 9 000 positions 27 us and 42; 7 tokens, all over 9 000, 38 and 41; 500 rows
+    // of 32 heads over themselves 17 and 23, 700 26 and 27, 1 000 33 and 30, 2 048 83 and 59; 4 times 64 of 32 over 2 900 41 and 42.  The
+    // border is where they meet for heads of 64 to 128; the rule is not made for wider ones (500 rows of 32 heads of 256: 55 and 42,
+    // 700 of 16: 47 and 52) nor for short windows (1 900 rows of 32 heads of 80 that see 100: 35 and 23).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
     int blocks = seen(KV_STEP_ROWS);
     // It is launched with the most tiles that a sequence has for every one, and those that are not there cost their start: as much as is

@@ -70,7 +70,8 @@ __device__ __forceinline__ void move_rows(const Rows& in, const Rotation& rot, b
                                           int thread, int threads, Out out, bool& bad)
 {
     const int nh = h1 - h0, half = turned ? rot.half : 0;
-    // what is turned, and the rest: loops of their own, without branches, so that the requests of several turns go out together
+    // what is turned, and the rest: loops of their own, so that a turn's requests go out together, whatever it moves.  (The next turn's
+    // wait for it: its stores may be to what they read, for all that the compiler knows.)
     auto all = [&](int per, auto body) {
         const int total = n * nh * per;
 #pragma unroll 4
