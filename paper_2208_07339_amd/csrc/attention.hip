@@ -220,7 +220,7 @@ __device__ __forceinline__ float open_unit(unsigned largest)
 // only reads: 6.6 to 6.9).  64 sequences of 200 to 4 100, 32 heads over 8: 276 MB in 55 us, 5.0 TB/s; the longest sequences end last.
 // Short ones are latency, from the page table to the codes to the sum of the four waves: 6.6 us for 76 positions of 12 heads of 64.
 // Heads of more than 128 take 353 to 512 registers a lane, 97 to 256 of them accumulation registers: one wave to a SIMD, and 2 (of d =
-// 224) or 11 (of 256) in memory.  One row over 4 000 positions of 16 heads of 256: 17 us; 64 of 200 to 4 100 of 16/2: 63.
+// 224) or 11 (of 256) in memory.  One row over 4 000 positions of 16 heads of 256: 17 us; 64 of 200 to 4 100 of 16/2: 53.
 // ---------------------------------------------------------------------------------------------------------------------------
 constexpr int JOIN_FLOATS = 32 * 36;  // for a wave's sums in LDS: 32 rows of 32 features, or fewer of more
 
@@ -1051,6 +1051,7 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     // 700 of 16: 47 and 52) nor for short windows (1 900 rows of 32 heads of 80 that see 100: 35 and 23).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
     int blocks = seen(KV_STEP_ROWS);
+    const int chip = wide ? 256 : 512;  // workgroups of the step kernel at a time: registers for one to a compute unit, or two
     // It is launched with the most tiles that a sequence has for every one, and those that are not there cost their start: as much as is
     // saved at about 8 000 (64 sequences of 300 positions, 8 heads, one of 500 rows and the others of one: 38 us against 40 by the
     // kernel for many rows; of 700: 47 against 40; 256 sequences, one of 2 048 rows that see 128 positions: 205 against 35).
@@ -1058,9 +1059,10 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     if (rows <= KV_STEP_ROWS || (few * (blocks > 1 ? blocks : 1) <= 24576 && launched - few <= 8192)) {
         // One workgroup to a compute unit: two to each read no faster and have more to join (one row over 4 000 positions of 32 heads
         // in 8 parts 11.8 us, in 16 13.4; 40 over 16 000 of 8 in 16 parts 19.3, in 32 22.8).  Sequences may differ in length, so
-        // that parts of some end early: there, twice as many (the eight above in 4 parts 33 us, in 7 25).
+        // that parts of some end early: there, as many as the chip holds (the eight above in 4 parts 33 us, in 7 25; of wide heads no more
+        // than one either: 8 times 6 tokens of 16/2 heads of 256 over 4 000 in 8 parts 29 us, in 16 44; 2 times 33 of 16 over 3 000 39 and 60).
         r.tile = KV_STEP_ROWS, r.tiles = (int)((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS);
-        const long long want = (p.n_seqs > 1 ? 512 : 256) / few, most = (blocks + 7) / 8;
+        const long long want = (p.n_seqs > 1 ? chip : 256) / few, most = (blocks + 7) / 8;
         r.splits = (int)(want < most ? want : most);
         r.ragged = 2 * launched >= 3 * few;
     } else {

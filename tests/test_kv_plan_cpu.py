@@ -101,3 +101,11 @@ def test_halves_by_rounds(L, seqs, rows, length, heads_q, heads, form):
 def test_workgroups_are_the_tiles_that_there_are(L, seqs, rows, length, heads_q, heads, tiles, parts):
     """Few parts: not rounded up to one for each XCD, which would leave XCDs without work."""
     assert plan(L, seqs, seqs * rows, rows, length, heads_q, heads, 128)[:4] == (32, parts, 0, tiles * parts)
+
+
+@pytest.mark.parametrize("d, most", [(128, 512), (129, 256), (256, 256)])
+def test_parts_of_several_sequences_are_one_round(L, d, most):
+    """Heads of more than 128 leave registers for one workgroup to a compute unit, others for two."""
+    for seqs, rows, length, heads_q, heads in [(8, 6, 4000, 16, 2), (2, 1, 100000, 16, 2), (30, 1, 3000, 16, 2), (3, 1, 5000, 16, 16), (32, 5, 1000, 16, 2)]:
+        tile, parts, _, workgroups = plan(L, seqs, seqs * rows, rows, length, heads_q, heads, d)
+        assert tile == 32 and parts > 1 and most * 3 // 4 <= workgroups <= most, (seqs, parts, workgroups)
