@@ -1047,8 +1047,8 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     // converts a block once for every 32 rows, but starts and ends in a third of the time.  By it and by the kernel for many rows: eight
     // times 5 tokens of 48 heads that share keys over 1 000 to 9 000 positions 27 us and 42; 7 tokens, all over 9 000, 38 and 41; 500 rows
     // of 32 heads over themselves 17 and 23, 700 26 and 27, 1 000 33 and 30, 2 048 83 and 59; 4 times 64 of 32 over 2 900 41 and 42.  The
-    // border is where they meet for heads of 64 to 128; the rule is not made for wider ones (500 rows of 32 heads of 256: 55 and 42,
-    // 700 of 16: 47 and 52) nor for short windows (1 900 rows of 32 heads of 80 that see 100: 35 and 23).
+    // border is where they meet for heads of 64 to 128; of wider ones some calls take the slower (400 rows of 32 heads of 256: 40 and 34,
+    // 1 500 of 8: 60 and 70).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
     int blocks = seen(KV_STEP_ROWS);
     const int chip = wide ? 256 : 512;  // workgroups of the step kernel at a time: registers for one to a compute unit, or two
@@ -1056,7 +1056,11 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     // saved at about 8 000 (64 sequences of 300 positions, 8 heads, one of 500 rows and the others of one: 38 us against 40 by the
     // kernel for many rows; of 700: 47 against 40; 256 sequences, one of 2 048 rows that see 128 positions: 205 against 35).
     const long long launched = p.n_seqs * ((rows + KV_STEP_ROWS - 1) / KV_STEP_ROWS) * p.heads;
-    if (rows <= KV_STEP_ROWS || (few * (blocks > 1 ? blocks : 1) <= 24576 && launched - few <= 8192)) {
+    // More than two rounds of it, where tiles of 128 rows are half as many or fewer: their starts are what short windows and sequences have
+    // (12 times 100 rows of 24 heads that see 100 positions 36 us, 24 by the other; 1 900 of 32 heads of 80 that see 100 35 and 23; 10
+    // times 200 rows of 40 heads over themselves 54 and 38; 7 times about 240 of 16/2 heads of 256 93 and 44).
+    const bool rounds = few > 2 * chip && few >= 2 * tiles(128) * p.heads;
+    if (rows <= KV_STEP_ROWS || (few * (blocks > 1 ? blocks : 1) <= 24576 && launched - few <= 8192 && !rounds)) {
         // One workgroup to a compute unit: two to each read no faster and have more to join (one row over 4 000 positions of 32 heads
         // in 8 parts 11.8 us, in 16 13.4; 40 over 16 000 of 8 in 16 parts 19.3, in 32 22.8).  Sequences may differ in length, so
         // that parts of some end early: there, as many as the chip holds (the eight above in 4 parts 33 us, in 7 25; of wide heads no more

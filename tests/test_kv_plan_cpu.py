@@ -109,3 +109,12 @@ def test_parts_of_several_sequences_are_one_round(L, d, most):
     for seqs, rows, length, heads_q, heads in [(8, 6, 4000, 16, 2), (2, 1, 100000, 16, 2), (30, 1, 3000, 16, 2), (3, 1, 5000, 16, 16), (32, 5, 1000, 16, 2)]:
         tile, parts, _, workgroups = plan(L, seqs, seqs * rows, rows, length, heads_q, heads, d)
         assert tile == 32 and parts > 1 and most * 3 // 4 <= workgroups <= most, (seqs, parts, workgroups)
+
+
+@pytest.mark.parametrize("seqs, rows, length, heads_q, heads, d, window, tile", [
+    (12, 100, 1000, 24, 24, 128, 100, 128), (1, 1900, 1900, 32, 32, 80, 100, 128), (10, 200, 200, 40, 40, 128, 0, 128), (7, 301, 350, 16, 2, 256, 0, 128),
+    (1, 1000, 1000, 32, 32, 256, 100, 128), (1, 3000, 3000, 48, 1, 128, 16, 128),
+    # two rounds, or fewer; tiles that a kernel with larger ones would have as many of
+    (1, 1000, 1000, 32, 32, 128, 100, 32), (1, 500, 500, 16, 16, 256, 0, 32), (100, 33, 33, 3, 3, 128, 0, 32), (200, 30, 90, 40, 40, 128, 0, 32)])
+def test_rounds_of_the_kernel_for_few_rows(L, seqs, rows, length, heads_q, heads, d, window, tile):
+    assert plan(L, seqs, seqs * rows, rows, length, heads_q, heads, d, window)[0] == tile
