@@ -1047,8 +1047,8 @@ KvPlan kv_plan(const Kv& p, int heads_q, int window)
     // converts a block once for every 32 rows, but starts and ends in a third of the time.  By it and by the kernel for many rows: eight
     // times 5 tokens of 48 heads that share keys over 1 000 to 9 000 positions 27 us and 42; 7 tokens, all over 9 000, 38 and 41; 500 rows
     // of 32 heads over themselves 17 and 23, 700 26 and 27, 1 000 33 and 30, 2 048 83 and 59; 4 times 64 of 32 over 2 900 41 and 42.  The
-    // border is where they meet for heads of 64 to 128; of wider ones some calls take the slower (400 rows of 32 heads of 256: 40 and 34,
-    // 1 500 of 8: 60 and 70).
+    // border is where they meet for heads of 64 to 128; of wider ones some calls would be faster by the other (400 rows of 32 heads of 256
+    // 40 and 34, 500 54 and 42), others not (700 of 16 47 and 52, 1 500 of 8 60 and 70).
     const long long few = tiles(KV_STEP_ROWS) * p.heads;
     int blocks = seen(KV_STEP_ROWS);
     const int chip = wide ? 256 : 512;  // workgroups of the step kernel at a time: registers for one to a compute unit, or two
