@@ -250,7 +250,7 @@ def run(state):
         state["kv_len"][case["seqs"] - case["ends"]:] = case["length"]
         L.kv_reserve(pool, seqs, state["row_start"], moves)
     else:
-        L.kv_reserve(pool, seqs, state["row_start"], moves)
+        L.kv_reserve(pool, seqs, state["row_start"], moves, more=True)
         for cache in state["caches"]:
             L.kv_copy(cache, moves)
     return _held(state)
@@ -338,7 +338,7 @@ def _plain_reserve(state):
     first = (old // page)[:, None]
     due = (j >= first) & (j < (-(-length // page))[:, None]) & (old < length)[:, None]
     missing = due & (pages < 0)
-    closing = (j * per < (length // BLOCK)[:, None]) & ((j + 1) * per > (old // BLOCK)[:, None])
+    closing = torch.maximum(j * per, (old // BLOCK)[:, None]) < torch.minimum((j + 1) * per, (length // BLOCK)[:, None])
     shared = due & ~missing & closing & (refs[pages.clamp(min=0)] > 1)
     here = shared & (j == first)
     at = torch.where(here, pages, len(refs)).flatten()  # (a page behind the last stands for none)
