@@ -264,7 +264,8 @@ def _plain_select(state):
     x = state["logits"].double()  # in 64 bits: which of two scores is the larger hangs on their last bits
     cum = state["scores"].double()[:, None]
     top = x.amax(1, keepdim=True)
-    x = cum + (x - ((x - top).exp().sum(1, keepdim=True).log() + top))
+    x = x - top
+    x = cum + (x - x.exp().sum(1, keepdim=True).log())
     done = state["ended"][:, None] > 0
     x.masked_fill_(done, float("-inf"))
     x[:, eos] = torch.where(done, cum, x[:, eos:eos + 1])[:, 0]
