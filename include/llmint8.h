@@ -321,6 +321,107 @@ int llmint8_kv_attention(const llmint8_kv_cache_t *cache, const llmint8_kv_batch
 int llmint8_kv_read(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *batch, void *k_out_f16, void *v_out_f16,
                     llmint8_stream_t stream);
 
+/* ---- pages and sequences of the cache ----------------------------------------------------------------------------------
+ * The cache's pages as a pool that sequences take pages from, share, and give back, all of it on the device: a step of a decoder
+ * that forks its sequences (beam search, several samples from a prompt) waits for no host and can be captured.  The tables are the
+ * same for all layers of a model: llmint8_kv_fork, _kv_reserve and _kv_compact change them, once a step, and write down what has to
+ * be copied; llmint8_kv_copy does that copying in one layer's cache, so it is called once a layer, before kv_append and before the
+ * next call that changes the tables.
+ *
+ *   refs   [n_pages]  how many table entries name a page.  0: the page is free.  (More than that keeps a page from being freed:
+ *                     a program may hold a page by adding to it.)  All zero to begin with
+ *   pages  [n_seqs][page_stride]  the sequences' tables: an entry that is negative names no page.  All negative to begin with
+ *   kv_len [n_seqs]   positions; 0: the sequence is idle
+ *   slots  [n_seqs]   slots of the ring, a different one for each sequence, idle ones too
+ *   status            one word, or NULL: LLMINT8_KV_BAD_BATCH, LLMINT8_KV_BAD_PAGE, LLMINT8_KV_NO_PAGE (see the calls)
+ * Every sequence that may name pages of the pool is one of n_seqs <= LLMINT8_KV_MAX_SEQS; pages, kv_len and slots are what
+ * llmint8_kv_batch_t names, too.  n_pages and page_stride <= LLMINT8_KV_MAX_PAGES, page_tokens <= 2^20.
+ *
+ *   moves: what is to be copied.  pages [max_pages][4]: from, to, blocks (the first ones of the page, of every head), 0;
+ *          slots [max_slots][4]: from, to, first position, positions;  count [2]: how many of both.  pages and slots start on 16
+ *          bytes.  A call says below which capacity it is refused.                                                            */
+#define LLMINT8_KV_MAX_SEQS 2048
+#define LLMINT8_KV_MAX_PAGES (1 << 18)
+enum { LLMINT8_KV_NO_PAGE = 8 };
+typedef struct {
+    int32_t *refs;
+    int n_pages, page_tokens;
+} llmint8_kv_pool_t;
+typedef struct {
+    int32_t *pages;
+    int32_t *kv_len;
+    int32_t *slots;
+    int32_t *status;
+    int n_seqs, page_stride;
+} llmint8_kv_seqs_t;
+typedef struct {
+    int32_t *pages;
+    int32_t *slots;
+    int32_t *count;
+    int max_pages, max_slots;
+} llmint8_kv_moves_t;
+
+/* Sequence i goes on from sequence parent[i] (its own number: it stays as it is), or, parent[i] = -1, ends and is idle: its table,
+ * length and what its slot holds become the parent's.  Sequences without children give their pages back.  Nothing of a page is
+ * copied: children share the parent's (llmint8_kv_reserve gives them pages of their own when they would write to them).  The first
+ * child has the parent's slot; the others, then the sequences that end, get those of sequences without children, all in order.  The
+ * ring's positions that the others need, those behind the last full block and the 32 before them, are noted in moves: a child may
+ * be shortened as llmint8_kv_batch_t says, as if it had never been longer than it is.
+ * grow >= 0: positions that are added to every length above 0 afterwards (the next token's).
+ * A parent that does not exist counts as -1, a table entry that names no page of the pool as negative; a length that cannot be goes on
+ * as it is, with nothing copied; all are told of in status.  moves: a new list; max_slots >= n_seqs.                          */
+int llmint8_kv_fork(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *seqs, const int32_t *parent, int grow,
+                    const llmint8_kv_moves_t *moves, llmint8_stream_t stream);
+
+/* Gives every sequence pages for its next tokens, before llmint8_kv_append: sequence b brings row_start[b+1] - row_start[b] of them,
+ * its last positions (kv_len includes them).  Pages that these positions lack are taken from the pool, the lowest free ones first, in
+ * order of sequences and positions.  A page that a block which gets full by these tokens will be written to, and that others
+ * hold too, is replaced by one of the sequence's own; the first such page's blocks before the tokens' are noted in moves.  (If all
+ * that hold a page are to be given another for their first tokens, the last sequence keeps it.)  Pages that are given back here
+ * are given out by later calls only.
+ * Too few free pages: a sequence that with those before it needs more than there are gets none, its table stays as it is, and
+ * status has LLMINT8_KV_NO_PAGE.  llmint8_kv_append must not have such a sequence: it would write to pages that others hold.
+ *   ready  NULL, or [n_seqs]: kv_len of the sequences that have their pages, 0 of the others and of those whose
+ *          row_start or kv_len cannot be (LLMINT8_KV_BAD_BATCH): as the kv_len of a batch it leaves these out
+ *   more   0: moves is a new list; else the list of a llmint8_kv_fork before goes on
+ * max_pages >= n_seqs.                                                                                                         */
+int llmint8_kv_reserve(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *seqs, const int32_t *row_start, int32_t *ready,
+                       int more, const llmint8_kv_moves_t *moves, llmint8_stream_t stream);
+
+/* Moves pages so that the U pages in use are pages 0 .. U-1: those above go, in order, to the free ones below, in order; tables and
+ * refs follow.  used: NULL, or one word that gets U.  moves: a new list; max_pages >= n_pages / 2.                              */
+int llmint8_kv_compact(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *seqs, int32_t *used,
+                       const llmint8_kv_moves_t *moves, llmint8_stream_t stream);
+
+/* Copies in one layer's cache what moves says.  No destination may be a source, or another entry's destination, which lists of the
+ * calls above never have; a page or slot that the cache does not have, or a count of blocks or positions that cannot be, is left
+ * out and told of in status (one word, or NULL): LLMINT8_KV_BAD_PAGE, LLMINT8_KV_BAD_BATCH.                                    */
+int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *moves, int32_t *status, llmint8_stream_t stream);
+
+/* ---- beam search ---------------------------------------------------------------------------------------------------------
+ * The n_out best continuations of each item's beams: beam b of an item (row item * beams + b) with token t has the score
+ * scores[row] + logits[row][t] - log(sum over t of exp(logits[row][t])); the largest are given, in falling order, equal ones in order
+ * of (b, t).  The order is that of these numbers in 64 bits (sums of 32 bits are made again in 64 where two beams' scores are
+ * too near to tell); scores_out is rounded to fp32.
+ *   logits      in   fp16, or with f32 != 0 fp32; row r at r * ld, ld >= vocab.  -inf: a token that cannot follow
+ *   scores      in   [items * beams] fp32.  -inf: a beam that there is not; its logits are not read
+ *   ended       in   NULL, or [items * beams]: not 0: the beam has ended: its only continuation is the token eos, its score stays as
+ *                    it is, its logits are not read
+ *   eos              the token that ends a beam, or -1 (with ended NULL): none
+ *   scores_out, parent, token  out  [items][n_out]; parent is the row (what llmint8_kv_fork takes).  Where there are fewer
+ *                    continuations: -inf, parent -1, token eos (0 if eos is -1)
+ *   ended_out   out  NULL, or [items][n_out]: 1 if the beam had ended or its token is eos, or where there is no continuation; else 0
+ *   status      one word, or NULL: LLMINT8_BEAM_NOT_FINITE is set (never cleared) if a row that is read holds NaN or +inf, or a score is
+ *                    NaN or +inf.  Such a beam has no continuations
+ * beams and n_out up to LLMINT8_BEAM_MAX.  scores_out may be scores and ended_out may be ended, if n_out = beams.
+ *   ws               llmint8_beam_select_workspace_bytes(items, beams, vocab, n_out) bytes; 0: sizes that are refused           */
+#define LLMINT8_BEAM_MAX 32
+enum { LLMINT8_BEAM_NOT_FINITE = 1 };
+size_t llmint8_beam_select_workspace_bytes(int items, int beams, int vocab, int n_out);
+int llmint8_beam_select(const void *logits, int64_t ld, int f32, int items, int beams, int vocab, const float *scores,
+                        const int32_t *ended, int eos, int n_out, float *scores_out, int32_t *parent, int32_t *token,
+                        int32_t *ended_out, int32_t *status, void *ws, size_t ws_bytes, llmint8_stream_t stream);
+
 /* Measurement support: the ceilings the roofline fractions are held against, measured on the box itself.
  * llmint8_probe_mfma: one workgroup per compute unit runs a register-only issue loop of the int8 MFMA
  *   (16 x 16 x 64) in the shape of the prefill GEMM's main loop (Eq. 7: eight waves, 8 x 4 accumulator tiles each,

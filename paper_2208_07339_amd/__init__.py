@@ -14,4 +14,6 @@ from .binding import (  # noqa: F401
     GRANULARITY, ZpWeight, ZpRows, zp_quantize_weight, zp_quantize_rows, zp_matmul, zp_linear,
     KvCache, KvBatch, kv_append, kv_attention, kv_attention_workspace, kv_read, debug_kv_plan_for,
     KV_BLOCK, KV_RING, KV_MAX_D, KV_BAD_BATCH, KV_BAD_PAGE, KV_NOT_FINITE,
+    KvPool, KvSeqs, KvMoves, kv_fork, kv_reserve, kv_compact, kv_copy, KV_MAX_SEQS, KV_MAX_PAGES, KV_NO_PAGE,
+    beam_select, beam_select_workspace, BEAM_MAX, BEAM_NOT_FINITE,
 )

@@ -20,6 +20,8 @@ SYMBOLS = [
     "llmint8_debug_weight_reads_for",
     "llmint8_kv_codes_bytes", "llmint8_kv_consts_bytes", "llmint8_kv_ring_bytes", "llmint8_kv_append",
     "llmint8_kv_attention_workspace_bytes", "llmint8_kv_attention", "llmint8_kv_read", "llmint8_debug_kv_plan_for",
+    "llmint8_kv_fork", "llmint8_kv_reserve", "llmint8_kv_compact", "llmint8_kv_copy",
+    "llmint8_beam_select_workspace_bytes", "llmint8_beam_select",
 ]
 
 _lib = None
@@ -35,6 +37,19 @@ class _KvBatch(C.Structure):  # llmint8_kv_batch_t
     _fields_ = [("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("slots", C.c_void_p),
                 ("status", C.c_void_p), ("n_seqs", C.c_int), ("n_rows", C.c_int), ("page_stride", C.c_int),
                 ("max_rows", C.c_int), ("max_len", C.c_int)]
+
+
+class _KvPool(C.Structure):  # llmint8_kv_pool_t
+    _fields_ = [("refs", C.c_void_p), ("n_pages", C.c_int), ("page_tokens", C.c_int)]
+
+
+class _KvSeqs(C.Structure):  # llmint8_kv_seqs_t
+    _fields_ = [("pages", C.c_void_p), ("kv_len", C.c_void_p), ("slots", C.c_void_p), ("status", C.c_void_p), ("n_seqs", C.c_int),
+                ("page_stride", C.c_int)]
+
+
+class _KvMoves(C.Structure):  # llmint8_kv_moves_t
+    _fields_ = [("pages", C.c_void_p), ("slots", C.c_void_p), ("count", C.c_void_p), ("max_pages", C.c_int), ("max_slots", C.c_int)]
 
 
 class KvPlan(C.Structure):  # llmint8_kv_plan_t
@@ -142,6 +157,19 @@ def lib():
     L.llmint8_debug_kv_plan_for.argtypes = [batch, i32, i32, i32, i32, C.POINTER(KvPlan)]
     L.llmint8_kv_read.restype = i32
     L.llmint8_kv_read.argtypes = [cache, batch, vp, vp, vp]
+    pool, seqs, moves = C.POINTER(_KvPool), C.POINTER(_KvSeqs), C.POINTER(_KvMoves)
+    L.llmint8_kv_fork.restype = i32
+    L.llmint8_kv_fork.argtypes = [pool, seqs, vp, i32, moves, vp]
+    L.llmint8_kv_reserve.restype = i32
+    L.llmint8_kv_reserve.argtypes = [pool, seqs, vp, vp, i32, moves, vp]
+    L.llmint8_kv_compact.restype = i32
+    L.llmint8_kv_compact.argtypes = [pool, seqs, vp, moves, vp]
+    L.llmint8_kv_copy.restype = i32
+    L.llmint8_kv_copy.argtypes = [cache, moves, vp, vp]
+    L.llmint8_beam_select_workspace_bytes.restype = sz
+    L.llmint8_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.llmint8_beam_select.restype = i32
+    L.llmint8_beam_select.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -604,6 +632,158 @@ def kv_read(cache, batch, k=None, v=None):
         assert t is None or (t.dtype == _f16 and t.shape == shape and t.is_contiguous() and t.is_cuda)
     _check(lib().llmint8_kv_read(cache._c, batch._c, _ptr(k), _ptr(v), _stream()))
     return k, v
+
+
+# ---- pages and sequences of the cache ------------------------------------------------
+
+KV_MAX_SEQS, KV_MAX_PAGES = 2048, 1 << 18  # LLMINT8_KV_MAX_SEQS / _PAGES
+KV_NO_PAGE = 8  # a bit of a status word, as KV_BAD_BATCH
+
+
+def _words(device, *tensors):
+    """The tensors that there are: int32 words, one after the other, on `device`."""
+    torch = _torch()
+    assert device.type == "cuda" and all(t.dtype == torch.int32 and t.is_contiguous() and t.device == device for t in tensors if t is not None)
+
+
+def _here(device):
+    """The current device's current stream, for tensors on `device`: work on another device's is not what the caller means."""
+    if _torch().cuda.current_device() != device.index:
+        raise Llmint8Error(f"the tensors are on {device}, which is not the current device")
+    return _stream()
+
+
+@dataclass(frozen=True)
+class KvPool:
+    """The pages that sequences take, share and give back (llmint8_kv_pool_t)."""
+    refs: object      # int32 [n_pages]: table entries that name a page
+    page_tokens: int
+
+    def __post_init__(self):
+        _words(self.refs.device, self.refs)
+        assert self.refs.dim() == 1
+        object.__setattr__(self, "_c", _KvPool(_ptr(self.refs), self.refs.numel(), self.page_tokens))
+        lib()
+
+    @staticmethod
+    def allocate(n_pages, page_tokens, device="cuda"):
+        return KvPool(_torch().zeros(n_pages, dtype=_torch().int32, device=device), page_tokens)
+
+
+@dataclass(frozen=True)
+class KvSeqs:
+    """Sequences with their pages, lengths and ring slots (llmint8_kv_seqs_t); a KvBatch of them has the same tensors."""
+    pages: object    # int32 [n_seqs, most pages of a sequence], negative: none
+    kv_len: object   # int32 [n_seqs]
+    slots: object    # int32 [n_seqs], all different
+    status: object = None  # int32 [1], or None
+
+    def __post_init__(self):
+        _words(self.pages.device, self.pages, self.kv_len, self.slots, self.status)
+        n, stride = self.pages.shape
+        assert self.kv_len.shape == self.slots.shape == (n,)
+        c = _KvSeqs(_ptr(self.pages), _ptr(self.kv_len), _ptr(self.slots), _ptr(self.status), n, stride)
+        object.__setattr__(self, "_c", c)
+
+    @staticmethod
+    def allocate(n_seqs, most_pages, device="cuda"):
+        """Idle sequences."""
+        torch = _torch()
+        return KvSeqs(torch.full((n_seqs, most_pages), -1, dtype=torch.int32, device=device),
+                      torch.zeros(n_seqs, dtype=torch.int32, device=device), torch.arange(n_seqs, dtype=torch.int32, device=device),
+                      torch.zeros(1, dtype=torch.int32, device=device))
+
+
+@dataclass(frozen=True)
+class KvMoves:
+    """What kv_copy is to copy (llmint8_kv_moves_t)."""
+    pages: object  # int32 [max_pages, 4]: from, to, blocks, 0
+    slots: object  # int32 [max_slots, 4]: from, to, first position, positions
+    count: object  # int32 [2]: how many of both
+
+    def __post_init__(self):
+        _words(self.pages.device, self.pages, self.slots, self.count)
+        assert self.pages.dim() == self.slots.dim() == 2 and self.pages.shape[1] == self.slots.shape[1] == 4 and self.count.numel() == 2
+        c = _KvMoves(_ptr(self.pages), _ptr(self.slots), _ptr(self.count), self.pages.shape[0], self.slots.shape[0])
+        object.__setattr__(self, "_c", c)
+
+    @staticmethod
+    def allocate(max_pages, max_slots, device="cuda"):
+        """max_pages: n_seqs for kv_reserve, n_pages / 2 for kv_compact; max_slots: n_seqs for kv_fork."""
+        return KvMoves(*(_torch().zeros(shape, dtype=_torch().int32, device=device) for shape in ((max(1, max_pages), 4), (max_slots, 4), 2)))
+
+
+def _pool_calls(pool, seqs, moves):
+    assert pool.refs.device == seqs.pages.device == moves.count.device
+    return pool._c, seqs._c
+
+
+def kv_fork(pool, seqs, parent, moves, grow=0):
+    """llmint8_kv_fork: sequence i goes on from sequence parent[i] (int32 [n_seqs]); -1: it ends."""
+    _words(seqs.pages.device, parent)
+    assert parent.numel() == seqs.kv_len.numel()
+    _check(lib().llmint8_kv_fork(*_pool_calls(pool, seqs, moves), _ptr(parent), grow, moves._c, _here(seqs.pages.device)))
+
+
+def kv_reserve(pool, seqs, row_start, moves, ready=None, more=False):
+    """llmint8_kv_reserve: pages for the sequences' next tokens, their own where they write; row_start int32 [n_seqs + 1].
+    ready: int32 [n_seqs], or None.  more: the list of a kv_fork before goes on."""
+    _words(seqs.pages.device, row_start, ready)
+    n = seqs.kv_len.numel()
+    assert row_start.numel() == n + 1 and (ready is None or ready.numel() == n)
+    _check(lib().llmint8_kv_reserve(*_pool_calls(pool, seqs, moves), _ptr(row_start), _ptr(ready), int(more), moves._c,
+                                    _here(seqs.pages.device)))
+
+
+def kv_compact(pool, seqs, moves, used=None):
+    """llmint8_kv_compact: the pages in use become the first ones; used: int32 [1] for their number, or None."""
+    _words(seqs.pages.device, used)
+    _check(lib().llmint8_kv_compact(*_pool_calls(pool, seqs, moves), _ptr(used), moves._c, _here(seqs.pages.device)))
+
+
+def kv_copy(cache, moves, status=None):
+    """llmint8_kv_copy: the moves' copies in one layer's cache."""
+    _words(cache.codes.device, moves.count, status)
+    _check(lib().llmint8_kv_copy(cache._c, moves._c, _ptr(status), _here(cache.codes.device)))
+
+
+# ---- beam search -----------------------------------------------------------------------
+
+BEAM_MAX = 32           # LLMINT8_BEAM_MAX
+BEAM_NOT_FINITE = 1     # a bit of beam_select's status word
+
+
+def beam_select_workspace(items, beams, vocab, n_out, device="cuda"):
+    """Scratch of beam_select for these sizes: kept from call to call."""
+    n = lib().llmint8_beam_select_workspace_bytes(items, beams, vocab, n_out)
+    return Workspace(_torch().empty(n, dtype=_torch().uint8, device=device))
+
+
+def beam_select(logits, scores, beams, n_out=None, ended=None, eos=-1, ws=None, out=None, status=None):
+    """llmint8_beam_select: logits [items * beams, vocab] fp16 or fp32 (rows may be slices of wider ones), scores fp32
+    [items * beams], ended int32 [items * beams] or None -> (scores fp32, parent, token, ended int32), each [items, n_out]
+    (n_out: beams if None).  out: those four; its scores may be `scores` and its ended `ended` where n_out is beams."""
+    torch = _torch()
+    rows, vocab = logits.shape
+    dev = logits.device
+    n_out = beams if n_out is None else n_out
+    assert beams >= 1 and rows % beams == 0 and logits.is_cuda and logits.dtype in (torch.float16, torch.float32)
+    assert logits.stride(1) == 1 or vocab == 1
+    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.device == dev
+    assert ended is None or ended.numel() == rows
+    items = rows // beams
+    if out is None:
+        out = (torch.empty((items, n_out), device=dev), *(torch.empty((items, n_out), dtype=torch.int32, device=dev) for _ in range(3)))
+    _words(dev, *out[1:], ended, status)
+    assert out[0].dtype == torch.float32 and out[0].is_contiguous() and out[0].device == dev
+    assert all(t is None or t.numel() == items * n_out for t in out)
+    if ws is None:
+        ws = beam_select_workspace(items, beams, vocab, n_out, dev)
+    assert ws.buf.device == dev
+    _check(lib().llmint8_beam_select(_ptr(logits), logits.stride(0) if rows > 1 else vocab, int(logits.dtype == torch.float32), items,
+                                     beams, vocab, _ptr(scores), _ptr(ended), eos, n_out, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
+                                     _ptr(out[3]), _ptr(status), _ptr(ws.buf), ws.nbytes, _here(dev)))
+    return out
 
 
 def export_weight(qw):

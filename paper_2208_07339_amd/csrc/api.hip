@@ -6,7 +6,9 @@
 
 #include "../../include/llmint8.h"
 #include "common.h"
+#include "beams.h"
 #include "kv.h"
+#include "kv_pages.h"
 
 using namespace llmint8;
 
@@ -680,6 +682,93 @@ int llmint8_kv_read(const llmint8_kv_cache_t* cache, const llmint8_kv_batch_t* b
     if (bad) return bad;
     if ((!k_out_f16 && !v_out_f16) || misaligned(k_out_f16, 2) || misaligned(v_out_f16, 2)) return LLMINT8_INVALID_ARG;
     return hip_status(launch_kv_read(kv_args(cache, batch), k_out_f16, v_out_f16, (hipStream_t)stream));
+}
+
+// ---- pages and sequences of the cache ----
+
+static int kv_pool_check(const llmint8_kv_pool_t* p, const llmint8_kv_seqs_t* s, const llmint8_kv_moves_t* m)
+{
+    if (!p || !s || !m || !p->refs || !s->pages || !s->kv_len || !s->slots || !m->pages || !m->slots || !m->count) return LLMINT8_INVALID_ARG;
+    const uintptr_t words = (uintptr_t)p->refs | (uintptr_t)s->pages | (uintptr_t)s->kv_len | (uintptr_t)s->slots | (uintptr_t)s->status | (uintptr_t)m->count;
+    if (words & 3 || ((uintptr_t)m->pages | (uintptr_t)m->slots) & 15) return LLMINT8_INVALID_ARG;
+    if (p->n_pages < 1 || p->page_tokens < 1 || s->n_seqs < 1 || s->page_stride < 1 || m->max_pages < 1 || m->max_slots < 1) return LLMINT8_INVALID_ARG;
+    if (p->page_tokens % KV_BLOCK || p->page_tokens > KV_MAX_PAGE || p->n_pages > LLMINT8_KV_MAX_PAGES || s->n_seqs > LLMINT8_KV_MAX_SEQS ||
+        s->page_stride > LLMINT8_KV_MAX_PAGES)
+        return LLMINT8_SHAPE;
+    return LLMINT8_OK;
+}
+
+int llmint8_kv_fork(const llmint8_kv_pool_t* pool, const llmint8_kv_seqs_t* seqs, const int32_t* parent, int grow,
+                    const llmint8_kv_moves_t* moves, llmint8_stream_t stream)
+{
+    const int bad = kv_pool_check(pool, seqs, moves);
+    if (bad) return bad;
+    if (!parent || misaligned(parent, 4) || parent == seqs->kv_len || parent == seqs->slots || grow < 0 || moves->max_slots < seqs->n_seqs)
+        return LLMINT8_INVALID_ARG;
+    if (grow > KV_MAX_LEN / 4) return LLMINT8_SHAPE;
+    return hip_status(launch_kv_fork(*pool, *seqs, parent, grow, *moves, (hipStream_t)stream));
+}
+
+int llmint8_kv_reserve(const llmint8_kv_pool_t* pool, const llmint8_kv_seqs_t* seqs, const int32_t* row_start, int32_t* ready,
+                       int more, const llmint8_kv_moves_t* moves, llmint8_stream_t stream)
+{
+    const int bad = kv_pool_check(pool, seqs, moves);
+    if (bad) return bad;
+    if (!row_start || misaligned(row_start, 4) || misaligned(ready, 4) || moves->max_pages < seqs->n_seqs || (ready && (ready == seqs->kv_len || ready == row_start)))
+        return LLMINT8_INVALID_ARG;
+    return hip_status(launch_kv_reserve(*pool, *seqs, row_start, ready, more != 0, *moves, (hipStream_t)stream));
+}
+
+int llmint8_kv_compact(const llmint8_kv_pool_t* pool, const llmint8_kv_seqs_t* seqs, int32_t* used,
+                       const llmint8_kv_moves_t* moves, llmint8_stream_t stream)
+{
+    const int bad = kv_pool_check(pool, seqs, moves);
+    if (bad) return bad;
+    if (misaligned(used, 4) || moves->max_pages < pool->n_pages / 2) return LLMINT8_INVALID_ARG;
+    return hip_status(launch_kv_compact(*pool, *seqs, used, *moves, (hipStream_t)stream));
+}
+
+int llmint8_kv_copy(const llmint8_kv_cache_t* c, const llmint8_kv_moves_t* m, int32_t* status, llmint8_stream_t stream)
+{
+    if (!c || !m || !c->codes || !c->consts || !c->ring || !m->pages || !m->slots || !m->count) return LLMINT8_INVALID_ARG;
+    if (((uintptr_t)c->codes | (uintptr_t)c->consts | (uintptr_t)c->ring | (uintptr_t)m->pages | (uintptr_t)m->slots) & 15 || misaligned(m->count, 4) ||
+        misaligned(status, 4))
+        return LLMINT8_INVALID_ARG;
+    if (c->n_pages < 1 || c->page_tokens < 1 || c->n_slots < 1 || c->heads < 1 || c->d < 1 || m->max_pages < 1 || m->max_slots < 1)
+        return LLMINT8_INVALID_ARG;
+    const int64_t most = m->max_pages > m->max_slots ? m->max_pages : m->max_slots;
+    if (c->page_tokens % KV_BLOCK || c->page_tokens > KV_MAX_PAGE || c->d > KV_MAX_D || c->heads > 65535 || 2 * most * c->heads >= (1ll << 31))
+        return LLMINT8_SHAPE;
+    return hip_status(launch_kv_copy(*c, *m, status, (hipStream_t)stream));
+}
+
+// ---- beam search ----
+
+static bool beam_sizes(int items, int beams, int vocab, int n_out)
+{
+    return items >= 1 && beams >= 1 && vocab >= 1 && n_out >= 1 && beams <= LLMINT8_BEAM_MAX && n_out <= LLMINT8_BEAM_MAX &&
+           (int64_t)items * beams * beam_parts(items * (int64_t)beams, vocab) < (1ll << 31);
+}
+
+size_t llmint8_beam_select_workspace_bytes(int items, int beams, int vocab, int n_out)
+{
+    return beam_sizes(items, beams, vocab, n_out) ? beam_ws((int64_t)items * beams, vocab, n_out) : 0;
+}
+
+int llmint8_beam_select(const void* logits, int64_t ld, int f32, int items, int beams, int vocab, const float* scores,
+                        const int32_t* ended, int eos, int n_out, float* scores_out, int32_t* parent, int32_t* token,
+                        int32_t* ended_out, int32_t* status, void* ws, size_t ws_bytes, llmint8_stream_t stream)
+{
+    if (!logits || !scores || !scores_out || !parent || !token || misaligned(logits, f32 ? 4 : 2) || misaligned(scores, 4) || misaligned(ended, 4) ||
+        misaligned(scores_out, 4) || misaligned(parent, 4) || misaligned(token, 4) || misaligned(ended_out, 4) || misaligned(status, 4))
+        return LLMINT8_INVALID_ARG;
+    if (items < 1 || beams < 1 || vocab < 1 || n_out < 1 || ld < vocab || eos < -1 || eos >= vocab || (ended && eos < 0)) return LLMINT8_INVALID_ARG;
+    // in place only where an item's results take the place of what it read
+    if ((scores_out == scores || (ended && ended_out == ended)) && n_out != beams) return LLMINT8_INVALID_ARG;
+    if (!beam_sizes(items, beams, vocab, n_out)) return LLMINT8_SHAPE;
+    if (!ws || ws_bytes < beam_ws((int64_t)items * beams, vocab, n_out)) return LLMINT8_WORKSPACE;
+    const BeamArgs a = {logits, ld, items, beams, vocab, scores, ended, eos, n_out, scores_out, parent, token, ended_out, status};
+    return hip_status(launch_beam_select(a, f32 != 0, ws_base(ws), (hipStream_t)stream));
 }
 
 }  // extern "C"
