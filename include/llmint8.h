@@ -341,7 +341,7 @@ int llmint8_kv_read(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *b
  *          slots [max_slots][4]: from, to, first position, positions;  count [2]: how many of both.  pages and slots start on 16
  *          bytes.  A call says below which capacity it is refused.                                                            */
 #define LLMINT8_KV_MAX_SEQS 2048
-#define LLMINT8_KV_MAX_PAGES (1 << 18)
+#define LLMINT8_KV_MAX_PAGES (1 << 17)
 enum { LLMINT8_KV_NO_PAGE = 8 };
 typedef struct {
     int32_t *refs;

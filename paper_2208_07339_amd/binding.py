@@ -636,7 +636,7 @@ def kv_read(cache, batch, k=None, v=None):
 
 # ---- pages and sequences of the cache ------------------------------------------------
 
-KV_MAX_SEQS, KV_MAX_PAGES = 2048, 1 << 18  # LLMINT8_KV_MAX_SEQS / _PAGES
+KV_MAX_SEQS, KV_MAX_PAGES = 2048, 1 << 17  # LLMINT8_KV_MAX_SEQS / _PAGES
 KV_NO_PAGE = 8  # a bit of a status word, as KV_BAD_BATCH
 
 

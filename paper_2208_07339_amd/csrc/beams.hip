@@ -1,7 +1,7 @@
 // beam_select: the best continuations of an item's beams, from their logits.
 //
 // s(b, t) = c_b + x_bt - lse_b, lse_b = log sum_t exp(x_bt).  Within a beam the order is that of the logits, which are exact; between
-// beams it hangs on the lse, sums in fp32 whose error is known (NEAR below): where two beams' scores are nearer than that, the sums
+// beams it hangs on the lse, sums in fp32 whose error is known (near_of): where two beams' scores are nearer than that, the sums
 // in question are made again in 64 bits.  So which tokens are picked does not hang on rounding.  Scores are c_b + ((x_bt - max) - log of
 // the sum against it): beams whose logits differ by a constant tie, as they should.
 //
@@ -12,7 +12,10 @@
 
 #include <float.h>
 
+#include <cmath>
+
 #include "kv.h"
+#include "wave.h"
 
 namespace llmint8 {
 
@@ -54,16 +57,11 @@ __device__ __forceinline__ float not_above_kth(float x, int k)
 
 __device__ __forceinline__ float wave_max(float x)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, d));
-    return x;
+    return wave_reduce(x, NONE, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
-template <class V>
-__device__ __forceinline__ V wave_sum(V x)
+__device__ __forceinline__ double wave_sum(double x)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    return x;
+    return wave_reduce(x, 0.0, [](double a, double b) { return a + b; });
 }
 
 // The k <= 64 best of what a wave is shown, best first, one to a lane: larger values, of equal ones the lower place.
@@ -97,6 +95,7 @@ struct Of;
 template <>
 struct Of<_Float16> {
     typedef h8v v8;
+    static constexpr float LOWEST = -65504.0f;
     static __device__ __forceinline__ v8 load(const _Float16* p) { return __builtin_bit_cast(h8v, load8((const unsigned short*)p)); }
     static __device__ __forceinline__ float largest(v8 v)
     {
@@ -104,10 +103,32 @@ struct Of<_Float16> {
         const h2 m = __builtin_bit_cast(h2, pk_max_f16(pk_max_f16(w[0], w[1]), pk_max_f16(w[2], w[3])));
         return __builtin_fmaxf((float)m[0], (float)m[1]);
     }
+    // sum of exp(x - M), M >= every x: 2^(x log2 e - r) with r = M log2 e rounded, which beyond() makes good.  A conversion, a product and a
+    // difference in one instruction, with one rounding.
+    struct Exp {
+        float r;
+        __device__ __forceinline__ explicit Exp(float M) : r(M * LOG2E) {}
+        __device__ __forceinline__ float of(v8 v) const
+        {
+            const u4 w = __builtin_bit_cast(u4, v);
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[1,0,0]" : "=v"(t[2 * e]) : "v"(w[e]), "s"(LOG2E), "v"(r));
+                asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(t[2 * e + 1]) : "v"(w[e]), "s"(LOG2E), "v"(r));
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) t[e] = __builtin_amdgcn_exp2f(t[e]);
+            return ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        }
+        // ln of what a sum against M is too large by
+        static __device__ __forceinline__ double beyond(float M) { return ((double)M * LOG2E - (double)(M * LOG2E)) * 0.69314718055994530942; }
+    };
 };
 template <>
 struct Of<float> {
     typedef f8v v8;
+    static constexpr float LOWEST = -FLT_MAX;
     typedef f8v at4 __attribute__((aligned(4)));
     static __device__ __forceinline__ v8 load(const float* p) { return *(const at4*)p; }
     static __device__ __forceinline__ float largest(v8 v)
@@ -117,6 +138,18 @@ struct Of<float> {
         for (int e = 1; e < 8; e++) m = __builtin_fmaxf(m, v[e]);
         return m;
     }
+    struct Exp {  // (products could be beyond fp32's range: the difference first)
+        float M;
+        __device__ __forceinline__ explicit Exp(float m) : M(m) {}
+        __device__ __forceinline__ float of(v8 v) const
+        {
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) t[e] = __builtin_amdgcn_exp2f((v[e] - M) * LOG2E);
+            return ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        }
+        static __device__ __forceinline__ double beyond(float) { return 0.0; }
+    };
 };
 
 // A row's beam has logits to look at.  (NaN and +inf as a score: beam_pick_kernel tells of it.)
@@ -126,47 +159,65 @@ __device__ __forceinline__ bool lives(const BeamArgs& a, long long row)
     return c > NONE && c <= FLT_MAX && !(a.ended && a.ended[row]);
 }
 
-constexpr int FEW = THREADS;  // what a piece's largest are picked from: most pieces have two to four times what they keep
+struct Sum {
+    double s;  // of the piece's exponentials against max
+    float max;
+};
+
+// Picks as integers in their order: larger logits, of equal ones the lower token (-0 and 0 are equal).
+__device__ __forceinline__ unsigned long long pick_key(const Pick& p)
+{
+    return (unsigned long long)order_key(p.x + 0.0f) << 32 | (unsigned)~p.t;
+}
+
+constexpr int SHOWN = 256;    // groups of 8 logits that a piece's largest are picked from
+constexpr int FEW = THREADS;  // those of their logits that are not below the bound: most pieces have two to four times what they keep
 
 // G groups of 8 logits to a thread: a wave's lanes side by side, the waves side by side, then the groups, so that a piece is
 // read in runs of 4 KiB (fp16).
 template <class T, int G>
-__global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, const Div parts, int keep, float2* __restrict__ sums, Pick* __restrict__ picks)
+__global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, const Div parts, int keep, Sum* __restrict__ sums, Pick* __restrict__ picks)
 {
-    __shared__ float s_max[WAVES], s_sum[WAVES], s_tau[WAVES];
-    __shared__ Pick few[FEW];
-    __shared__ int s_n;
     typedef Of<T> O;
+    typedef typename O::v8 v8;
+    __shared__ float s_max[WAVES], s_tau[WAVES];
+    __shared__ double s_sum[WAVES];
+    __shared__ v8 shown[SHOWN];
+    __shared__ int shown_at[SHOWN], s_shown, s_n;
+    __shared__ Pick few[FEW];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = parts.quot((int)blockIdx.x), part = (int)blockIdx.x - row * (int)parts.d;
     if (!lives(a, row)) return;
     const T* const src = (const T*)a.logits + row * a.ld;
-    const int base = part * (8 * THREADS * G) + 512 * w, vocab = a.vocab;
-    if (tid == 0) s_n = 0;
+    const int vocab = a.vocab, start = part * (8 * THREADS * G);
+    if (tid == 0) s_shown = 0, s_n = 0;
 
-    typename O::v8 x[G];
-    if ((part + 1) * (8ll * THREADS * G) <= vocab) {
+    // First token of group g of a lane.  The row's last piece: a group that reaches past the row's end is its last 8 tokens instead,
+    // without those that come before the group.
+    const bool last = vocab - start < 8 * THREADS * G;
+    auto meant = [&](int g, int l) { return start + g * (8 * THREADS) + 512 * w + 8 * l; };
+    auto first = [&](int g, int l) {
+        const int t = meant(g, l), most = vocab - 8;
+        return t < most ? t : most < 0 ? 0 : most;
+    };
+    v8 x[G];
+    if (vocab >= 8) {
 #pragma unroll
-        for (int g = 0; g < G; g++) x[g] = O::load(src + base + g * (8 * THREADS) + 8 * lane);
-    } else {  // the row's last piece
+        for (int g = 0; g < G; g++) x[g] = O::load(src + first(g, lane));
+        if (last) {
 #pragma unroll
-        for (int g = 0; g < G; g++) {
-            const long long at = (long long)base + g * (8 * THREADS);
-            if (at + 512 <= vocab) {
-                x[g] = O::load(src + at + 8 * lane);
-            } else {
+            for (int g = 0; g < G; g++) {
+                const int d = meant(g, lane) - first(g, lane);
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[g][e] = (T)NONE;
-                if (at < vocab) {
-                    T y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; e++) y[e] = src[at + 8 * lane + e < vocab ? at + 8 * lane + e : vocab - 1];
-#pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        if (at + 8 * lane + e < vocab) x[g][e] = y[e];
-                }
+                for (int e = 0; e < 8; e++)
+                    if (e < d) x[g][e] = (T)NONE;
             }
         }
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; g++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[g][e] = g == 0 && tid == 0 && e < vocab ? src[e < vocab ? e : 0] : (T)NONE;
     }
 
     float top[G], m = NONE;
@@ -175,45 +226,56 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
         top[g] = O::largest(x[g]);
         m = __builtin_fmaxf(m, top[g]);
     }
-    // (A mask of the type's lowest value is a logit like others: the reference is the maximum itself, -inf apart.)
-    const float M = __builtin_fmaxf(wave_max(m), -FLT_MAX);
-    float sum = 0.0f;
-#pragma unroll
-    for (int g = 0; g < G; g++) {
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) t[e] = __builtin_amdgcn_exp2f(((float)x[g][e] - M) * LOG2E);
-        sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
-    }
-    sum = wave_sum(sum);
-    const float tau_w = not_above_kth<12>(m, keep);
-    if (lane == 0) s_max[w] = M, s_sum[w] = sum, s_tau[w] = tau_w;
+    const float M_w = wave_max(m), tau_w = not_above_kth<16>(m, keep);
+    if (lane == 0) s_max[w] = M_w, s_tau[w] = tau_w;
     __syncthreads();
 
-    // Every wave has `keep` logits that are not below its own bound: nothing below the largest bound is wanted.
-    const float tau = __builtin_fmaxf(__builtin_fmaxf(s_tau[0], s_tau[1]), __builtin_fmaxf(s_tau[2], s_tau[3]));
+    // Every wave has `keep` logits that are not below its own bound: nothing below the largest bound is wanted.  The groups that have more
+    // go to LDS.
+    const float tau = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s_tau[0], s_tau[1]), __builtin_fmaxf(s_tau[2], s_tau[3])), -FLT_MAX);
+    int mine_shown = 0;
+#pragma unroll
+    for (int g = 0; g < G; g++) mine_shown += top[g] >= tau;
+    int slot = mine_shown ? atomicAdd(&s_shown, mine_shown) : 0;
 #pragma unroll
     for (int g = 0; g < G; g++)
-        if (__ballot(top[g] >= tau && top[g] > NONE)) {
+        if (top[g] >= tau) {
+            if (slot < SHOWN) shown[slot] = x[g], shown_at[slot] = first(g, lane);
+            slot++;
+        }
+
+    // (A mask of the type's lowest value is a logit like others: the reference is the maximum itself, -inf apart.)
+    const float M = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s_max[0], s_max[1]), __builtin_fmaxf(s_max[2], s_max[3])), O::LOWEST);
+    const typename O::Exp ex(M);
+    double sum = 0.0;
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float v = (float)x[g][e];
-                if (v >= tau && v > NONE) {
-                    const int at = atomicAdd(&s_n, 1);
-                    if (at < FEW) few[at] = {v, base + g * (8 * THREADS) + 8 * lane + e};
-                }
-            }
+    for (int g = 0; g < G; g++) sum += (double)ex.of(x[g]);
+    sum = wave_sum(sum);
+    if (lane == 0) s_sum[w] = sum;
+    __syncthreads();
+
+    const int groups = s_shown;
+    if (groups <= SHOWN)
+        for (int t0 = 64 * w; t0 < 8 * groups; t0 += THREADS) {
+            const int t = t0 + lane;
+            const float v = t < 8 * groups ? (float)((const T*)shown)[t] : NONE;
+            const unsigned long long hits = __ballot(v >= tau);
+            if (!hits) continue;
+            int base = 0;
+            if (v >= tau && !(hits & ((1ull << lane) - 1))) base = atomicAdd(&s_n, __popcll(hits));
+            base = lane_of(base, __ffsll(hits) - 1);
+            const int at = base + __popcll(hits & ((1ull << lane) - 1));
+            if (v >= tau && at < FEW) few[at] = {v, shown_at[t >> 3] + (t & 7)};
         }
     __syncthreads();
     int n = s_n;
-    if (n > FEW) {
-        // Many equal logits, or large ones side by side: each wave shows its own, group by group, best first, so that a group has at most
+    if (groups > SHOWN || n > FEW) {
+        // Many equal logits, or large ones far apart: each wave shows its own, group by group, best first, so that a group has at most
         // `keep` to add.
-        __syncthreads();
         Best<float, int> best(keep);
 #pragma unroll 1
         for (int g = 0; g < G; g++) {
-            typename O::v8 y = x[0];
+            v8 y = x[0];
 #pragma unroll
             for (int q = 1; q < G; q++)
                 if (q == g) y = x[q];
@@ -228,9 +290,10 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
                 if (!(V > best.last)) break;
                 const int l = __ffsll(__ballot(v == V)) - 1;
                 if (lane == l) left &= ~(1u << e);
-                best.add(V, base + g * (8 * THREADS) + 8 * l + __shfl(e, l));
+                best.add(V, first(g, l) + __shfl(e, l));
             }
         }
+        __syncthreads();
         if (lane < keep) few[w * keep + lane] = {best.v, best.at};
         n = WAVES * keep;
         __syncthreads();
@@ -238,52 +301,71 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
     const long long at = (long long)row * parts.d + part;
     const Pick mine = few[tid < n ? tid : 0];
     const bool counts = tid < n && mine.x > NONE;
-    int rank = 0;
-    for (int q = 0; q < n; q++) {
-        const Pick o = few[q];
-        rank += o.x > mine.x || (o.x == mine.x && o.t < mine.t);
+    if (64 * w < n) {
+        int rank = 0;
+        for (int q0 = 0; q0 < n; q0 += 64) {
+            const unsigned long long key = q0 + lane < n ? pick_key(few[q0 + lane]) : 0, own = pick_key(mine);
+            const int end = n - q0 < 64 ? n - q0 : 64;
+            for (int q = 0; q < end; q += 4) {  // (keys of 0 behind the last count for nothing)
+#pragma unroll
+                for (int u = 0; u < 4; u++) rank += lane_of(key, q + u) > own;
+            }
+        }
+        if (counts && rank < keep) picks[at * keep + rank] = mine;
     }
-    if (counts && rank < keep) picks[at * keep + rank] = mine;
     const int all = __syncthreads_count(counts);
     if (tid >= all && tid < keep) picks[at * keep + tid] = {NONE, -1};
-    if (tid == 0) {
-        const float top4 = __builtin_fmaxf(__builtin_fmaxf(s_max[0], s_max[1]), __builtin_fmaxf(s_max[2], s_max[3]));
-        float s = 0.0f;
-#pragma unroll
-        for (int q = 0; q < WAVES; q++) s += s_sum[q] * __builtin_amdgcn_exp2f((s_max[q] - top4) * LOG2E);
-        sums[at] = {top4, s};
-    }
+    if (tid == 0) sums[at] = {(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), M};
 }
 
-// Two scores of different beams that are nearer than this are compared by sums in 64 bits.  In units of 2^-24, with p_t the softmax: an
-// exponential's argument is rounded twice, sum p_t |x_t - M| (1 + 1) <= 2 log(vocab) + 2 < 45 for vocab < 2^31; v_exp_f32 2; a
-// thread's sum at most 3 + 8, a wave's 6, the workgroup's 4 and its exponential's 2 + 2 |M - M'| p < 4; the rest is in 64 bits.  Below 80
-// of a score's error, 160 of a difference: 1e-5.
-constexpr double NEAR = 1e-5;
+// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).
+__device__ __forceinline__ double exp_of(double x)
+{
+    x = __builtin_fmax(x, -1000.0);
+    const double n = __builtin_rint(x * 1.4426950408889634074);
+    double r = __builtin_fma(n, -0.693147180369123816490, x);  // ln 2 in two parts, the first of 32 bits: n times it is exact
+    r = __builtin_fma(n, -1.90821492927058770002e-10, r);
+    double p = 1.0 / 479001600.0;
+    constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+    for (int i = 0; i < 12; i++) p = __builtin_fma(p, r, c[i]);
+    return __builtin_ldexp(p, (int)n);
+}
+
+constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64;
 constexpr int SOME = 512;  // candidates that are ranked by counting
+constexpr int HELD = 4;    // candidates that a thread has in registers
 
 struct Candidate {
     double s;
     int b, t;
 };
 
+// near: two scores of different beams that are not further apart are compared by sums in 64 bits (near_of).
 template <class T>
-__global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, const Div parts, const Div per_row, const float2* __restrict__ sums,
-                                                            const Pick* __restrict__ picks)
+__global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs a, const Div parts, const Div per_row, double near,
+                                                                 const Sum* __restrict__ sums, const Pick* __restrict__ picks)
 {
     constexpr int B = LLMINT8_BEAM_MAX;
     enum { DEAD, LIVE, ENDED };
-    __shared__ double s_log[B], s_cum[B], s_part[WAVES];  // s_log: of the sum of exp(x - maximum)
-    __shared__ float s_max[B], s_tau[WAVES];
-    __shared__ int s_state[B], s_exact[B], s_redo[B], s_n, s_again;
+    __shared__ double s_log[B], s_cum[B], s_part[PICK_WAVES];  // s_log: of the sum of exp(x - maximum)
+    __shared__ float s_max[B], s_tau[PICK_WAVES];
+    __shared__ int s_state[B], s_n;
+    __shared__ unsigned s_redo;  // a bit for each beam: its sum is to be made again
     __shared__ Candidate some[SOME], top[B];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long long row0 = (long long)blockIdx.x * a.beams;
     const double none = -__builtin_inf();
+    const int C = a.beams * (int)per_row.d;  // the pieces' largest; behind them one candidate for each beam that has ended
+
+    Pick held[HELD];  // (requested before what they hang on; a row without any has whatever the workspace had)
+#pragma unroll
+    for (int u = 0; u < HELD; u++) held[u] = picks[row0 * per_row.d + (tid + u * PICK_THREADS < C ? tid + u * PICK_THREADS : C - 1)];
 
     // sums of the rows
-    for (int b = w; b < a.beams; b += WAVES) {
+    for (int b = w; b < a.beams; b += PICK_WAVES) {
         const long long row = row0 + b;
+        const Sum first = sums[row * parts.d + (lane < (int)parts.d ? lane : 0)];
         const float c = a.scores[row];
         int state = a.ended && a.ended[row] ? ENDED : LIVE;
         bool bad = !(c <= FLT_MAX);  // NaN, +inf
@@ -291,13 +373,12 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, co
         float M = NONE;
         double log_sum = 0.0;
         if (state == LIVE) {
-            for (int q = lane; q < (int)parts.d; q += 64) M = __builtin_fmaxf(M, sums[row * parts.d + q].x);
+            M = lane < (int)parts.d ? first.max : NONE;
+            for (int q = lane + 64; q < (int)parts.d; q += 64) M = __builtin_fmaxf(M, sums[row * parts.d + q].max);
             M = wave_max(M);
-            double s = 0.0;
-            for (int q = lane; q < (int)parts.d; q += 64) {
-                const float2 v = sums[row * parts.d + q];
-                s += (double)v.y * exp((double)v.x - (double)M);
-            }
+            auto one = [&](const Sum& v) { return v.s * exp_of(((double)v.max - (double)M) - Of<T>::Exp::beyond(v.max)); };
+            double s = lane < (int)parts.d ? one(first) : 0.0;
+            for (int q = lane + 64; q < (int)parts.d; q += 64) s += one(sums[row * parts.d + q]);
             s = wave_sum(s);
             // NaN, or +inf (whose distance to itself is NaN), anywhere in the row makes the sum NaN.  Nothing but masked tokens: 0
             if (!(s <= DBL_MAX)) bad = true;
@@ -305,19 +386,17 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, co
             log_sum = log(s);
         }
         if (lane == 0) {
-            s_log[b] = log_sum, s_cum[b] = c, s_max[b] = M, s_state[b] = state, s_exact[b] = state != LIVE;
+            s_log[b] = log_sum, s_cum[b] = c, s_max[b] = M, s_state[b] = state;
             if (bad && a.status) atomicOr(a.status, LLMINT8_BEAM_NOT_FINITE);
         }
     }
     __syncthreads();
 
-    const int C = a.beams * (int)per_row.d;  // the pieces' largest; behind them one for each beam that has ended
-    auto candidate = [&](int c) {
+    auto candidate = [&](int c, Pick p) {
         Candidate r = {none, 0, 0};
         if (c < C) {
             r.b = per_row.quot(c);
             if (s_state[r.b] == LIVE) {
-                const Pick p = picks[row0 * per_row.d + c];
                 r.t = p.t;
                 if (p.t >= 0) r.s = s_cum[r.b] + (((double)p.x - (double)s_max[r.b]) - s_log[r.b]);
             }
@@ -327,34 +406,49 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, co
         }
         return r;
     };
+    auto pick_of = [&](int c) { return picks[row0 * per_row.d + (c < C ? c : C - 1)]; };
+    const int all = C + a.beams;
+    Candidate mine[HELD];
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int u = 0; u < HELD; u++)
+            if (tid + u * PICK_THREADS < all) f(mine[u]);
+        for (int c = tid + HELD * PICK_THREADS; c < all; c += PICK_THREADS) f(candidate(c, pick_of(c)));
+    };
     auto place = [](const Candidate& c) { return (long long)c.b << 32 | c.t; };
 
+    unsigned exact = 0;
+    for (int b = 0; b < a.beams; b++) exact |= s_state[b] == LIVE ? 0u : 1u << b;
+    const unsigned every = a.beams < 32 ? (1u << a.beams) - 1 : ~0u;
     int found;
     for (;;) {
-        if (tid == 0) s_n = 0, s_again = 0;
-        if (tid < B) s_redo[tid] = 0;
+        if (tid == 0) s_n = 0, s_redo = 0;
+#pragma unroll
+        for (int u = 0; u < HELD; u++)
+            if (tid + u * PICK_THREADS < all) mine[u] = candidate(tid + u * PICK_THREADS, held[u]);
         double m = none;
-        for (int c = tid; c < C + a.beams; c += THREADS) m = __builtin_fmax(m, candidate(c).s);
-        const float tau_w = not_above_kth<8>(__double2float_rd(m), a.n_out);
+        each([&](const Candidate& r) { m = __builtin_fmax(m, r.s); });
+        const float tau_w = not_above_kth<14>(__double2float_rd(m), a.n_out);
         if (lane == 0) s_tau[w] = tau_w;
         __syncthreads();
-        // what is picked, and what it may have to be told from
-        const double tau = (double)__builtin_fmaxf(__builtin_fmaxf(s_tau[0], s_tau[1]), __builtin_fmaxf(s_tau[2], s_tau[3])) - 1.01 * NEAR;
-        for (int c = tid; c < C + a.beams; c += THREADS) {
-            const Candidate r = candidate(c);
+        float t = s_tau[0];
+#pragma unroll
+        for (int q = 1; q < PICK_WAVES; q++) t = __builtin_fmaxf(t, s_tau[q]);
+        const double tau = (double)t - 1.01 * near;  // what is picked, and what it may have to be told from
+        each([&](const Candidate& r) {
             if (r.s >= tau && r.s > none) {
                 const int at = atomicAdd(&s_n, 1);
                 if (at < SOME) some[at] = r;
             }
-        }
+        });
         __syncthreads();
         int n = s_n;
-        const bool many = n > SOME, all_exact = !__syncthreads_or(tid < a.beams && !s_exact[tid]);
+        const bool many = n > SOME, all_exact = exact == every;
         if (many && all_exact) {
             Best<double, long long> best(a.n_out);
-            for (int c0 = 64 * w; c0 < C + a.beams; c0 += THREADS) {
+            for (int c0 = 64 * w; c0 < all; c0 += PICK_THREADS) {
                 Candidate r = {none, 0, 0};
-                if (c0 + lane < C + a.beams) r = candidate(c0 + lane);
+                if (c0 + lane < all) r = candidate(c0 + lane, pick_of(c0 + lane));
                 for (;;) {
                     const unsigned long long take = __ballot(r.s > none && best.takes(r.s, place(r)));
                     if (!take) break;
@@ -364,61 +458,72 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, co
                 }
             }
             if (lane < a.n_out) some[w * a.n_out + lane] = {best.v, (int)(best.at >> 32), (int)best.at};
-            n = WAVES * a.n_out;
+            n = PICK_WAVES * a.n_out;
             __syncthreads();
         }
         found = 0;
-        for (int t0 = 0; t0 < n && !(many && !all_exact); t0 += THREADS) {
-            const int t = t0 + tid;
-            const Candidate mine = some[t < n ? t : 0];
-            const bool counts = t < n && mine.s > none;
-            int rank = 0;
-            for (int q = 0; q < n; q++) {
-                const Candidate o = some[q];
-                rank += o.s > mine.s || (o.s == mine.s && place(o) < place(mine));
-            }
-            if (counts && rank < a.n_out) top[rank] = mine;
-            found += __syncthreads_count(counts);
-        }
-        found = found < a.n_out ? found : a.n_out;
-        if (all_exact) break;
-        if (many) {  // too many to compare them
-            if (tid < a.beams && !s_exact[tid]) s_redo[tid] = 1, s_again = 1;
-        } else {
-            for (int t = tid; t < n; t += THREADS) {
-                const Candidate q = some[t];
-                for (int r = 0; r < found; r++) {
-                    const Candidate p = top[r];
-                    if (p.b != q.b && __builtin_fabs(p.s - q.s) < NEAR && !(s_exact[p.b] && s_exact[q.b])) {
-                        s_again = 1;
-                        if (!s_exact[p.b]) s_redo[p.b] = 1;
-                        if (!s_exact[q.b]) s_redo[q.b] = 1;
+        if (!many || all_exact) {
+            const Candidate one = some[tid < n ? tid : 0];
+            const bool counts = tid < n && one.s > none;
+            if (64 * w < n) {
+                int rank = 0;
+                unsigned close = 0;  // beams that have a candidate near this one
+                const long long own = place(one);
+                for (int q0 = 0; q0 < n; q0 += 64) {
+                    const Candidate o = some[q0 + lane < n ? q0 + lane : 0];
+                    const double s = q0 + lane < n ? o.s : none;
+                    const long long at = place(o);
+                    const int end = n - q0 < 64 ? n - q0 : 64;
+                    for (int q = 0; q < end; q += 4) {  // (none behind the last)
+#pragma unroll
+                        for (int u = 0; u < 4; u++) {
+                            const double os = lane_of(s, q + u);
+                            const long long oat = lane_of(at, q + u);
+                            rank += os > one.s || (os == one.s && oat < own);
+                            close |= __builtin_fabs(os - one.s) <= near ? 1u << (oat >> 32 & 31) : 0u;
+                        }
                     }
                 }
+                if (counts && rank < a.n_out) {
+                    top[rank] = one;
+                    close &= ~(1u << one.b);
+                    const unsigned redo = (close & ~exact) | (close && !(exact >> one.b & 1) ? 1u << one.b : 0u);
+                    if (redo) atomicOr(&s_redo, redo);
+                }
             }
+            found = __syncthreads_count(counts);
+            found = found < a.n_out ? found : a.n_out;
+        } else {  // too many to compare them
+            if (tid == 0) s_redo = every & ~exact;
+            __syncthreads();
         }
-        __syncthreads();
-        if (!s_again) break;
+        const unsigned redo = s_redo;
+        if (!redo) break;
         for (int b = 0; b < a.beams; b++) {
-            if (!s_redo[b]) continue;  // the same for all threads
+            if (!(redo >> b & 1)) continue;
             const T* const src = (const T*)a.logits + (row0 + b) * a.ld;
             const double M = s_max[b];
             double s = 0.0;
             int t = tid;
-            for (; t + 7 * THREADS < a.vocab; t += 8 * THREADS) {
+            for (; t + 7 * PICK_THREADS < a.vocab; t += 8 * PICK_THREADS) {
                 T v[8];
 #pragma unroll
-                for (int u = 0; u < 8; u++) v[u] = src[t + u * THREADS];
+                for (int u = 0; u < 8; u++) v[u] = src[t + u * PICK_THREADS];
 #pragma unroll
-                for (int u = 0; u < 8; u++) s += exp((double)v[u] - M);
+                for (int u = 0; u < 8; u++) s += exp_of((double)v[u] - M);
             }
-            for (; t < a.vocab; t += THREADS) s += exp((double)src[t] - M);
+            for (; t < a.vocab; t += PICK_THREADS) s += exp_of((double)src[t] - M);
             s = wave_sum(s);
             if (lane == 0) s_part[w] = s;
             __syncthreads();
-            if (tid == 0) s_log[b] = log((s_part[0] + s_part[1]) + (s_part[2] + s_part[3])), s_exact[b] = 1;
+            if (tid == 0) {
+                s = 0.0;
+                for (int q = 0; q < PICK_WAVES; q++) s += s_part[q];
+                s_log[b] = log(s);
+            }
             __syncthreads();
         }
+        exact |= redo;
     }
     const long long o = (long long)blockIdx.x * a.n_out + tid;
     if (tid < a.n_out) {
@@ -431,38 +536,45 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const BeamArgs a, co
     }
 }
 
+// How far two scores may be from where they are known to be, together.  A sum's relative error in units of 2^-24, with p_t the softmax: an
+// exponential's argument is rounded once (fp32 logits: twice), and log2 e is a quarter of a unit off: sum p_t (max - x_t) times that,
+// where sum p_t (max - x_t) is the entropy less log(sum) and so at most log(vocab); v_exp_f32 2, the sum of a group of 8 3; the rest is in 64 bits.
+double near_of(int vocab, bool f32) { return 2.0 / 16777216.0 * ((f32 ? 2.25 : 1.25) * std::log((double)vocab) + 6.0); }
+
 struct Plan {
     int groups, parts;
 };
 
-// Logits to a thread.
+// Groups of 8 logits to a thread: 8 of them (a piece of 16 384) from two workgroups a compute unit on, 4 from one, else 2.  Larger pieces
+// are fewer starts and fewer picks to join, smaller ones reach more units.  us a call with 2 / 4 / 8, one box: 64 x 8 rows of 131072
+// 55 / 39 / 33, 64 x 4 of 50257 20 / 17 / 18, 32 x 4 15.6 / 14.5 / 14.9, 16 x 4 12.3 / 12.5 / 12.7, 1 x 4 11.0 / 11.4 / 12.2, 8 x 8
+// fp32 rows of 131072, 16 out, 36 / 26 / 21.
 Plan plan(long long rows, int vocab)
 {
     auto parts = [&](int g) { return (int)(((long long)vocab + 8 * THREADS * g - 1) / (8 * THREADS * g)); };
-    for (int g : {8, 4, 2})
-        if (rows * parts(g) >= 1024) return {g, parts(g)};
-    return {1, parts(1)};
+    if (rows * parts(8) >= 512) return {8, parts(8)};
+    if (rows * parts(4) >= 256) return {4, parts(4)};
+    return {2, parts(2)};
 }
 
 template <class T>
-hipError_t launch(const BeamArgs& a, const Plan& p, float2* sums, Pick* picks, hipStream_t st)
+hipError_t launch(const BeamArgs& a, const Plan& p, Sum* sums, Pick* picks, hipStream_t st)
 {
     const int keep = a.n_out;
     const unsigned grid = (unsigned)((long long)a.items * a.beams * p.parts);
     const Div parts(p.parts);
     switch (p.groups) {
-    case 1: beam_scan_kernel<T, 1><<<grid, THREADS, 0, st>>>(a, parts, keep, sums, picks); break;
     case 2: beam_scan_kernel<T, 2><<<grid, THREADS, 0, st>>>(a, parts, keep, sums, picks); break;
     case 4: beam_scan_kernel<T, 4><<<grid, THREADS, 0, st>>>(a, parts, keep, sums, picks); break;
     default: beam_scan_kernel<T, 8><<<grid, THREADS, 0, st>>>(a, parts, keep, sums, picks); break;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    beam_pick_kernel<T><<<(unsigned)a.items, THREADS, 0, st>>>(a, parts, Div(p.parts * keep), sums, picks);
+    beam_pick_kernel<T><<<(unsigned)a.items, PICK_THREADS, 0, st>>>(a, parts, Div(p.parts * keep), near_of(a.vocab, std::is_same<T, float>::value), sums, picks);
     return hipGetLastError();
 }
 
-size_t sums_bytes(long long rows, int parts) { return ((size_t)rows * parts * sizeof(float2) + 255) & ~(size_t)255; }
+size_t sums_bytes(long long rows, int parts) { return ((size_t)rows * parts * sizeof(Sum) + 255) & ~(size_t)255; }
 
 }  // namespace
 
@@ -478,7 +590,7 @@ hipError_t launch_beam_select(const BeamArgs& a, bool f32, void* ws, hipStream_t
 {
     const long long rows = (long long)a.items * a.beams;
     const Plan p = plan(rows, a.vocab);
-    float2* const sums = (float2*)ws;
+    Sum* const sums = (Sum*)ws;
     Pick* const picks = (Pick*)((char*)ws + sums_bytes(rows, p.parts));
     return f32 ? launch<float>(a, p, sums, picks, st) : launch<_Float16>(a, p, sums, picks, st);
 }

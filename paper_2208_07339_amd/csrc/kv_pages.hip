@@ -6,6 +6,8 @@
 // pages first).
 #include "kv_pages.h"
 
+#include "wave.h"
+
 namespace llmint8 {
 
 namespace {
@@ -130,58 +132,59 @@ __global__ void __launch_bounds__(FORK_THREADS) kv_fork_kernel(const ForkArgs a)
 
 constexpr int WIDE = 1024;  // threads of the kernels that go by such a set
 
-// Sum of v over the threads before this one, and over all.
+// Sum of v over the threads before this one, and over all.  TURN: calls one behind the other have 0 and 1 in turn, so that one barrier
+// is enough: what a call writes was read before the barrier of the one before it.
+template <int TURN>
 __device__ __forceinline__ int block_rank(int v, int& total)
 {
-    __shared__ int sums[WIDE / 64];
+    __shared__ int sums[2][WIDE / 64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    int incl = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(incl, d);
-        if (lane >= d) incl += y;
-    }
-    __syncthreads();  // an earlier call's sums have been read
-    if (lane == 63) sums[w] = incl;
+    const int incl = wave_upto(v, 0, [](int a, int b) { return a + b; });
+    if (lane == 63) sums[TURN][w] = incl;
     __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int q = 0; q < WIDE / 64; q++) {
-        before += q < w ? sums[q] : 0;
-        total += sums[q];
-    }
-    return before + incl - v;
+    const int mine = lane < WIDE / 64 ? sums[TURN][lane] : 0;
+    const int upto = wave_upto(mine, 0, [](int a, int b) { return a + b; });
+    total = lane_of(upto, 63);
+    return lane_of(upto - mine, __builtin_amdgcn_readfirstlane(w)) + incl - v;
 }
 
 // Pages as bits, with the number of set ones before each 256.
 struct PageSet {
     unsigned long long* bits;  // [words] page p: bit p % 64 of word p / 64
     int* before;               // [groups]
-    int words, groups, total;
+    int groups, total;
+    static constexpr int BATCH = 10;  // up to 10 240 pages in one
 
-    static __host__ __device__ int words_of(int n_pages) { return (n_pages + 63) / 64; }
     static __host__ __device__ int groups_of(int n_pages) { return (n_pages + 255) / 256; }
     static __host__ size_t bytes(int n_pages) { return (size_t)groups_of(n_pages) * (4 * 8 + 4); }
 
-    // The pages whose count says so.  One wave instruction reads a word's counts; eight are in flight.
-    template <class F>
-    __device__ void make(char* at, const int* refs, int n_pages, F f)
-    {
-        words = words_of(n_pages), groups = groups_of(n_pages);
-        bits = (unsigned long long*)at, before = (int*)(at + (size_t)groups * 32);
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = WIDE / 64;
-        for (int q0 = w; q0 < 4 * groups; q0 += 8 * waves) {
-            int v[8];
+    // The counts of a batch of words, a word to a wave instruction.
+    struct Batch {
+        int v[BATCH];
+        __device__ __forceinline__ void load(const int* refs, int n_pages, int q0)
+        {
+            const int lane = threadIdx.x & 63;
 #pragma unroll
-            for (int u = 0; u < 8; u++) {
-                const int p = 64 * (q0 + u * waves) + lane;
+            for (int u = 0; u < BATCH; u++) {
+                const int p = 64 * (q0 + u * (WIDE / 64)) + lane;
                 v[u] = refs[p < n_pages ? p : n_pages - 1];
             }
+        }
+    };
+    // The pages whose count says so.  batch: the first batch's counts (of words w, w + WIDE / 64, ..., for wave w).  Has a turn of
+    // block_rank, TURN.
+    template <int TURN, class F>
+    __device__ __forceinline__ void make(char* at, const int* refs, int n_pages, Batch& batch, F f)
+    {
+        groups = groups_of(n_pages);
+        bits = (unsigned long long*)at, before = (int*)(at + (size_t)groups * 32);
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = WIDE / 64;
+        for (int q0 = w; q0 < 4 * groups; q0 += BATCH * waves) {
+            if (q0 >= BATCH * waves) batch.load(refs, n_pages, q0);
 #pragma unroll
-            for (int u = 0; u < 8; u++) {
+            for (int u = 0; u < BATCH; u++) {
                 const int q = q0 + u * waves;
-                const unsigned long long m = __ballot(64 * q + lane < n_pages && f(v[u]));
+                const unsigned long long m = __ballot(64 * q + lane < n_pages && f(batch.v[u]));
                 if (lane == 0 && q < 4 * groups) bits[q] = m;
             }
         }
@@ -191,7 +194,7 @@ struct PageSet {
         if (g < groups)
 #pragma unroll
             for (int u = 0; u < 4; u++) c += __popcll(bits[4 * g + u]);
-        const int r = block_rank(c, total);
+        const int r = block_rank<TURN>(c, total);
         if (g < groups) before[g] = r;
         __syncthreads();
     }
@@ -235,6 +238,8 @@ struct PageSet {
 static_assert((LLMINT8_KV_MAX_PAGES + 255) / 256 <= WIDE, "a thread to a group");
 
 // ---- reserve -----------------------------------------------------------------------------------------------------------------
+
+constexpr int GIVEN = 2048;  // pages given out by one call that are listed first; where there are more, each is looked for by itself
 
 struct ReserveArgs {
     int* refs;
@@ -282,7 +287,12 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
     int* const same = (int*)mem;     // [n4] a sequence's first page that others hold, too, and that it is to write; then its place among needs
     int* const need = same + n4;     // [n4] pages that it needs
     int* const behind = need + n4;   // [n4] pages behind the first, of the sequences before
-    char* const set = (char*)(behind + n4);
+    int* const second = behind + n4; // [n4] the first of those
+    int* const given = second + n4;  // [GIVEN] the pages that are given out, in order
+    char* const set = (char*)(given + GIVEN);
+    // Counts for the set of free pages, ahead of what they wait for: where sequences are few, mostly nothing is needed, and they are left
+    // until it is.
+    PageSet::Batch batch;
 
     int entry[2], kept[2];
     NewRows s[2];
@@ -293,6 +303,12 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
         const int b = 2 * tid + u;
         ok[u] = new_rows(a, b < n ? b : n - 1, s[u]);
         if (b >= n) s[u] = {}, ok[u] = true;
+    }
+    const bool ahead = n >= 32;
+    if (ahead) batch.load(a.refs, a.n_pages, tid >> 6);
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const int b = 2 * tid + u;
         const int e = a.pages[(long long)(b < n ? b : n - 1) * a.stride + s[u].first];
         const bool due = s[u].end > s[u].first;
         if (due && e >= a.n_pages) bad_page = 1;
@@ -301,35 +317,48 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
         held[u] = a.refs[entry[u]];
         shared[u] = due && !missing[u] && s[u].len / KV_BLOCK > s[u].old / KV_BLOCK && held[u] > 1;
         kept[u] = s[u].old / KV_BLOCK - s[u].first * per;
-        if (b < n4) same[b] = shared[u] ? entry[u] : -1;
+        if (b < n4) same[b] = shared[u] ? entry[u] : -1, second[b] = s[u].first + 1;
     }
     const int c0 = s[0].end > s[0].first ? s[0].end - s[0].first - 1 : 0, c1 = s[1].end > s[1].first ? s[1].end - s[1].first - 1 : 0;
     int T;  // pages behind the first ones
-    const int r = block_rank(c0 + c1, T);
+    const int r = block_rank<0>(c0 + c1, T);
     if (2 * tid < n4) behind[2 * tid] = r, behind[2 * tid + 1] = r + c0;
-    // (block_rank's barriers: same[] is there)
+    // (block_rank's barrier: same[] is there)
+    // How many want the page that a sequence shares, or -1 where a later one does: a wave to a sequence, its lanes to all of them.
+    const int lane = tid & 63, w = tid >> 6;
+    int x[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) x[k] = 64 * k + lane < n ? same[64 * k + lane] : -1;
+    for (int b0 = w; b0 < n; b0 += WIDE) {
+        const int p = b0 + WIDE / 64 * lane < n ? same[b0 + WIDE / 64 * lane] : -1;
+        for (unsigned long long left = __ballot(p >= 0); left; left &= left - 1) {
+            const int l = __ffsll(left) - 1, b = b0 + WIDE / 64 * l, page = lane_of(p, l);
+            int all = 0;
+            bool later = false;
+            auto look = [&](int y, int q0) {
+                const unsigned long long same_page = __ballot(y == page);
+                all += __popcll(same_page);
+                const int d = b - q0;  // those behind place d
+                later |= d < 0 ? same_page != 0 : d < 63 && same_page >> (d + 1) != 0;
+            };
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (64 * k < n) look(x[k], 64 * k);
+            for (int q0 = 256; q0 < n; q0 += 64) look(q0 + lane < n ? same[q0 + lane] : -1, q0);
+            if (lane == 0) need[b] = later ? -1 : all;
+        }
+    }
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < 2; u++) {
         const int b = 2 * tid + u;
-        copy[u] = false;
-        if (shared[u]) {
-            int all = 0;
-            bool later = false;
-            for (int q = 0; q < n4; q += 4) {
-                const int4 v = *(const int4*)(same + q);
-                const int x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int y = 0; y < 4; y++)
-                    if (x[y] == entry[u]) all++, later |= q + y > b;
-            }
-            copy[u] = all < held[u] || later;
-        }
+        copy[u] = shared[u] && need[b] < held[u];
         if (b < n4) need[b] = missing[u] || copy[u];
     }
     __syncthreads();
 
-    // The sequence that page t of those behind is of, and its place in the table.
-    auto place = [&](int t, NewRows& w) {
+    // The sequence that page t of those behind is of; its place in the tables.
+    auto of = [&](int t) {
         int lo = 0, hi = n;
         while (hi - lo > 1) {
             const int m = (lo + hi) >> 1;
@@ -338,18 +367,16 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
             else
                 hi = m;
         }
-        new_rows(a, lo, w);
-        w.first += 1 + t - behind[lo];
         return lo;
     };
+    auto column = [&](int b, int t) { return second[b] + t - behind[b]; };
     // Those to be replaced are marked in the table, -2 less the page; the others that are needed are -1.
     for (int t = tid; t < T; t += WIDE) {
-        NewRows w;
-        const int b = place(t, w);
-        int* const at = a.pages + (long long)b * a.stride + w.first;
+        const int b = of(t), j = column(b, t);
+        int* const at = a.pages + (long long)b * a.stride + j;
         const int e = *at;
         if ((unsigned)e < (unsigned)a.n_pages) {
-            if ((long long)w.first * per >= w.len / KV_BLOCK || a.refs[e] <= 1) continue;
+            if ((long long)j * per >= a.kv_len[b] / KV_BLOCK || a.refs[e] <= 1) continue;
             *at = -2 - e;
         } else {
             if (e >= 0) bad_page = 1;
@@ -361,56 +388,82 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
 
     const int n0 = 2 * tid < n4 ? need[2 * tid] : 0, n1 = 2 * tid < n4 ? need[2 * tid + 1] : 0;
     int N;
-    const int rank = block_rank(n0 + n1, N);
+    const int rank = block_rank<1>(n0 + n1, N);
     bool late = false, served[2] = {true, true};
     int copies = 0;
     if (N) {
         PageSet free;
-        free.make(set, a.refs, a.n_pages, [](int c) { return c == 0; });
+        if (!ahead) batch.load(a.refs, a.n_pages, tid >> 6);
+        free.make<0>(set, a.refs, a.n_pages, batch, [](int c) { return c == 0; });
+        const bool listed = N <= GIVEN;
+        if (listed) {
+            // a lane to a word, then a wave to each word that has some
+            for (int q0 = w; q0 < 4 * free.groups; q0 += WIDE) {
+                const int q = q0 + WIDE / 64 * lane;
+                unsigned long long m = 0;
+                int r = N;
+                if (q < 4 * free.groups) {
+                    m = free.bits[q];
+                    r = free.before[q >> 2];
+#pragma unroll
+                    for (int y = 0; y < 3; y++) r += y < (q & 3) ? __popcll(free.bits[(q & ~3) + y]) : 0;
+                }
+                for (unsigned long long left = __ballot(m != 0 && r < N); left; left &= left - 1) {
+                    const int l = __ffsll(left) - 1;
+                    const unsigned long long ml = lane_of(m, l);
+                    const int rl = lane_of(r, l) + __popcll(ml & ((1ull << lane) - 1));
+                    if ((ml >> lane & 1) && rl < N) given[rl] = 64 * (q0 + WIDE / 64 * l) + lane;
+                }
+            }
+            __syncthreads();
+        }
+        auto page_of = [&](int r) { return listed ? given[r] : free.find<true>(r); };
         served[0] = n0 == 0 || rank + n0 <= free.total, served[1] = n1 == 0 || rank + n0 + n1 <= free.total;
         late = !served[0] || !served[1];
         int firsts = 0;
         const int f0 = missing[0] || copy[0], f1 = missing[1] || copy[1];
         if (T) {
-            const int before = block_rank(f0 + f1, firsts);
+            const int before = block_rank<1>(f0 + f1, firsts);
             if (2 * tid < n4) same[2 * tid] = served[0] ? before + f0 : -1, same[2 * tid + 1] = served[1] ? before + f0 + f1 : -1;
         }
         bool note[2];
 #pragma unroll
         for (int u = 0; u < 2; u++) note[u] = copy[u] && served[u] && kept[u] > 0;
-        const int k = block_rank(note[0] + note[1], copies);
+        const int k = block_rank<0>(note[0] + note[1], copies);
 #pragma unroll
         for (int u = 0; u < 2; u++) {
             const int b = 2 * tid + u;
             if (!served[u] || !(missing[u] || copy[u])) continue;
-            const int p = free.find<true>(rank + (u ? n0 : 0));
+            const int p = page_of(rank + (u ? n0 : 0));
             a.pages[(long long)b * a.stride + s[u].first] = p;
             a.refs[p] = 1;
             if (copy[u]) atomicSub(&a.refs[entry[u]], 1);
             if (note[u]) a.list[k + (u ? note[0] : 0)] = int4{entry[u], p, kept[u], 0};
         }
-        for (int t0 = 0, base = 0; t0 < T; t0 += WIDE) {
-            const int t = t0 + tid;
-            NewRows w;
-            int* at = nullptr;
-            int b = 0, e = 0;
-            if (t < T) {
-                b = place(t, w);
-                at = a.pages + (long long)b * a.stride + w.first;
-                e = *at;
-            }
-            int all;
-            const int q = base + block_rank(e < 0, all);
-            base += all;
-            if (e >= 0) continue;
-            const int firsts_before = same[b];
-            if (firsts_before >= 0) {
-                const int p = free.find<true>(q + firsts_before);
-                *at = p;
-                a.refs[p] = 1;
-                if (e < -1) atomicSub(&a.refs[-2 - e], 1);
-            } else if (e < -1) {
-                *at = -2 - e;
+        for (int t0 = 0, base = 0; t0 < T; t0 += 2 * WIDE) {
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const int t = t0 + u * WIDE + tid;
+                int* at = nullptr;
+                int b = 0, e = 0;
+                if (t < T) {
+                    b = of(t);
+                    at = a.pages + (long long)b * a.stride + column(b, t);
+                    e = *at;
+                }
+                int all;
+                const int q = base + (u ? block_rank<0>(e < 0, all) : block_rank<1>(e < 0, all));
+                base += all;
+                if (e >= 0) continue;
+                const int firsts_before = same[b];
+                if (firsts_before >= 0) {
+                    const int p = page_of(q + firsts_before);
+                    *at = p;
+                    a.refs[p] = 1;
+                    if (e < -1) atomicSub(&a.refs[-2 - e], 1);
+                } else if (e < -1) {
+                    *at = -2 - e;
+                }
             }
         }
     }
@@ -432,12 +485,14 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
 // ---- compact -----------------------------------------------------------------------------------------------------------------
 
 // One workgroup: the list, and the counts moved along with it.  With U pages in use, the k-th of those from U on goes to the k-th free
-// page below U; there are as many of both.
-__global__ void __launch_bounds__(WIDE) kv_compact_kernel(int* refs, int n_pages, int per, int* used_out, int4* list, int* count)
+// page below U; there are as many of both.  entries > 0: the tables, too, which saves a launch (4 us) where they are small.
+__global__ void __launch_bounds__(WIDE) kv_compact_kernel(int* refs, int n_pages, int per, int* used_out, int4* list, int* count, int* pages, int entries)
 {
     extern __shared__ __align__(16) char mem[];
+    PageSet::Batch batch;
+    batch.load(refs, n_pages, threadIdx.x >> 6);
     PageSet used;
-    used.make(mem, refs, n_pages, [](int c) { return c != 0; });
+    used.make<0>(mem, refs, n_pages, batch, [](int c) { return c != 0; });
     const int U = used.total, below = U < n_pages ? used.rank(U) : U;  // (used pages below U)
     for (int p = U + (int)threadIdx.x; p < n_pages; p += WIDE) {
         if (!(used.bits[p >> 6] >> (p & 63) & 1)) continue;
@@ -446,6 +501,11 @@ __global__ void __launch_bounds__(WIDE) kv_compact_kernel(int* refs, int n_pages
         refs[p] = 0;
         list[k] = int4{p, to, per, 0};
     }
+    if (below < U)
+        for (int i = threadIdx.x; i < entries; i += WIDE) {
+            const int e = pages[i];
+            if (e >= U && e < n_pages && (used.bits[e >> 6] >> (e & 63) & 1)) pages[i] = used.find<false>(used.rank(e) - below);
+        }
     if (threadIdx.x == 0) {
         count[0] = U - below, count[1] = 0;
         if (used_out) *used_out = U;
@@ -558,16 +618,18 @@ hipError_t launch_kv_reserve(const llmint8_kv_pool_t& p, const llmint8_kv_seqs_t
 {
     const ReserveArgs a = {p.refs, p.n_pages, s.pages, s.kv_len, row_start, ready, s.status, s.n_seqs, s.page_stride, Div(p.page_tokens), (int4*)m.pages,
                            m.count, more};
-    kv_reserve_kernel<<<1, WIDE, (size_t)((s.n_seqs + 3) & ~3) * 12 + PageSet::bytes(p.n_pages), st>>>(a);
+    kv_reserve_kernel<<<1, WIDE, (size_t)((s.n_seqs + 3) & ~3) * 16 + GIVEN * 4 + PageSet::bytes(p.n_pages), st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_compact(const llmint8_kv_pool_t& p, const llmint8_kv_seqs_t& s, int* used, const llmint8_kv_moves_t& m, hipStream_t st)
 {
-    kv_compact_kernel<<<1, WIDE, PageSet::bytes(p.n_pages), st>>>(p.refs, p.n_pages, p.page_tokens / KV_BLOCK, used, (int4*)m.pages, m.count);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     const long long entries = (long long)s.n_seqs * s.page_stride;
+    const bool small = entries <= 8 * WIDE;
+    kv_compact_kernel<<<1, WIDE, PageSet::bytes(p.n_pages), st>>>(p.refs, p.n_pages, p.page_tokens / KV_BLOCK, used, (int4*)m.pages, m.count, s.pages,
+                                                                  small ? (int)entries : 0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || small) return e;
     kv_rename_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, st>>>(s.pages, entries, p.n_pages, (const int4*)m.pages, m.count);
     return hipGetLastError();
 }

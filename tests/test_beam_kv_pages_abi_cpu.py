@@ -63,11 +63,11 @@ def test_pool_refusals(L):
         assert call(p=None) == call(s=None) == call(m=None) == INVALID
         assert call(p=pool(refs=None)) == call(p=pool(refs=P + 2)) == call(p=pool(n_pages=0)) == call(p=pool(page_tokens=0)) == INVALID
         assert call(p=pool(page_tokens=-32)) == INVALID
-        assert call(p=pool(page_tokens=48)) == call(p=pool(page_tokens=(1 << 20) + 32)) == call(p=pool(n_pages=(1 << 18) + 1)) == SHAPE
+        assert call(p=pool(page_tokens=48)) == call(p=pool(page_tokens=(1 << 20) + 32)) == call(p=pool(n_pages=(1 << 17) + 1)) == SHAPE
         for name in ("pages", "kv_len", "slots"):
             assert call(s=seqs(**{name: None})) == call(s=seqs(**{name: P + 1})) == INVALID
         assert call(s=seqs(status=2)) == call(s=seqs(n_seqs=0)) == call(s=seqs(page_stride=0)) == INVALID
-        assert call(s=seqs(n_seqs=2049), m=moves(max_pages=4096, max_slots=4096)) == call(s=seqs(page_stride=(1 << 18) + 1)) == SHAPE
+        assert call(s=seqs(n_seqs=2049), m=moves(max_pages=4096, max_slots=4096)) == call(s=seqs(page_stride=(1 << 17) + 1)) == SHAPE
         for name in ("pages", "slots"):
             assert call(m=moves(**{name: None})) == call(m=moves(**{name: P + 8})) == INVALID
         assert call(m=moves(count=None)) == call(m=moves(count=P + 2)) == call(m=moves(max_pages=0)) == call(m=moves(max_slots=0)) == INVALID
@@ -99,8 +99,8 @@ def test_beam_workspace(L):
     f = L.lib().llmint8_beam_select_workspace_bytes
     for items, beams, vocab, n_out in ((1, 4, 50257, 4), (64, 8, 131072, 8), (1, 1, 1, 1), (3, 32, 7, 32), (1000, 4, 32000, 8)):
         n = f(items, beams, vocab, n_out)
-        parts = [-(-vocab // (2048 * g)) for g in (1, 2, 4, 8)]  # pieces of a row: a sum and n_out picks each
-        assert n in [(items * beams * p * 8 + 255) // 256 * 256 + items * beams * p * 8 * n_out + 256 for p in parts]
+        parts = [-(-vocab // (2048 * g)) for g in (2, 4, 8)]  # pieces of a row: a sum and n_out picks each
+        assert n in [(items * beams * p * 16 + 255) // 256 * 256 + items * beams * p * 8 * n_out + 256 for p in parts]
     for refused in ((0, 4, 100, 4), (1, 0, 100, 4), (1, 33, 100, 4), (1, 4, 0, 4), (1, 4, 100, 0), (1, 4, 100, 33), (-1, 4, 100, 4),
                     (2 ** 31 - 1, 32, 2 ** 31 - 1, 32)):
         assert f(*refused) == 0

@@ -216,7 +216,7 @@ def test_reserve_what_cannot_be(torch, L):
     assert s.book.status == BAD_BATCH | BAD_PAGE
 
 
-@pytest.mark.parametrize("n_pages, seed", [(1, 0), (63, 1), (64, 2), (65, 3), (255, 4), (257, 5), (5000, 6), (65536, 7), (262144, 8)])
+@pytest.mark.parametrize("n_pages, seed", [(1, 0), (63, 1), (64, 2), (65, 3), (255, 4), (257, 5), (5000, 6), (10241, 9), (65536, 7), (131072, 8)])
 def test_compact(torch, L, n_pages, seed):
     r = random.Random(seed)
     n, stride = (8, 40) if n_pages < 50000 else (40, 3000)
