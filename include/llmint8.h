@@ -413,7 +413,7 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
  *   ended_out   out  NULL, or [items][n_out]: 1 if the beam had ended or its token is eos, or where there is no continuation; else 0
  *   status      one word, or NULL: LLMINT8_BEAM_NOT_FINITE is set (never cleared) if a row that is read holds NaN or +inf, or a score is
  *                    NaN or +inf.  Such a beam has no continuations
- * beams and n_out up to LLMINT8_BEAM_MAX.  scores_out may be scores and ended_out may be ended, if n_out = beams.
+ * beams and n_out up to LLMINT8_BEAM_MAX, vocab up to 2^30.  scores_out may be scores and ended_out may be ended, if n_out = beams.
  *   ws               llmint8_beam_select_workspace_bytes(items, beams, vocab, n_out) bytes; 0: sizes that are refused           */
 #define LLMINT8_BEAM_MAX 32
 enum { LLMINT8_BEAM_NOT_FINITE = 1 };

@@ -103,6 +103,17 @@ struct Of<_Float16> {
         const h2 m = __builtin_bit_cast(h2, pk_max_f16(pk_max_f16(w[0], w[1]), pk_max_f16(w[2], w[3])));
         return __builtin_fmaxf((float)m[0], (float)m[1]);
     }
+    // v without its first d elements
+    static __device__ __forceinline__ v8 without(v8 v, int d)
+    {
+        u4 w = __builtin_bit_cast(u4, v);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const unsigned upper = (w[q] & 0xffff0000u) | 0xfc00u;
+            w[q] = d >= 2 * q + 2 ? 0xfc00fc00u : d == 2 * q + 1 ? upper : w[q];
+        }
+        return __builtin_bit_cast(v8, w);
+    }
     // sum of exp(x - M), M >= every x: 2^(x log2 e - r) with r = M log2 e rounded, which beyond() makes good.  A conversion, a product and a
     // difference in one instruction, with one rounding.
     struct Exp {
@@ -138,6 +149,12 @@ struct Of<float> {
         for (int e = 1; e < 8; e++) m = __builtin_fmaxf(m, v[e]);
         return m;
     }
+    static __device__ __forceinline__ v8 without(v8 v, int d)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = e < d ? NONE : v[e];
+        return v;
+    }
     struct Exp {  // (products could be beyond fp32's range: the difference first)
         float M;
         __device__ __forceinline__ explicit Exp(float m) : M(m) {}
@@ -159,6 +176,37 @@ __device__ __forceinline__ bool lives(const BeamArgs& a, long long row)
     return c > NONE && c <= FLT_MAX && !(a.ended && a.ended[row]);
 }
 
+// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).  N of them side
+// by side: one alone is a chain of twenty instructions that wait for each other.
+template <int N>
+__device__ __forceinline__ void exp_of(double (&x)[N])
+{
+    constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+    double n[N], p[N];
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        x[e] = __builtin_fmax(x[e], -1000.0);
+        n[e] = __builtin_rint(x[e] * 1.4426950408889634074);
+        x[e] = __builtin_fma(n[e], -0.693147180369123816490, x[e]);  // ln 2 in two parts, the first of 32 bits: n times it is exact
+        x[e] = __builtin_fma(n[e], -1.90821492927058770002e-10, x[e]);
+        p[e] = 1.0 / 479001600.0;
+    }
+#pragma unroll
+    for (int i = 0; i < 12; i++) {
+#pragma unroll
+        for (int e = 0; e < N; e++) p[e] = __builtin_fma(p[e], x[e], c[i]);
+        __builtin_amdgcn_sched_barrier(0);  // (else they are done one after the other, which saves registers)
+    }
+#pragma unroll
+    for (int e = 0; e < N; e++) x[e] = __builtin_ldexp(p[e], (int)n[e]);
+}
+__device__ __forceinline__ double exp_of(double x)
+{
+    double y[1] = {x};
+    exp_of(y);
+    return y[0];
+}
+
 struct Sum {
     double s;  // of the piece's exponentials against max
     float max;
@@ -170,27 +218,28 @@ __device__ __forceinline__ unsigned long long pick_key(const Pick& p)
     return (unsigned long long)order_key(p.x + 0.0f) << 32 | (unsigned)~p.t;
 }
 
-constexpr int SHOWN = 256;    // groups of 8 logits that a piece's largest are picked from
-constexpr int FEW = THREADS;  // those of their logits that are not below the bound: most pieces have two to four times what they keep
+constexpr int SHOWN = 96;  // groups of 8 logits that a wave's largest are picked from
+constexpr int FEW = 128;   // those of their logits that are not below the bound: little more than what is kept, mostly
 
 // G groups of 8 logits to a thread: a wave's lanes side by side, the waves side by side, then the groups, so that a piece is
-// read in runs of 4 KiB (fp16).
+// read in runs of 4 KiB (fp16).  The waves work by themselves until their largest are joined at the end, behind the only barrier.
 template <class T, int G>
 __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, const Div parts, int keep, Sum* __restrict__ sums, Pick* __restrict__ picks)
 {
     typedef Of<T> O;
     typedef typename O::v8 v8;
-    __shared__ float s_max[WAVES], s_tau[WAVES];
+    __shared__ float s_max[WAVES];
     __shared__ double s_sum[WAVES];
-    __shared__ v8 shown[SHOWN];
-    __shared__ int shown_at[SHOWN], s_shown, s_n;
-    __shared__ Pick few[FEW];
+    __shared__ int s_n[WAVES];
+    __shared__ v8 s_shown[WAVES][SHOWN];
+    __shared__ int s_shown_at[WAVES][SHOWN];
+    __shared__ Pick s_few[WAVES][FEW], s_best[WAVES * LLMINT8_BEAM_MAX];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = parts.quot((int)blockIdx.x), part = (int)blockIdx.x - row * (int)parts.d;
     if (!lives(a, row)) return;
     const T* const src = (const T*)a.logits + row * a.ld;
     const int vocab = a.vocab, start = part * (8 * THREADS * G);
-    if (tid == 0) s_shown = 0, s_n = 0;
+    const unsigned long long below = (1ull << lane) - 1;
 
     // First token of group g of a lane.  The row's last piece: a group that reaches past the row's end is its last 8 tokens instead,
     // without those that come before the group.
@@ -204,15 +253,9 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
     if (vocab >= 8) {
 #pragma unroll
         for (int g = 0; g < G; g++) x[g] = O::load(src + first(g, lane));
-        if (last) {
+        if (last)
 #pragma unroll
-            for (int g = 0; g < G; g++) {
-                const int d = meant(g, lane) - first(g, lane);
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (e < d) x[g][e] = (T)NONE;
-            }
-        }
+            for (int g = 0; g < G; g++) x[g] = O::without(x[g], meant(g, lane) - first(g, lane));
     } else {
 #pragma unroll
         for (int g = 0; g < G; g++)
@@ -226,53 +269,68 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
         top[g] = O::largest(x[g]);
         m = __builtin_fmaxf(m, top[g]);
     }
-    const float M_w = wave_max(m), tau_w = not_above_kth<16>(m, keep);
-    if (lane == 0) s_max[w] = M_w, s_tau[w] = tau_w;
-    __syncthreads();
-
-    // Every wave has `keep` logits that are not below its own bound: nothing below the largest bound is wanted.  The groups that have more
-    // go to LDS.
-    const float tau = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s_tau[0], s_tau[1]), __builtin_fmaxf(s_tau[2], s_tau[3])), -FLT_MAX);
-    int mine_shown = 0;
+    // `keep` lanes have a logit that is not below tau: nothing below it is wanted.  The groups that have others go to LDS.
+    const float tau = __builtin_fmaxf(not_above_kth<16>(m, keep), -FLT_MAX);
+    v8* const shown = s_shown[w];
+    int* const shown_at = s_shown_at[w];
+    int groups = 0;
 #pragma unroll
-    for (int g = 0; g < G; g++) mine_shown += top[g] >= tau;
-    int slot = mine_shown ? atomicAdd(&s_shown, mine_shown) : 0;
-#pragma unroll
-    for (int g = 0; g < G; g++)
-        if (top[g] >= tau) {
-            if (slot < SHOWN) shown[slot] = x[g], shown_at[slot] = first(g, lane);
-            slot++;
-        }
+    for (int g = 0; g < G; g++) {
+        const unsigned long long hits = __ballot(top[g] >= tau);
+        const int slot = groups + __popcll(hits & below);
+        if (top[g] >= tau && slot < SHOWN) shown[slot] = x[g], shown_at[slot] = first(g, lane);
+        groups += __popcll(hits);
+    }
 
     // (A mask of the type's lowest value is a logit like others: the reference is the maximum itself, -inf apart.)
-    const float M = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s_max[0], s_max[1]), __builtin_fmaxf(s_max[2], s_max[3])), O::LOWEST);
+    const float M = __builtin_fmaxf(wave_max(m), O::LOWEST);
     const typename O::Exp ex(M);
     double sum = 0.0;
 #pragma unroll
     for (int g = 0; g < G; g++) sum += (double)ex.of(x[g]);
     sum = wave_sum(sum);
-    if (lane == 0) s_sum[w] = sum;
-    __syncthreads();
+    if (lane == 0) s_max[w] = M, s_sum[w] = sum;
 
-    const int groups = s_shown;
+    wave_order();
+    Pick* const few = s_few[w];
+    Pick* const best = s_best + w * keep;
+    int n = 0;
     if (groups <= SHOWN)
-        for (int t0 = 64 * w; t0 < 8 * groups; t0 += THREADS) {
+        for (int t0 = 0; t0 < 8 * groups; t0 += 64) {
             const int t = t0 + lane;
             const float v = t < 8 * groups ? (float)((const T*)shown)[t] : NONE;
             const unsigned long long hits = __ballot(v >= tau);
-            if (!hits) continue;
-            int base = 0;
-            if (v >= tau && !(hits & ((1ull << lane) - 1))) base = atomicAdd(&s_n, __popcll(hits));
-            base = lane_of(base, __ffsll(hits) - 1);
-            const int at = base + __popcll(hits & ((1ull << lane) - 1));
+            const int at = n + __popcll(hits & below);
             if (v >= tau && at < FEW) few[at] = {v, shown_at[t >> 3] + (t & 7)};
+            n += __popcll(hits);
         }
-    __syncthreads();
-    int n = s_n;
-    if (groups > SHOWN || n > FEW) {
-        // Many equal logits, or large ones far apart: each wave shows its own, group by group, best first, so that a group has at most
-        // `keep` to add.
-        Best<float, int> best(keep);
+    if (groups <= SHOWN && n <= FEW) {
+        wave_order();
+        unsigned long long key[FEW / 64];
+        Pick mine[FEW / 64];
+        int rank[FEW / 64] = {};
+#pragma unroll
+        for (int k = 0; k < FEW / 64; k++) {
+            mine[k] = few[64 * k + lane < n ? 64 * k + lane : 0];
+            key[k] = 64 * k + lane < n ? pick_key(mine[k]) : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < FEW / 64; k++)
+            for (int q = 0; q < n - 64 * k && q < 64; q += 4) {  // (keys of 0 behind the last count for nothing)
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    const unsigned long long o = lane_of(key[k], q + u);
+#pragma unroll
+                    for (int y = 0; y < FEW / 64; y++) rank[y] += o > key[y];
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < FEW / 64; k++)
+            if (64 * k + lane < n && rank[k] < keep) best[rank[k]] = mine[k];
+        n = n < keep ? n : keep;
+    } else {
+        // Many equal logits, or large ones far apart: group by group, best first, so that a group has at most `keep` to add.
+        Best<float, int> found(keep);
 #pragma unroll 1
         for (int g = 0; g < G; g++) {
             v8 y = x[0];
@@ -287,53 +345,47 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
                 for (int q = 7; q >= 0; q--)
                     if ((left >> q & 1) && (float)y[q] >= v) v = (float)y[q], e = q;
                 const float V = wave_max(v);
-                if (!(V > best.last)) break;
+                if (!(V > found.last)) break;
                 const int l = __ffsll(__ballot(v == V)) - 1;
                 if (lane == l) left &= ~(1u << e);
-                best.add(V, first(g, l) + __shfl(e, l));
+                found.add(V, first(g, l) + __shfl(e, l));
             }
         }
-        __syncthreads();
-        if (lane < keep) few[w * keep + lane] = {best.v, best.at};
-        n = WAVES * keep;
-        __syncthreads();
+        if (lane < keep) best[lane] = {found.v, found.at};
+        n = __popcll(__ballot(lane < keep && found.v > NONE));
     }
+    if (lane == 0) s_n[w] = n;
+    __syncthreads();
+
     const long long at = (long long)row * parts.d + part;
-    const Pick mine = few[tid < n ? tid : 0];
-    const bool counts = tid < n && mine.x > NONE;
-    if (64 * w < n) {
+    const int all = WAVES * keep;
+    auto listed = [&](int i) { return i < all && i % keep < s_n[i < all ? i / keep : 0]; };
+    if (64 * w < all) {
+        const bool there = listed(tid);
+        const Pick mine = s_best[there ? tid : 0];
+        const unsigned long long own = pick_key(mine);
         int rank = 0;
-        for (int q0 = 0; q0 < n; q0 += 64) {
-            const unsigned long long key = q0 + lane < n ? pick_key(few[q0 + lane]) : 0, own = pick_key(mine);
-            const int end = n - q0 < 64 ? n - q0 : 64;
-            for (int q = 0; q < end; q += 4) {  // (keys of 0 behind the last count for nothing)
+        for (int q0 = 0; q0 < all; q0 += 64) {
+            const unsigned long long key = listed(q0 + lane) ? pick_key(s_best[q0 + lane]) : 0;
+            for (int q = 0; q < all - q0 && q < 64; q += 4) {
 #pragma unroll
                 for (int u = 0; u < 4; u++) rank += lane_of(key, q + u) > own;
             }
         }
-        if (counts && rank < keep) picks[at * keep + rank] = mine;
+        if (there && rank < keep) picks[at * keep + rank] = mine;
     }
-    const int all = __syncthreads_count(counts);
-    if (tid >= all && tid < keep) picks[at * keep + tid] = {NONE, -1};
-    if (tid == 0) sums[at] = {(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), M};
-}
-
-// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).
-__device__ __forceinline__ double exp_of(double x)
-{
-    x = __builtin_fmax(x, -1000.0);
-    const double n = __builtin_rint(x * 1.4426950408889634074);
-    double r = __builtin_fma(n, -0.693147180369123816490, x);  // ln 2 in two parts, the first of 32 bits: n times it is exact
-    r = __builtin_fma(n, -1.90821492927058770002e-10, r);
-    double p = 1.0 / 479001600.0;
-    constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
-#pragma unroll
-    for (int i = 0; i < 12; i++) p = __builtin_fma(p, r, c[i]);
-    return __builtin_ldexp(p, (int)n);
+    const int total = s_n[0] + s_n[1] + s_n[2] + s_n[3];
+    if (tid >= total && tid < keep) picks[at * keep + tid] = {NONE, -1};
+    if (w == WAVES - 1) {
+        const float max4 = __builtin_fmaxf(__builtin_fmaxf(s_max[0], s_max[1]), __builtin_fmaxf(s_max[2], s_max[3])), own = s_max[lane & 3];
+        const double part_sum = lane < WAVES ? s_sum[lane] * exp_of(((double)own - (double)max4) - O::Exp::beyond(own)) : 0.0;
+        const double s = wave_sum(part_sum);
+        if (lane == 0) sums[at] = {s, max4};
+    }
 }
 
 constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64;
-constexpr int SOME = 512;  // candidates that are ranked by counting
+constexpr int SOME = PICK_THREADS;  // candidates that are ranked by counting: one a thread
 constexpr int HELD = 4;    // candidates that a thread has in registers
 
 struct Candidate {
@@ -349,7 +401,7 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
     constexpr int B = LLMINT8_BEAM_MAX;
     enum { DEAD, LIVE, ENDED };
     __shared__ double s_log[B], s_cum[B], s_part[PICK_WAVES];  // s_log: of the sum of exp(x - maximum)
-    __shared__ float s_max[B], s_tau[PICK_WAVES];
+    __shared__ float s_max[B], s_tau[PICK_WAVES], s_share[PICK_WAVES];
     __shared__ int s_state[B], s_n;
     __shared__ unsigned s_redo;  // a bit for each beam: its sum is to be made again
     __shared__ Candidate some[SOME], top[B];
@@ -376,7 +428,7 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
             M = lane < (int)parts.d ? first.max : NONE;
             for (int q = lane + 64; q < (int)parts.d; q += 64) M = __builtin_fmaxf(M, sums[row * parts.d + q].max);
             M = wave_max(M);
-            auto one = [&](const Sum& v) { return v.s * exp_of(((double)v.max - (double)M) - Of<T>::Exp::beyond(v.max)); };
+            auto one = [&](const Sum& v) { return v.s * exp_of((double)v.max - (double)M); };
             double s = lane < (int)parts.d ? one(first) : 0.0;
             for (int q = lane + 64; q < (int)parts.d; q += 64) s += one(sums[row * parts.d + q]);
             s = wave_sum(s);
@@ -428,12 +480,18 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
             if (tid + u * PICK_THREADS < all) mine[u] = candidate(tid + u * PICK_THREADS, held[u]);
         double m = none;
         each([&](const Candidate& r) { m = __builtin_fmax(m, r.s); });
-        const float tau_w = not_above_kth<14>(__double2float_rd(m), a.n_out);
-        if (lane == 0) s_tau[w] = tau_w;
+        // Two bounds below the n_out-th: the largest of the waves' own, and, where many are picked, the smallest of those that each of the
+        // waves that all have candidates has its share above.
+        const float best_of_thread = __double2float_rd(m), tau_w = not_above_kth<14>(best_of_thread, a.n_out);
+        const int full = all / 64 < PICK_WAVES ? all / 64 : PICK_WAVES;
+        const bool shares = a.n_out > 8 && full > 1;
+        const float share_w = shares && w < full ? not_above_kth<14>(best_of_thread, (a.n_out + full - 1) / full) : -NONE;
+        if (lane == 0) s_tau[w] = tau_w, s_share[w] = share_w;
         __syncthreads();
-        float t = s_tau[0];
+        float t = s_tau[0], share = s_share[0];
 #pragma unroll
-        for (int q = 1; q < PICK_WAVES; q++) t = __builtin_fmaxf(t, s_tau[q]);
+        for (int q = 1; q < PICK_WAVES; q++) t = __builtin_fmaxf(t, s_tau[q]), share = __builtin_fminf(share, s_share[q]);
+        if (shares) t = __builtin_fmaxf(t, share);
         const double tau = (double)t - 1.01 * near;  // what is picked, and what it may have to be told from
         each([&](const Candidate& r) {
             if (r.s >= tau && r.s > none) {
@@ -460,6 +518,19 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
             if (lane < a.n_out) some[w * a.n_out + lane] = {best.v, (int)(best.at >> 32), (int)best.at};
             n = PICK_WAVES * a.n_out;
             __syncthreads();
+        }
+        if (!many && n > 128) {
+            // Ranking takes time by their number: the bound again, over all of them, first.
+            const Candidate one = some[tid < n ? tid : 0];
+            const unsigned key = tid < n ? order_key(__double2float_rd(one.s)) : 0u;
+            unsigned at = 0;
+            for (int bit = 31; bit >= 14; bit--)
+                if (__syncthreads_count(key >= (at | 1u << bit)) >= a.n_out) at |= 1u << bit;
+            if (tid == 0) s_n = 0;
+            __syncthreads();
+            if (tid < n && one.s >= (double)key_value(at) - 1.01 * near) some[atomicAdd(&s_n, 1)] = one;
+            __syncthreads();
+            n = s_n;
         }
         found = 0;
         if (!many || all_exact) {
@@ -504,15 +575,22 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
             const T* const src = (const T*)a.logits + (row0 + b) * a.ld;
             const double M = s_max[b];
             double s = 0.0;
-            int t = tid;
-            for (; t + 7 * PICK_THREADS < a.vocab; t += 8 * PICK_THREADS) {
-                T v[8];
+            int t = 8 * tid;
+            for (; t + 24 * PICK_THREADS + 8 <= a.vocab; t += 32 * PICK_THREADS) {
+                typename Of<T>::v8 v[4];
 #pragma unroll
-                for (int u = 0; u < 8; u++) v[u] = src[t + u * PICK_THREADS];
+                for (int u = 0; u < 4; u++) v[u] = Of<T>::load(src + t + 8 * u * PICK_THREADS);
 #pragma unroll
-                for (int u = 0; u < 8; u++) s += exp_of((double)v[u] - M);
+                for (int u = 0; u < 4; u++) {
+                    double y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) y[e] = (double)v[u][e] - M;
+                    exp_of(y);
+                    s += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+                }
             }
-            for (; t < a.vocab; t += PICK_THREADS) s += exp_of((double)src[t] - M);
+            for (; t < a.vocab; t += 8 * PICK_THREADS)
+                for (int e = 0; e < 8 && t + e < a.vocab; e++) s += exp_of((double)src[t + e] - M);
             s = wave_sum(s);
             if (lane == 0) s_part[w] = s;
             __syncthreads();

@@ -54,4 +54,12 @@ __device__ __forceinline__ V wave_reduce(V x, V none, F f)
     return lane_of(wave_upto(x, none, f), 63);
 }
 
+// Between a wave's accesses to memory that its lanes share: they are done in order, and so they are to be compiled.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 }  // namespace llmint8
