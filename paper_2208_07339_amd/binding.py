@@ -25,7 +25,7 @@ SYMBOLS = [
 ]
 
 _lib = None
-_f16 = None  # torch.float16, once torch is there
+_f16 = _i32 = None  # torch.float16 and torch.int32, once torch is there
 
 
 class _KvCache(C.Structure):  # llmint8_kv_cache_t
@@ -71,8 +71,8 @@ def lib():
     # torch first: it ships its own HIP runtime, and the library must bind to the one the tensors and
     # streams it is handed come from (a second runtime loaded earlier sees no device)
     import torch
-    global _f16
-    _f16 = torch.float16
+    global _f16, _i32
+    _f16, _i32 = torch.float16, torch.int32
     L = C.CDLL(LIB_PATH)
     vp, i32, sz, f32 = C.c_void_p, C.c_int, C.c_size_t, C.c_float
     L.llmint8_status_string.restype = C.c_char_p
@@ -157,7 +157,7 @@ def lib():
     L.llmint8_debug_kv_plan_for.argtypes = [batch, i32, i32, i32, i32, C.POINTER(KvPlan)]
     L.llmint8_kv_read.restype = i32
     L.llmint8_kv_read.argtypes = [cache, batch, vp, vp, vp]
-    pool, seqs, moves = C.POINTER(_KvPool), C.POINTER(_KvSeqs), C.POINTER(_KvMoves)
+    pool = seqs = moves = vp  # (of structs: a handle has its struct's address)
     L.llmint8_kv_fork.restype = i32
     L.llmint8_kv_fork.argtypes = [pool, seqs, vp, i32, moves, vp]
     L.llmint8_kv_reserve.restype = i32
@@ -641,16 +641,28 @@ KV_NO_PAGE = 8  # a bit of a status word, as KV_BAD_BATCH
 
 
 def _words(device, *tensors):
-    """The tensors that there are: int32 words, one after the other, on `device`."""
-    torch = _torch()
-    assert device.type == "cuda" and all(t.dtype == torch.int32 and t.is_contiguous() and t.device == device for t in tensors if t is not None)
+    """The tensors that there are: int32 words, one after the other, on the device of that number.  (Numbers, not torch's device
+    objects, whose comparison takes 0.3 us: a step makes some tens of these checks.)"""
+    assert device >= 0
+    for t in tensors:
+        assert t is None or (t.dtype == _i32 and t.is_contiguous() and t.get_device() == device)
 
 
 def _here(device):
-    """The current device's current stream, for tensors on `device`: work on another device's is not what the caller means."""
-    if _torch().cuda.current_device() != device.index:
-        raise Llmint8Error(f"the tensors are on {device}, which is not the current device")
-    return _stream()
+    """The current device's current stream, for tensors on the device of that number: work on another one's is not what the caller
+    means."""
+    if _raw_stream is None:
+        _stream()
+    current = _raw_stream[0]() if _raw_stream is not None else _torch().cuda.current_device()
+    if current != device:
+        raise Llmint8Error(f"the tensors are on device {device}, the current one is {current}")
+    return _raw_stream[1](current) if _raw_stream is not None else _stream()
+
+
+def _held(handle, struct, device):
+    """A handle's C struct, its address (which ctypes takes faster than the struct), and the number of its tensors' device."""
+    for name, value in (("_c", struct), ("_at", C.addressof(struct)), ("_device", device)):
+        object.__setattr__(handle, name, value)
 
 
 @dataclass(frozen=True)
@@ -660,10 +672,11 @@ class KvPool:
     page_tokens: int
 
     def __post_init__(self):
-        _words(self.refs.device, self.refs)
+        lib()  # (fails here if it is missing, and sets torch up)
+        device = self.refs.get_device()
+        _words(device, self.refs)
         assert self.refs.dim() == 1
-        object.__setattr__(self, "_c", _KvPool(_ptr(self.refs), self.refs.numel(), self.page_tokens))
-        lib()
+        _held(self, _KvPool(_ptr(self.refs), self.refs.numel(), self.page_tokens), device)
 
     @staticmethod
     def allocate(n_pages, page_tokens, device="cuda"):
@@ -679,11 +692,12 @@ class KvSeqs:
     status: object = None  # int32 [1], or None
 
     def __post_init__(self):
-        _words(self.pages.device, self.pages, self.kv_len, self.slots, self.status)
+        lib()
+        device = self.pages.get_device()
+        _words(device, self.pages, self.kv_len, self.slots, self.status)
         n, stride = self.pages.shape
-        assert self.kv_len.shape == self.slots.shape == (n,)
-        c = _KvSeqs(_ptr(self.pages), _ptr(self.kv_len), _ptr(self.slots), _ptr(self.status), n, stride)
-        object.__setattr__(self, "_c", c)
+        assert self.kv_len.shape == self.slots.shape == (n,) and (self.status is None or self.status.numel() == 1)
+        _held(self, _KvSeqs(_ptr(self.pages), _ptr(self.kv_len), _ptr(self.slots), _ptr(self.status), n, stride), device)
 
     @staticmethod
     def allocate(n_seqs, most_pages, device="cuda"):
@@ -702,10 +716,11 @@ class KvMoves:
     count: object  # int32 [2]: how many of both
 
     def __post_init__(self):
-        _words(self.pages.device, self.pages, self.slots, self.count)
+        lib()
+        device = self.pages.get_device()
+        _words(device, self.pages, self.slots, self.count)
         assert self.pages.dim() == self.slots.dim() == 2 and self.pages.shape[1] == self.slots.shape[1] == 4 and self.count.numel() == 2
-        c = _KvMoves(_ptr(self.pages), _ptr(self.slots), _ptr(self.count), self.pages.shape[0], self.slots.shape[0])
-        object.__setattr__(self, "_c", c)
+        _held(self, _KvMoves(_ptr(self.pages), _ptr(self.slots), _ptr(self.count), self.pages.shape[0], self.slots.shape[0]), device)
 
     @staticmethod
     def allocate(max_pages, max_slots, device="cuda"):
@@ -713,38 +728,40 @@ class KvMoves:
         return KvMoves(*(_torch().zeros(shape, dtype=_torch().int32, device=device) for shape in ((max(1, max_pages), 4), (max_slots, 4), 2)))
 
 
-def _pool_calls(pool, seqs, moves):
-    assert pool.refs.device == seqs.pages.device == moves.count.device
-    return pool._c, seqs._c
+def _pool_call(f, pool, seqs, moves, *rest):
+    device = seqs._device
+    assert pool._device == moves._device == device
+    _check(f(pool._at, seqs._at, *rest, moves._at, _here(device)))
 
 
 def kv_fork(pool, seqs, parent, moves, grow=0):
     """llmint8_kv_fork: sequence i goes on from sequence parent[i] (int32 [n_seqs]); -1: it ends."""
-    _words(seqs.pages.device, parent)
-    assert parent.numel() == seqs.kv_len.numel()
-    _check(lib().llmint8_kv_fork(*_pool_calls(pool, seqs, moves), _ptr(parent), grow, moves._c, _here(seqs.pages.device)))
+    _words(seqs._device, parent)
+    assert parent.numel() == seqs._c.n_seqs
+    _pool_call(lib().llmint8_kv_fork, pool, seqs, moves, _ptr(parent), grow)
 
 
 def kv_reserve(pool, seqs, row_start, moves, ready=None, more=False):
     """llmint8_kv_reserve: pages for the sequences' next tokens, their own where they write; row_start int32 [n_seqs + 1].
     ready: int32 [n_seqs], or None.  more: the list of a kv_fork before goes on."""
-    _words(seqs.pages.device, row_start, ready)
-    n = seqs.kv_len.numel()
-    assert row_start.numel() == n + 1 and (ready is None or ready.numel() == n)
-    _check(lib().llmint8_kv_reserve(*_pool_calls(pool, seqs, moves), _ptr(row_start), _ptr(ready), int(more), moves._c,
-                                    _here(seqs.pages.device)))
+    _words(seqs._device, row_start, ready)
+    assert row_start.numel() == seqs._c.n_seqs + 1 and (ready is None or ready.numel() == seqs._c.n_seqs)
+    _pool_call(lib().llmint8_kv_reserve, pool, seqs, moves, _ptr(row_start), _ptr(ready), int(more))
 
 
 def kv_compact(pool, seqs, moves, used=None):
     """llmint8_kv_compact: the pages in use become the first ones; used: int32 [1] for their number, or None."""
-    _words(seqs.pages.device, used)
-    _check(lib().llmint8_kv_compact(*_pool_calls(pool, seqs, moves), _ptr(used), moves._c, _here(seqs.pages.device)))
+    _words(seqs._device, used)
+    assert used is None or used.numel() == 1
+    _pool_call(lib().llmint8_kv_compact, pool, seqs, moves, _ptr(used))
 
 
 def kv_copy(cache, moves, status=None):
     """llmint8_kv_copy: the moves' copies in one layer's cache."""
-    _words(cache.codes.device, moves.count, status)
-    _check(lib().llmint8_kv_copy(cache._c, moves._c, _ptr(status), _here(cache.codes.device)))
+    device = moves._device
+    _words(device, status)
+    assert cache.codes.get_device() == device and (status is None or status.numel() == 1)
+    _check(lib().llmint8_kv_copy(cache._c, moves._at, _ptr(status), _here(device)))
 
 
 # ---- beam search -----------------------------------------------------------------------
@@ -764,25 +781,30 @@ def beam_select(logits, scores, beams, n_out=None, ended=None, eos=-1, ws=None, 
     [items * beams], ended int32 [items * beams] or None -> (scores fp32, parent, token, ended int32), each [items, n_out]
     (n_out: beams if None).  out: those four; its scores may be `scores` and its ended `ended` where n_out is beams."""
     torch = _torch()
+    lib()
     rows, vocab = logits.shape
-    dev = logits.device
+    device = logits.get_device()
     n_out = beams if n_out is None else n_out
-    assert beams >= 1 and rows % beams == 0 and logits.is_cuda and logits.dtype in (torch.float16, torch.float32)
+    f32 = logits.dtype == torch.float32
+    assert device >= 0 and beams >= 1 and rows % beams == 0 and (f32 or logits.dtype == _f16)
     assert logits.stride(1) == 1 or vocab == 1
-    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.device == dev
-    assert ended is None or ended.numel() == rows
+    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.get_device() == device
+    assert (ended is None or ended.numel() == rows) and (status is None or status.numel() == 1)
     items = rows // beams
     if out is None:
-        out = (torch.empty((items, n_out), device=dev), *(torch.empty((items, n_out), dtype=torch.int32, device=dev) for _ in range(3)))
-    _words(dev, *out[1:], ended, status)
-    assert out[0].dtype == torch.float32 and out[0].is_contiguous() and out[0].device == dev
-    assert all(t is None or t.numel() == items * n_out for t in out)
+        out = (torch.empty((items, n_out), device=logits.device),
+               *(torch.empty((items, n_out), dtype=torch.int32, device=logits.device) for _ in range(3)))
+    best, parent, token, over = out
+    _words(device, parent, token, over, ended, status)
+    assert best.dtype == torch.float32 and best.is_contiguous() and best.get_device() == device
+    n = items * n_out
+    assert best.numel() == parent.numel() == token.numel() == n and (over is None or over.numel() == n)
     if ws is None:
-        ws = beam_select_workspace(items, beams, vocab, n_out, dev)
-    assert ws.buf.device == dev
-    _check(lib().llmint8_beam_select(_ptr(logits), logits.stride(0) if rows > 1 else vocab, int(logits.dtype == torch.float32), items,
-                                     beams, vocab, _ptr(scores), _ptr(ended), eos, n_out, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
-                                     _ptr(out[3]), _ptr(status), _ptr(ws.buf), ws.nbytes, _here(dev)))
+        ws = beam_select_workspace(items, beams, vocab, n_out, logits.device)
+    assert ws.buf.get_device() == device
+    _check(lib().llmint8_beam_select(_ptr(logits), logits.stride(0) if rows > 1 else vocab, int(f32), items, beams, vocab, _ptr(scores),
+                                     _ptr(ended), eos, n_out, _ptr(best), _ptr(parent), _ptr(token), _ptr(over), _ptr(status),
+                                     _ptr(ws.buf), ws.nbytes, _here(device)))
     return out
 
 
