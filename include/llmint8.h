@@ -389,7 +389,8 @@ int llmint8_kv_reserve(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *s
                        int more, const llmint8_kv_moves_t *moves, llmint8_stream_t stream);
 
 /* Moves pages so that the U pages in use are pages 0 .. U-1: those above go, in order, to the free ones below, in order; tables and
- * refs follow.  used: NULL, or one word that gets U.  moves: a new list; max_pages >= n_pages / 2.                              */
+ * refs follow, and what a program itself holds pages by has to (moves says how).  used: NULL, or one word that gets U.  moves: a new
+ * list; max_pages >= n_pages / 2.                                                                                              */
 int llmint8_kv_compact(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *seqs, int32_t *used,
                        const llmint8_kv_moves_t *moves, llmint8_stream_t stream);
 
@@ -413,7 +414,8 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
  *   ended_out   out  NULL, or [items][n_out]: 1 if the beam had ended or its token is eos, or where there is no continuation; else 0
  *   status      one word, or NULL: LLMINT8_BEAM_NOT_FINITE is set (never cleared) if a row that is read holds NaN or +inf, or a score is
  *                    NaN or +inf.  Such a beam has no continuations
- * beams and n_out up to LLMINT8_BEAM_MAX, vocab up to 2^30.  scores_out may be scores and ended_out may be ended, if n_out = beams.
+ * beams and n_out up to LLMINT8_BEAM_MAX, vocab up to 2^30, and below 2^24 pieces of 4 096 logits or more in all.  scores_out may be
+ * scores and ended_out may be ended, if n_out = beams.
  *   ws               llmint8_beam_select_workspace_bytes(items, beams, vocab, n_out) bytes; 0: sizes that are refused           */
 #define LLMINT8_BEAM_MAX 32
 enum { LLMINT8_BEAM_NOT_FINITE = 1 };

@@ -41,7 +41,8 @@ __device__ __forceinline__ float key_value(unsigned k)
     return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// A value that is not above the k-th largest of the wave's 64, and not far below: the key's last LOW bits are left open.
+// A value that is not above the k-th largest of the wave's 64, and not far below: the key's last LOW bits are left open.  (Two bits at a time,
+// three counts that do not wait for each other: more code and 0.5 us slower in both kernels.)
 template <int LOW>
 __device__ __forceinline__ float not_above_kth(float x, int k)
 {
@@ -176,35 +177,18 @@ __device__ __forceinline__ bool lives(const BeamArgs& a, long long row)
     return c > NONE && c <= FLT_MAX && !(a.ended && a.ended[row]);
 }
 
-// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).  N of them side
-// by side: one alone is a chain of twenty instructions that wait for each other.
-template <int N>
-__device__ __forceinline__ void exp_of(double (&x)[N])
-{
-    constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
-    double n[N], p[N];
-#pragma unroll
-    for (int e = 0; e < N; e++) {
-        x[e] = __builtin_fmax(x[e], -1000.0);
-        n[e] = __builtin_rint(x[e] * 1.4426950408889634074);
-        x[e] = __builtin_fma(n[e], -0.693147180369123816490, x[e]);  // ln 2 in two parts, the first of 32 bits: n times it is exact
-        x[e] = __builtin_fma(n[e], -1.90821492927058770002e-10, x[e]);
-        p[e] = 1.0 / 479001600.0;
-    }
-#pragma unroll
-    for (int i = 0; i < 12; i++) {
-#pragma unroll
-        for (int e = 0; e < N; e++) p[e] = __builtin_fma(p[e], x[e], c[i]);
-        __builtin_amdgcn_sched_barrier(0);  // (else they are done one after the other, which saves registers)
-    }
-#pragma unroll
-    for (int e = 0; e < N; e++) x[e] = __builtin_ldexp(p[e], (int)n[e]);
-}
+// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).
 __device__ __forceinline__ double exp_of(double x)
 {
-    double y[1] = {x};
-    exp_of(y);
-    return y[0];
+    x = __builtin_fmax(x, -1000.0);
+    const double n = __builtin_rint(x * 1.4426950408889634074);
+    double r = __builtin_fma(n, -0.693147180369123816490, x);  // ln 2 in two parts, the first of 32 bits: n times it is exact
+    r = __builtin_fma(n, -1.90821492927058770002e-10, r);
+    constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+    double p = 1.0 / 479001600.0;
+#pragma unroll
+    for (int i = 0; i < 12; i++) p = __builtin_fma(p, r, c[i]);
+    return __builtin_ldexp(p, (int)n);
 }
 
 struct Sum {
@@ -223,6 +207,9 @@ constexpr int FEW = 128;   // those of their logits that are not below the bound
 
 // G groups of 8 logits to a thread: a wave's lanes side by side, the waves side by side, then the groups, so that a piece is
 // read in runs of 4 KiB (fp16).  The waves work by themselves until their largest are joined at the end, behind the only barrier.
+// Bound by HBM and by vector instructions, about equally: 512 rows of 131072 fp16 logits, 134 MB, in 27 us, 5.0 TB/s (a read: 6.6); a
+// wave's 4 096 logits are 64 exponentials of four turns and some 500 other instructions.  Where rows are few, by latency: the parts
+// of a workgroup's 5 to 8 us are the logits (1 to 2), maximum and bound (1), exponentials (0.8), the join (1).
 template <class T, int G>
 __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, const Div parts, int keep, Sum* __restrict__ sums, Pick* __restrict__ picks)
 {
@@ -386,14 +373,16 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
 
 constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64;
 constexpr int SOME = PICK_THREADS;  // candidates that are ranked by counting: one a thread
-constexpr int HELD = 4;    // candidates that a thread has in registers
 
 struct Candidate {
     double s;
     int b, t;
 };
 
-// near: two scores of different beams that are not further apart are compared by sums in 64 bits (near_of).
+// A workgroup to an item: latency, 5 to 7 us of dependent steps (2.4 of them the launch): sums of the rows, scores and a bound, the
+// candidates above it, their ranks.  near: two scores of different beams that are not further apart are compared by sums in 64 bits
+// (near_of), which takes 20 us for each row of 131072.  That is rare: fp16 logits are a grid, and where two beams' sums differ by about a
+// multiple of its step, candidates of both can be near each other (1 of 192 items with 32 picked of 8 beams).
 template <class T>
 __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs a, const Div parts, const Div per_row, double near,
                                                                  const Sum* __restrict__ sums, const Pick* __restrict__ picks)
@@ -410,9 +399,8 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
     const double none = -__builtin_inf();
     const int C = a.beams * (int)per_row.d;  // the pieces' largest; behind them one candidate for each beam that has ended
 
-    Pick held[HELD];  // (requested before what they hang on; a row without any has whatever the workspace had)
-#pragma unroll
-    for (int u = 0; u < HELD; u++) held[u] = picks[row0 * per_row.d + (tid + u * PICK_THREADS < C ? tid + u * PICK_THREADS : C - 1)];
+    const Pick held = picks[row0 * per_row.d + (tid < C ? tid : C - 1)];  // (requested before what it hangs on; a row without any has whatever
+                                                                          // the workspace had)
 
     // sums of the rows
     for (int b = w; b < a.beams; b += PICK_WAVES) {
@@ -460,12 +448,10 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
     };
     auto pick_of = [&](int c) { return picks[row0 * per_row.d + (c < C ? c : C - 1)]; };
     const int all = C + a.beams;
-    Candidate mine[HELD];
-    auto each = [&](auto f) {
-#pragma unroll
-        for (int u = 0; u < HELD; u++)
-            if (tid + u * PICK_THREADS < all) f(mine[u]);
-        for (int c = tid + HELD * PICK_THREADS; c < all; c += PICK_THREADS) f(candidate(c, pick_of(c)));
+    Candidate mine;
+    auto each = [&](auto f) {  // (one of a thread's candidates is kept in registers: the code of four took 0.5 us longer)
+        if (tid < all) f(mine);
+        for (int c = tid + PICK_THREADS; c < all; c += PICK_THREADS) f(candidate(c, pick_of(c)));
     };
     auto place = [](const Candidate& c) { return (long long)c.b << 32 | c.t; };
 
@@ -475,9 +461,7 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
     int found;
     for (;;) {
         if (tid == 0) s_n = 0, s_redo = 0;
-#pragma unroll
-        for (int u = 0; u < HELD; u++)
-            if (tid + u * PICK_THREADS < all) mine[u] = candidate(tid + u * PICK_THREADS, held[u]);
+        if (tid < all) mine = candidate(tid, held);
         double m = none;
         each([&](const Candidate& r) { m = __builtin_fmax(m, r.s); });
         // Two bounds below the n_out-th: the largest of the waves' own, and, where many are picked, the smallest of those that each of the
@@ -581,13 +565,9 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
 #pragma unroll
                 for (int u = 0; u < 4; u++) v[u] = Of<T>::load(src + t + 8 * u * PICK_THREADS);
 #pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    double y[8];
+                for (int u = 0; u < 4; u++)
 #pragma unroll
-                    for (int e = 0; e < 8; e++) y[e] = (double)v[u][e] - M;
-                    exp_of(y);
-                    s += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-                }
+                    for (int e = 0; e < 8; e++) s += exp_of((double)v[u][e] - M);
             }
             for (; t < a.vocab; t += 8 * PICK_THREADS)
                 for (int e = 0; e < 8 && t + e < a.vocab; e++) s += exp_of((double)src[t + e] - M);
@@ -625,8 +605,9 @@ struct Plan {
 
 // Groups of 8 logits to a thread: 8 of them (a piece of 16 384) from two workgroups a compute unit on, 4 from one, else 2.  Larger pieces
 // are fewer starts and fewer picks to join, smaller ones reach more units.  us a call with 2 / 4 / 8, one box: 64 x 8 rows of 131072
-// 55 / 39 / 33, 64 x 4 of 50257 20 / 17 / 18, 32 x 4 15.6 / 14.5 / 14.9, 16 x 4 12.3 / 12.5 / 12.7, 1 x 4 11.0 / 11.4 / 12.2, 8 x 8
-// fp32 rows of 131072, 16 out, 36 / 26 / 21.
+// 58 / 41 / 35, 64 x 4 of 50257 21 / 17.5 / 16.4, 32 x 4 15.9 / 14.5 / 14.1, 16 x 4 11.8 / 11.4 / 11.5, 1 x 4 9.9 / 10.1 / 10.8, 8 x 8
+// fp32 rows of 131072, 16 picked, 37 / 26 / 23; where one beam of eight lives, which only the device knows, the smaller are ahead: 48 x 8
+// of 65024 15.4 / 16.6 / 18.0.
 Plan plan(long long rows, int vocab)
 {
     auto parts = [&](int g) { return (int)(((long long)vocab + 8 * THREADS * g - 1) / (8 * THREADS * g)); };
