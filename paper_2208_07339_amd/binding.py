@@ -25,7 +25,7 @@ SYMBOLS = [
 ]
 
 _lib = None
-_f16 = _i32 = None  # torch.float16 and torch.int32, once torch is there
+_f16 = _f32 = _i32 = None  # torch.float16, torch.float32 and torch.int32, once torch is there
 
 
 class _KvCache(C.Structure):  # llmint8_kv_cache_t
@@ -71,8 +71,8 @@ def lib():
     # torch first: it ships its own HIP runtime, and the library must bind to the one the tensors and
     # streams it is handed come from (a second runtime loaded earlier sees no device)
     import torch
-    global _f16, _i32
-    _f16, _i32 = torch.float16, torch.int32
+    global _f16, _f32, _i32
+    _f16, _f32, _i32 = torch.float16, torch.float32, torch.int32
     L = C.CDLL(LIB_PATH)
     vp, i32, sz, f32 = C.c_void_p, C.c_int, C.c_size_t, C.c_float
     L.llmint8_status_string.restype = C.c_char_p
@@ -780,31 +780,30 @@ def beam_select(logits, scores, beams, n_out=None, ended=None, eos=-1, ws=None, 
     """llmint8_beam_select: logits [items * beams, vocab] fp16 or fp32 (rows may be slices of wider ones), scores fp32
     [items * beams], ended int32 [items * beams] or None -> (scores fp32, parent, token, ended int32), each [items, n_out]
     (n_out: beams if None).  out: those four; its scores may be `scores` and its ended `ended` where n_out is beams."""
-    torch = _torch()
-    lib()
+    f = lib().llmint8_beam_select
     rows, vocab = logits.shape
-    device = logits.get_device()
-    n_out = beams if n_out is None else n_out
-    f32 = logits.dtype == torch.float32
-    assert device >= 0 and beams >= 1 and rows % beams == 0 and (f32 or logits.dtype == _f16)
-    assert logits.stride(1) == 1 or vocab == 1
-    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.get_device() == device
-    assert (ended is None or ended.numel() == rows) and (status is None or status.numel() == 1)
+    ld, one = logits.stride()
+    device, kind = logits.get_device(), logits.dtype
+    if n_out is None:
+        n_out = beams
+    assert device >= 0 and (kind == _f16 or kind == _f32) and (one == 1 or vocab == 1) and beams >= 1 and rows % beams == 0
     items = rows // beams
     if out is None:
+        torch = _torch()
         out = (torch.empty((items, n_out), device=logits.device),
                *(torch.empty((items, n_out), dtype=torch.int32, device=logits.device) for _ in range(3)))
     best, parent, token, over = out
-    _words(device, parent, token, over, ended, status)
-    assert best.dtype == torch.float32 and best.is_contiguous() and best.get_device() == device
-    n = items * n_out
-    assert best.numel() == parent.numel() == token.numel() == n and (over is None or over.numel() == n)
     if ws is None:
         ws = beam_select_workspace(items, beams, vocab, n_out, logits.device)
-    assert ws.buf.get_device() == device
-    _check(lib().llmint8_beam_select(_ptr(logits), logits.stride(0) if rows > 1 else vocab, int(f32), items, beams, vocab, _ptr(scores),
-                                     _ptr(ended), eos, n_out, _ptr(best), _ptr(parent), _ptr(token), _ptr(over), _ptr(status),
-                                     _ptr(ws.buf), ws.nbytes, _here(device)))
+    given = ((scores, _f32, rows), (best, _f32, items * n_out), (parent, _i32, items * n_out), (token, _i32, items * n_out),
+             (over, _i32, items * n_out), (ended, _i32, rows), (status, _i32, 1))
+    for t, dtype, n in given:
+        if t is not None:
+            assert t.dtype == dtype and t.numel() == n and t.is_contiguous() and t.get_device() == device
+    buf = ws.buf
+    assert buf.get_device() == device
+    _check(f(logits.data_ptr(), ld if rows > 1 else vocab, kind == _f32, items, beams, vocab, scores.data_ptr(), _ptr(ended), eos, n_out,
+             best.data_ptr(), parent.data_ptr(), token.data_ptr(), _ptr(over), _ptr(status), buf.data_ptr(), buf.numel(), _here(device)))
     return out
 
 
