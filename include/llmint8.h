@@ -402,8 +402,8 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
 /* ---- beam search ---------------------------------------------------------------------------------------------------------
  * The n_out best continuations of each item's beams: beam b of an item (row item * beams + b) with token t has the score
  * scores[row] + logits[row][t] - log(sum over t of exp(logits[row][t])); the largest are given, in falling order, equal ones in order
- * of (b, t).  The order is that of these numbers in 64 bits (sums of 32 bits are made again in 64 where two beams' scores are
- * too near to tell); scores_out is rounded to fp32.
+ * of b, a beam's in order of falling logits and then of t.  The order is that of these numbers in 64 bits (sums of 32 bits are made
+ * again in 64 where two beams' scores are too near to tell); scores_out is rounded to fp32.
  *   logits      in   fp16, or with f32 != 0 fp32; row r at r * ld, ld >= vocab.  -inf: a token that cannot follow
  *   scores      in   [items * beams] fp32.  -inf: a beam that there is not; its logits are not read
  *   ended       in   NULL, or [items * beams]: not 0: the beam has ended: its only continuation is the token eos, its score stays as
@@ -414,10 +414,11 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
  *   ended_out   out  NULL, or [items][n_out]: 1 if the beam had ended or its token is eos, or where there is no continuation; else 0
  *   status      one word, or NULL: LLMINT8_BEAM_NOT_FINITE is set (never cleared) if a row that is read holds NaN or +inf, or a score is
  *                    NaN or +inf.  Such a beam has no continuations
- * beams and n_out up to LLMINT8_BEAM_MAX, vocab up to 2^30, and below 2^24 pieces of 4 096 logits or more in all.  scores_out may be
+ * beams and n_out up to LLMINT8_BEAM_MAX, vocab up to LLMINT8_BEAM_MAX_VOCAB, and below 2^24 pieces of 4 096 logits or more in all.  scores_out may be
  * scores and ended_out may be ended, if n_out = beams.
  *   ws               llmint8_beam_select_workspace_bytes(items, beams, vocab, n_out) bytes; 0: sizes that are refused           */
 #define LLMINT8_BEAM_MAX 32
+#define LLMINT8_BEAM_MAX_VOCAB (1 << 27)
 enum { LLMINT8_BEAM_NOT_FINITE = 1 };
 size_t llmint8_beam_select_workspace_bytes(int items, int beams, int vocab, int n_out);
 int llmint8_beam_select(const void *logits, int64_t ld, int f32, int items, int beams, int vocab, const float *scores,

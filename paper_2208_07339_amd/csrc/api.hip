@@ -746,7 +746,7 @@ int llmint8_kv_copy(const llmint8_kv_cache_t* c, const llmint8_kv_moves_t* m, in
 
 static bool beam_sizes(int items, int beams, int vocab, int n_out)
 {
-    return items >= 1 && beams >= 1 && vocab >= 1 && vocab <= (1 << 30) && n_out >= 1 && beams <= LLMINT8_BEAM_MAX && n_out <= LLMINT8_BEAM_MAX &&
+    return items >= 1 && beams >= 1 && vocab >= 1 && vocab <= LLMINT8_BEAM_MAX_VOCAB && n_out >= 1 && beams <= LLMINT8_BEAM_MAX && n_out <= LLMINT8_BEAM_MAX &&
            items < (1 << 23) && (int64_t)items * beams * beam_parts(items * (int64_t)beams, vocab) < (1ll << 24);  // (launches of < 2^32 threads)
 }
 

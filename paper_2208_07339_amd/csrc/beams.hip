@@ -374,9 +374,20 @@ __global__ void __launch_bounds__(THREADS) beam_scan_kernel(const BeamArgs a, co
 constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64;
 constexpr int SOME = PICK_THREADS;  // candidates that are ranked by counting: one a thread
 
+// A score and its place among equal ones: the beam, then larger logits (64 bits of a score need not tell fp32 logits apart), then the
+// token.
 struct Candidate {
     double s;
-    int b, t;
+    unsigned long long at;
+
+    static constexpr int TOKEN_BITS = 27;
+    static_assert(LLMINT8_BEAM_MAX <= 32 && LLMINT8_BEAM_MAX_VOCAB <= 1 << TOKEN_BITS, "5 bits of beam, 32 of logit, 27 of token");
+    __device__ __forceinline__ void place(int b, float x, int t)
+    {
+        at = (unsigned long long)b << (32 + TOKEN_BITS) | (unsigned long long)~order_key(x + 0.0f) << TOKEN_BITS | (unsigned)t;
+    }
+    __device__ __forceinline__ int beam() const { return (int)(at >> (32 + TOKEN_BITS)); }
+    __device__ __forceinline__ int token() const { return (int)at & ((1 << TOKEN_BITS) - 1); }
 };
 
 // A workgroup to an item: latency, 5 to 7 us of dependent steps (2.4 of them the launch): sums of the rows, scores and a bound, the
@@ -433,16 +444,16 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
     __syncthreads();
 
     auto candidate = [&](int c, Pick p) {
-        Candidate r = {none, 0, 0};
+        Candidate r = {none, 0};
         if (c < C) {
-            r.b = per_row.quot(c);
-            if (s_state[r.b] == LIVE) {
-                r.t = p.t;
-                if (p.t >= 0) r.s = s_cum[r.b] + (((double)p.x - (double)s_max[r.b]) - s_log[r.b]);
+            const int b = per_row.quot(c);
+            if (s_state[b] == LIVE && p.t >= 0) {
+                r.place(b, p.x, p.t);
+                r.s = s_cum[b] + (((double)p.x - (double)s_max[b]) - s_log[b]);
             }
-        } else {
-            r.b = c - C, r.t = a.eos;
-            if (s_state[r.b] == ENDED) r.s = s_cum[r.b];
+        } else if (s_state[c - C] == ENDED) {
+            r.place(c - C, 0.0f, a.eos);
+            r.s = s_cum[c - C];
         }
         return r;
     };
@@ -453,7 +464,6 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
         if (tid < all) f(mine);
         for (int c = tid + PICK_THREADS; c < all; c += PICK_THREADS) f(candidate(c, pick_of(c)));
     };
-    auto place = [](const Candidate& c) { return (long long)c.b << 32 | c.t; };
 
     unsigned exact = 0;
     for (int b = 0; b < a.beams; b++) exact |= s_state[b] == LIVE ? 0u : 1u << b;
@@ -487,19 +497,19 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
         int n = s_n;
         const bool many = n > SOME, all_exact = exact == every;
         if (many && all_exact) {
-            Best<double, long long> best(a.n_out);
+            Best<double, unsigned long long> best(a.n_out);
             for (int c0 = 64 * w; c0 < all; c0 += PICK_THREADS) {
-                Candidate r = {none, 0, 0};
+                Candidate r = {none, 0};
                 if (c0 + lane < all) r = candidate(c0 + lane, pick_of(c0 + lane));
                 for (;;) {
-                    const unsigned long long take = __ballot(r.s > none && best.takes(r.s, place(r)));
+                    const unsigned long long take = __ballot(r.s > none && best.takes(r.s, r.at));
                     if (!take) break;
                     const int l = __ffsll(take) - 1;
-                    best.add(__shfl(r.s, l), __shfl(place(r), l));
+                    best.add(__shfl(r.s, l), __shfl(r.at, l));
                     if (lane == l) r.s = none;
                 }
             }
-            if (lane < a.n_out) some[w * a.n_out + lane] = {best.v, (int)(best.at >> 32), (int)best.at};
+            if (lane < a.n_out) some[w * a.n_out + lane] = {best.v, best.at};
             n = PICK_WAVES * a.n_out;
             __syncthreads();
         }
@@ -523,26 +533,25 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
             if (64 * w < n) {
                 int rank = 0;
                 unsigned close = 0;  // beams that have a candidate near this one
-                const long long own = place(one);
+                const unsigned long long own = one.at;
+                const int beam = one.beam();
                 for (int q0 = 0; q0 < n; q0 += 64) {
                     const Candidate o = some[q0 + lane < n ? q0 + lane : 0];
                     const double s = q0 + lane < n ? o.s : none;
-                    const long long at = place(o);
                     const int end = n - q0 < 64 ? n - q0 : 64;
                     for (int q = 0; q < end; q += 4) {  // (none behind the last)
 #pragma unroll
                         for (int u = 0; u < 4; u++) {
-                            const double os = lane_of(s, q + u);
-                            const long long oat = lane_of(at, q + u);
-                            rank += os > one.s || (os == one.s && oat < own);
-                            close |= __builtin_fabs(os - one.s) <= near ? 1u << (oat >> 32 & 31) : 0u;
+                            const Candidate other = {lane_of(s, q + u), lane_of(o.at, q + u)};
+                            rank += other.s > one.s || (other.s == one.s && other.at < own);
+                            close |= __builtin_fabs(other.s - one.s) <= near ? 1u << other.beam() : 0u;
                         }
                     }
                 }
                 if (counts && rank < a.n_out) {
                     top[rank] = one;
-                    close &= ~(1u << one.b);
-                    const unsigned redo = (close & ~exact) | (close && !(exact >> one.b & 1) ? 1u << one.b : 0u);
+                    close &= ~(1u << beam);
+                    const unsigned redo = (close & ~exact) | (close && !(exact >> beam & 1) ? 1u << beam : 0u);
                     if (redo) atomicOr(&s_redo, redo);
                 }
             }
@@ -588,9 +597,9 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
         const bool there = tid < found;
         const Candidate c = top[there ? tid : 0];
         a.scores_out[o] = there ? (float)c.s : NONE;
-        a.parent[o] = there ? (int)(row0 + c.b) : -1;
-        a.token[o] = there ? c.t : a.eos < 0 ? 0 : a.eos;
-        if (a.ended_out) a.ended_out[o] = !there || s_state[c.b] == ENDED || c.t == a.eos;
+        a.parent[o] = there ? (int)row0 + c.beam() : -1;
+        a.token[o] = there ? c.token() : a.eos < 0 ? 0 : a.eos;
+        if (a.ended_out) a.ended_out[o] = !there || s_state[c.beam()] == ENDED || c.token() == a.eos;
     }
 }
 

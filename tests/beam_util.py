@@ -13,7 +13,7 @@ def select(logits, scores, beams, n_out, ended=None, eos=-1):
     bad = False
     got = [np.full((rows // beams, n_out), fill, dtype) for fill, dtype in ((-np.inf, np.float64), (-1, np.int64), (max(eos, 0), np.int64), (1, np.int64))]
     for item in range(rows // beams):
-        s, b, t, done = [], [], [], []
+        s, b, t, done, logit = [], [], [], [], []
         for row in range(item * beams, (item + 1) * beams):
             c = float(scores[row])
             if np.isnan(c) or c == np.inf:
@@ -21,7 +21,7 @@ def select(logits, scores, beams, n_out, ended=None, eos=-1):
             elif c == -np.inf:
                 pass
             elif ended is not None and ended[row]:
-                s.append([c]), b.append([row]), t.append([eos]), done.append([1])
+                s.append([c]), b.append([row]), t.append([eos]), done.append([1]), logit.append([0.0])
             elif np.isnan(x[row]).any() or (x[row] == np.inf).any():
                 bad = True
             else:
@@ -30,11 +30,11 @@ def select(logits, scores, beams, n_out, ended=None, eos=-1):
                     v = x[row][some]
                     top = v.max()
                     s.append(c + ((v - top) - np.log(np.exp(v - top).sum())))  # (a constant added to a row changes nothing)
-                    b.append(np.full(len(some), row)), t.append(some), done.append((some == eos).astype(np.int64))
+                    b.append(np.full(len(some), row)), t.append(some), done.append((some == eos).astype(np.int64)), logit.append(v)
         if not s:
             continue
-        s, b, t, done = (np.concatenate(y) for y in (s, b, t, done))
-        best = np.lexsort((t, b, -s))[:n_out]
+        s, b, t, done, logit = (np.concatenate(y) for y in (s, b, t, done, logit))
+        best = np.lexsort((t, -logit, b, -s))[:n_out]
         for out, y in zip(got, (s, b, t, done)):
             out[item, :len(best)] = y[best]
     return got[0], got[1], got[2], got[3], bad

@@ -102,7 +102,7 @@ def test_beam_workspace(L):
         parts = [-(-vocab // (2048 * g)) for g in (2, 4, 8)]  # pieces of a row: a sum and n_out picks each
         assert n in [(items * beams * p * 16 + 255) // 256 * 256 + items * beams * p * 8 * n_out + 256 for p in parts]
     for refused in ((0, 4, 100, 4), (1, 0, 100, 4), (1, 33, 100, 4), (1, 4, 0, 4), (1, 4, 100, 0), (1, 4, 100, 33), (-1, 4, 100, 4),
-                    (2 ** 31 - 1, 32, 2 ** 31 - 1, 32), (1, 1, 2 ** 30 + 1, 1), (2 ** 23, 1, 10, 1), (2 ** 17, 32, 131072, 8)):
+                    (2 ** 31 - 1, 32, 2 ** 31 - 1, 32), (1, 1, 2 ** 27 + 1, 1), (2 ** 23, 1, 10, 1), (2 ** 17, 32, 131072, 8)):
         assert f(*refused) == 0
 
 

@@ -117,6 +117,18 @@ def test_orders_that_leave_many_candidates(torch, L, vocab, items, f32):
             check(torch, L, logits, scores, 3, n_out)
 
 
+@pytest.mark.parametrize("f32", [False, True])
+def test_zeros_of_either_sign_and_the_smallest_numbers(torch, L, f32):
+    """-0 and 0 are equal; denormal numbers are not."""
+    dtype = torch.float32 if f32 else torch.float16
+    for vocab in (9, 3000, 40000):
+        t = torch.arange(vocab, device="cuda")
+        tiny = torch.finfo(dtype).smallest_normal / 4
+        for x in (torch.where(t % 2 == 0, -0.0, 0.0), torch.where(t % 3 == 1, 0.0, -0.0), torch.where(t % 5 == 4, tiny, -0.0), (t % 7 - 6) * tiny):
+            logits = x.to(dtype).repeat(4, 1)
+            check(torch, L, logits, torch.tensor([-1.0, -1.0, -2.0, -0.5], device="cuda"), 2, 5)
+
+
 def test_beams_that_are_alike(torch, L):
     """Equal rows with equal scores: the lower beam first.  As many candidates as there are, all of one score."""
     for beams, vocab, n_out in ((4, 5000, 8), (32, 600, 32), (32, 40000, 32), (2, 9, 20)):
@@ -190,6 +202,17 @@ def test_more_than_2_31_logits(torch, L):
     want = np.array([18.0 - lse[1], 20.0 - lse[0], 19.0 - lse[0]])
     assert (np.abs(s[-1].double().cpu().numpy() - want) <= LSE_ERROR + 2.0 ** -24 * np.abs(want)).all()
     assert parent[0].tolist() == [0, 0, 0] and token[0].tolist() == [0, 1, 2]
+
+
+def test_the_largest_vocabulary(torch, L):
+    vocab = 2 ** 27  # LLMINT8_BEAM_MAX_VOCAB
+    logits = torch.zeros((2, vocab), dtype=torch.float16, device="cuda")
+    logits[1, vocab - 1], logits[0, vocab - 2] = 25.0, 24.0
+    s, parent, token, _ = L.beam_select(logits, torch.zeros(2, device="cuda"), 2, 3)
+    assert parent.tolist() == [[1, 0, 0]] and token.tolist() == [[vocab - 1, vocab - 2, 0]]
+    lse = [np.log(vocab - 1 + np.exp(24.0)), np.log(vocab - 1 + np.exp(25.0))]
+    want = np.array([25.0 - lse[1], 24.0 - lse[0], -lse[0]])
+    assert (np.abs(s[0].double().cpu().numpy() - want) <= LSE_ERROR + 2.0 ** -24 * np.abs(want)).all()
 
 
 def test_streams_and_replays(torch, L):
