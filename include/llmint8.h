@@ -403,7 +403,8 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
  * The n_out best continuations of each item's beams: beam b of an item (row item * beams + b) with token t has the score
  * scores[row] + logits[row][t] - log(sum over t of exp(logits[row][t])); the largest are given, in falling order, equal ones in order
  * of b, a beam's in order of falling logits and then of t.  The order is that of these numbers in 64 bits (sums of 32 bits are made
- * again in 64 where two beams' scores are too near to tell); scores_out is rounded to fp32.
+ * again in 64 where two beams' scores are too near to tell); scores_out is rounded to fp32: -inf, with its parent and token, where a
+ * score is below fp32's range (logits further apart than the largest number, or a large negative score over masked ones).
  *   logits      in   fp16, or with f32 != 0 fp32; row r at r * ld, ld >= vocab.  -inf: a token that cannot follow
  *   scores      in   [items * beams] fp32.  -inf: a beam that there is not; its logits are not read
  *   ended       in   NULL, or [items * beams]: not 0: the beam has ended: its only continuation is the token eos, its score stays as

@@ -36,9 +36,11 @@ __device__ __forceinline__ unsigned order_key(float x)
     const unsigned u = __builtin_bit_cast(unsigned, x);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(unsigned k)
+// The value of a key whose last bits are cleared; -inf where that is none: -inf's key without its last bits, and any below, would be a NaN,
+// which nothing is above.
+__device__ __forceinline__ float bound_of(unsigned k)
 {
-    return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
+    return k < order_key(-FLT_MAX) ? NONE : __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
 // A value that is not above the k-th largest of the wave's 64, and not far below: the key's last LOW bits are left open.  (Two bits at a time,
@@ -53,7 +55,7 @@ __device__ __forceinline__ float not_above_kth(float x, int k)
         const unsigned c = at | (1u << bit);
         if (__popcll(__ballot(key >= c)) >= k) at = c;
     }
-    return at >= order_key(-FLT_MAX) ? key_value(at) : NONE;  // (below that: -inf, its last bits cleared)
+    return bound_of(at);
 }
 
 __device__ __forceinline__ float wave_max(float x)
@@ -522,7 +524,8 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const BeamArgs 
                 if (__syncthreads_count(key >= (at | 1u << bit)) >= a.n_out) at |= 1u << bit;
             if (tid == 0) s_n = 0;
             __syncthreads();
-            if (tid < n && one.s >= (double)key_value(at) - 1.01 * near) some[atomicAdd(&s_n, 1)] = one;
+            // (scores below fp32's range are -inf here and are all kept)
+            if (tid < n && one.s >= (double)bound_of(at) - 1.01 * near) some[atomicAdd(&s_n, 1)] = one;
             __syncthreads();
             n = s_n;
         }
