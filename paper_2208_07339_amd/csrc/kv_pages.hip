@@ -422,6 +422,22 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
         }
         auto page_of = [&](int r) { return listed ? given[r] : free.find<true>(r); };
         served[0] = n0 == 0 || rank + n0 <= free.total, served[1] = n1 == 0 || rank + n0 + n1 <= free.total;
+        if (N > free.total) {
+            // A sequence that was to keep a page, since all others that hold it would get another, must not write to blocks of one that gets
+            // none: then it is not served, either.  Those others are before it, and behind a sequence that is not served none gets a page, so
+            // only what needs no page is left out here: no other sequence's pages change by it.  need[]: full blocks of those that go on
+            // holding the page same[].  (Looked for by a thread each: calls that find the pool empty may take longer.)
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (2 * tid < n4) need[2 * tid + u] = copy[u] && !served[u] ? s[u].old / KV_BLOCK : -1;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (shared[u] && !copy[u])
+                    for (int q = 0; q < 2 * tid + u; q++)
+                        if (same[q] == entry[u] && need[q] > s[u].old / KV_BLOCK) served[u] = false;
+            // (same[] is written to behind block_rank's barrier)
+        }
         late = !served[0] || !served[1];
         int firsts = 0;
         const int f0 = missing[0] || copy[0], f1 = missing[1] || copy[1];
