@@ -379,10 +379,10 @@ int llmint8_kv_fork(const llmint8_kv_pool_t *pool, const llmint8_kv_seqs_t *seqs
  * hold too, is replaced by one of the sequence's own; the first such page's blocks before the tokens' are noted in moves.  (If all
  * that hold a page are to be given another for their first tokens, the last sequence keeps it.)  Pages that are given back here
  * are given out by later calls only.
- * Too few free pages: a sequence that with those before it needs more than there are gets none, its table stays as it is, and
- * status has LLMINT8_KV_NO_PAGE.  llmint8_kv_append must not have such a sequence: it would write to pages that others hold.  The same
- * goes for a sequence that was to keep a page, if one of the others that hold it does not get another and has blocks full that the
- * sequence's tokens would be written to (it is the shorter one).
+ * Too few free pages: a sequence that with those before it needs more than there are gets none, its table stays as it is (but an
+ * entry below n_pages - 2^31 may become -1), and status has LLMINT8_KV_NO_PAGE.  llmint8_kv_append must not have such a sequence: it
+ * would write to pages that others hold.  The same goes for a sequence that was to keep a page, if one of the others that hold it
+ * does not get another and has blocks full that the sequence's tokens would be written to (the sequence is the shorter one).
  *   ready  NULL, or [n_seqs]: kv_len of the sequences that have their pages, 0 of the others and of those whose
  *          row_start or kv_len cannot be (LLMINT8_KV_BAD_BATCH): as the kv_len of a batch it leaves these out
  *   more   0: moves is a new list; else the list of a llmint8_kv_fork before goes on

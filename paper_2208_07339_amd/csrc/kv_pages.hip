@@ -373,17 +373,20 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
         return lo;
     };
     auto column = [&](int b, int t) { return second[b] + t - behind[b]; };
-    // Those to be replaced are marked in the table, -2 less the page; the others that are needed are -1.
+    // Those to be replaced are marked in the table, by MARK + page; the others that are needed are what they were, no page of the pool (but for
+    // those that look like marks): a sequence that is not served keeps its table.
+    constexpr int MARK = -2147483647 - 1;
+    auto marked = [&](int e) { return e < MARK + a.n_pages; };
     for (int t = tid; t < T; t += WIDE) {
         const int b = of(t), j = column(b, t);
         int* const at = a.pages + (long long)b * a.stride + j;
         const int e = *at;
         if ((unsigned)e < (unsigned)a.n_pages) {
             if ((long long)j * per >= a.kv_len[b] / KV_BLOCK || a.refs[e] <= 1) continue;
-            *at = -2 - e;
+            *at = MARK + e;
         } else {
             if (e >= 0) bad_page = 1;
-            if (e != -1) *at = -1;
+            if (marked(e)) *at = -1;
         }
         atomicAdd(&need[b], 1);
     }
@@ -471,17 +474,18 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
                     e = *at;
                 }
                 int all;
-                const int q = base + (u ? block_rank<0>(e < 0, all) : block_rank<1>(e < 0, all));
+                const bool needed = (unsigned)e >= (unsigned)a.n_pages;
+                const int q = base + (u ? block_rank<0>(needed, all) : block_rank<1>(needed, all));
                 base += all;
-                if (e >= 0) continue;
+                if (!needed) continue;
                 const int firsts_before = same[b];
                 if (firsts_before >= 0) {
                     const int p = page_of(q + firsts_before);
                     *at = p;
                     a.refs[p] = 1;
-                    if (e < -1) atomicSub(&a.refs[-2 - e], 1);
-                } else if (e < -1) {
-                    *at = -2 - e;
+                    if (marked(e)) atomicSub(&a.refs[e - MARK], 1);
+                } else if (marked(e)) {
+                    *at = e - MARK;
                 }
             }
         }
