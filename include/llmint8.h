@@ -339,7 +339,8 @@ int llmint8_kv_read(const llmint8_kv_cache_t *cache, const llmint8_kv_batch_t *b
  *
  *   moves: what is to be copied.  pages [max_pages][4]: from, to, blocks (the first ones of the page, of every head), 0;
  *          slots [max_slots][4]: from, to, first position, positions;  count [2]: how many of both.  pages and slots start on 16
- *          bytes.  A call says below which capacity it is refused.                                                            */
+ *          bytes.  A call says below which capacity it is refused.  A call that begins a new list drops what the list before still
+ *          had to copy: fork, copy, compact, copy, reserve, copy; or fork, reserve with more = 1, copy.                        */
 #define LLMINT8_KV_MAX_SEQS 2048
 #define LLMINT8_KV_MAX_PAGES (1 << 17)
 enum { LLMINT8_KV_NO_PAGE = 8 };
@@ -405,8 +406,10 @@ int llmint8_kv_copy(const llmint8_kv_cache_t *cache, const llmint8_kv_moves_t *m
  * The n_out best continuations of each item's beams: beam b of an item (row item * beams + b) with token t has the score
  * scores[row] + logits[row][t] - log(sum over t of exp(logits[row][t])); the largest are given, in falling order, equal ones in order
  * of b, a beam's in order of falling logits and then of t.  The order is that of these numbers in 64 bits (sums of 32 bits are made
- * again in 64 where two beams' scores are too near to tell); scores_out is rounded to fp32: -inf, with its parent and token, where a
- * score is below fp32's range (logits further apart than the largest number, or a large negative score over masked ones).
+ * again in 64 where two beams' scores are too near to tell).  scores_out is rounded to fp32, and off by the error of its beam's sum
+ * besides, where that was not made again: at most 2^-24 (1.25 ln(vocab) + 6), 1.3e-6 for 131 072 tokens (fp32 logits: 2.25 for 1.25,
+ * 2.0e-6).  A score below fp32's range (logits further apart than the largest number, or a large negative score over masked ones)
+ * is -inf there, with its parent and token; as the next call's score that is a beam that there is not.
  *   logits      in   fp16, or with f32 != 0 fp32; row r at r * ld, ld >= vocab.  -inf: a token that cannot follow
  *   scores      in   [items * beams] fp32.  -inf: a beam that there is not; its logits are not read
  *   ended       in   NULL, or [items * beams]: not 0: the beam has ended: its only continuation is the token eos, its score stays as

@@ -179,13 +179,15 @@ __device__ __forceinline__ bool lives(const BeamArgs& a, long long row)
     return c > NONE && c <= FLT_MAX && !(a.ended && a.ended[row]);
 }
 
-// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).
+// exp(x) for x <= 0, within some units of 1e-16: x = n ln 2 + r, |r| <= ln 2 / 2, the series to r^12 (the rest is below 2e-16).  ln 2 in two
+// parts, as Cody and Waite reduce arguments (Software Manual for the Elementary Functions, 1980): floor(2^32 ln 2) / 2^32, which n times is
+// exact, and what is left.
 __device__ __forceinline__ double exp_of(double x)
 {
     x = __builtin_fmax(x, -1000.0);
     const double n = __builtin_rint(x * 1.4426950408889634074);
-    double r = __builtin_fma(n, -0.693147180369123816490, x);  // ln 2 in two parts, the first of 32 bits: n times it is exact
-    r = __builtin_fma(n, -1.90821492927058770002e-10, r);
+    double r = __builtin_fma(n, -2977044471.0 / 4294967296.0, x);
+    r = __builtin_fma(n, -0x1.a39ef35793c76p-33, r);
     constexpr double c[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
     double p = 1.0 / 479001600.0;
 #pragma unroll
@@ -209,7 +211,7 @@ constexpr int FEW = 128;   // those of their logits that are not below the bound
 
 // G groups of 8 logits to a thread: a wave's lanes side by side, the waves side by side, then the groups, so that a piece is
 // read in runs of 4 KiB (fp16).  The waves work by themselves until their largest are joined at the end, behind the only barrier.
-// Bound by HBM and by vector instructions, about equally: 512 rows of 131072 fp16 logits, 134 MB, in 27 us, 5.0 TB/s (a read: 6.6); a
+// Bound by HBM and by vector instructions, about equally: 512 rows of 131072 fp16 logits, 134 MB, in 27 to 28 us, 4.9 TB/s (a read: 6.6); a
 // wave's 4 096 logits are 64 exponentials of four turns and some 500 other instructions.  Where rows are few, by latency: the parts
 // of a workgroup's 5 to 8 us are the logits (1 to 2), maximum and bound (1), exponentials (0.8), the join (1).
 template <class T, int G>
@@ -392,7 +394,7 @@ struct Candidate {
     __device__ __forceinline__ int token() const { return (int)at & ((1 << TOKEN_BITS) - 1); }
 };
 
-// A workgroup to an item: latency, 5 to 7 us of dependent steps (2.4 of them the launch): sums of the rows, scores and a bound, the
+// A workgroup to an item: latency, 5 to 8 us of dependent steps (2.4 of them the launch): sums of the rows, scores and a bound, the
 // candidates above it, their ranks.  near: two scores of different beams that are not further apart are compared by sums in 64 bits
 // (near_of), which takes 20 us for each row of 131072.  That is rare: fp16 logits are a grid, and where two beams' sums differ by about a
 // multiple of its step, candidates of both can be near each other (1 of 192 items with 32 picked of 8 beams).

@@ -34,8 +34,8 @@ struct ForkArgs {
 
 // Workgroup 0: lengths, slots and the list of ring copies.  The others: `columns` columns of all tables each, which makes the exchange
 // of rows one in place: a workgroup has read its columns before it writes them.  A row's pages change their counts by the row's
-// children less one.  Latency: three dependent round trips (parents and entries; counts and entries written).  2.7 us for 4 tables of
-// 21 entries, 4.5 for 128 of 79, 5.3 for 16 of 2 302; a kernel that does nothing takes 2.4.
+// children less one.  Latency: three dependent round trips (parents and entries; counts and entries written).  2.3 us for 4 tables of
+// 21 entries, about what a kernel that does nothing takes, 4.5 for 128 of 79, 5.3 for 16 of 2 302.
 __global__ void __launch_bounds__(FORK_THREADS) kv_fork_kernel(const ForkArgs a)
 {
     extern __shared__ int lds[];
@@ -280,9 +280,9 @@ __device__ __forceinline__ bool new_rows(const ReserveArgs& a, int b, NewRows& s
 // A page is missing, or is to be replaced, or stays: that is settled for all before anything is changed, so that counts are those of
 // the call's start.  Needs are ranked (sequences in order, a sequence's pages in order) and the r-th gets the r-th free page, which a
 // set of the free pages in LDS finds.
-// Latency: rows and lengths, entries, counts, the free pages' counts: four round trips, and the barriers of four rankings.  4 us for 128
-// sequences (1 279 pages) of which none needs any, 9.2 where they all get a page of their own (943 pages), 11 for 940 pages of 20 prompts
-// (9 405 pages).
+// Latency: rows and lengths, entries, counts, the free pages' counts: four round trips, and the barriers of four rankings.  4.2 us for 128
+// sequences (1 279 pages) of which none needs any, 9.5 where they all get a page of their own (943 pages), 11 for 940 pages of 20 prompts
+// (9 405 pages).  Where a call gives thousands, by one workgroup's instructions: 14 for 2 048 pages of 4 prompts, 75 for 20 480 of 20.
 __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
 {
     extern __shared__ __align__(16) char mem[];
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(WIDE) kv_reserve_kernel(const ReserveArgs a)
 
 // One workgroup: the list, and the counts moved along with it.  With U pages in use, the k-th of those from U on goes to the k-th free
 // page below U; there are as many of both.  entries > 0: the tables, too, which saves a launch (4 us) where they are small.
-// Latency, as above: 4.3 us with 48 tables of 42 entries and 1 589 pages.
+// Latency, as above: 4.5 us with 48 tables of 42 entries and 1 589 pages, 8.7 with 25 005 pages.
 __global__ void __launch_bounds__(WIDE) kv_compact_kernel(int* refs, int n_pages, int per, int* used_out, int4* list, int* count, int* pages, int entries)
 {
     extern __shared__ __align__(16) char mem[];
@@ -586,8 +586,8 @@ __device__ __forceinline__ void move(V* __restrict__ dst, const V* __restrict__ 
 }
 
 // A workgroup to an entry and a head (of a ring also to keys or values), one after the other: how many there are only the device knows.
-// V: what a row of the ring is moved in.  Bound by HBM: 133 MB read and written in two calls of 15.4 us each (4.3 TB/s), 130 MB in one of
-// 26.4 (4.9 TB/s); a large copy by itself reaches 4.8 TB/s.
+// V: what a row of the ring is moved in.  Bound by HBM: 133 MB read and written in two calls of 15.1 us each (4.4 TB/s), 130 MB in one of
+// 26.6 (4.9 TB/s); a large copy by itself reaches 4.8 TB/s.
 template <class V>
 __global__ void __launch_bounds__(256) kv_copy_kernel(const CopyArgs a)
 {
